@@ -408,6 +408,73 @@ int32_t rptq_kv_quant(const void* x, int64_t T, int32_t d, const void* table, in
 int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* table, int32_t bits, void* out,
                         void* stream);
 
+/* ---- the key/value cache in pages: written, read back and attended to as codes ----------------
+ * A serving program keeps the keys and values of many sequences of different lengths in one
+ * pool of pages.  A page holds page_size tokens of one tensor (keys or values) of one layer:
+ *    [d / 128 blocks][page_size tokens][128 codes]
+ * i.e. for every 128 consecutive positions of the per-head cluster order (rptq_kv_quant's
+ * order) one row of 16 * bits bytes per token, four groups of 32 codes in the formats above.
+ * d = n_kv_heads * head_dim channels, a multiple of 128; page_size a power of two, 16 to 4096;
+ * rptq_kv_page_bytes(d, page_size, bits) bytes per page, page i at i times that.  Slot
+ * i * page_size + r is token row r of page i.  1 <= n_pages < 2^31.  The tables are
+ * rptq_kv_tables' of the key and the value tensor.
+ *
+ * rptq_kv_quant_paged: keys and values of T new tokens into the cache, one launch.  Row t is
+ * quantized as by rptq_kv_quant and stored at slot slots[t]; a row whose slot is negative or
+ * not below n_pages * page_size is stored nowhere.  No two rows of a call, nor of calls that
+ * overlap in time, may have the same slot (it then holds codes of either, byte by byte).
+ *   k, v    device bf16, rows of d channels in the original channel order, ld_k and ld_v
+ *           channels apart (>= d, a multiple of 8): they may be columns of a wider tensor
+ *   slots   device int64 [T]
+ *   k_pages, v_pages  device, n_pages * rptq_kv_page_bytes(d, page_size, bits) bytes each
+ * As for rptq_ln_quant a NaN or infinity gives unspecified codes for its channel, no more.
+ *
+ * rptq_kv_dequant_paged: the rows at T slots (any, also one several times) as bf16 in the
+ * original channel order: channel perm[j] of row t is rptq_kv_dequant's value at position j,
+ * bit for bit.  A row whose slot lies outside the pages is left as it was in k and v.
+ *
+ * rptq_attend_paged: attention of one new token of each of B sequences over the cache.  Query
+ * head h reads key/value head h / (n_q_heads / n_kv_heads).  With key and value codes k_tj, v_tj
+ * at position j of the head, their tables' (src, s, z) and x_hat = s (code - z) unrounded:
+ *     a_t = scale * sum_j q[src_j] * s^K_j (k_tj - z^K_j)
+ *     out[src_j] = sum_t exp(a_t) s^V_j (v_tj - z^V_j) / sum_t exp(a_t)
+ *     lse = log(sum_t exp(a_t))                                      (natural logarithm)
+ * over the tokens t < lens[b] whose page is there: token t of sequence b is row t % page_size
+ * of page page_table[b, t / page_size], and a number outside 0 .. n_pages - 1 stands for a page
+ * that is not there (its tokens take no part).  lens[b] below 0 counts as 0, beyond
+ * pages_per_seq * page_size as that.  A sequence without tokens gets zeros, and -infinity as lse.
+ *   q       device bf16 [B, n_q_heads * head_dim], original channel order, rows ld_q apart
+ *   head_dim  32, 64, 128 or 256; n_q_heads a multiple of n_kv_heads
+ *   page_table device int32 [B, pages_per_seq], rows ld_page_table apart;  lens device int32 [B]
+ *   out     device out [B, n_q_heads * head_dim], original channel order, rows ld_out apart,
+ *           out_dtype RPTQ_DTYPE_BF16 or RPTQ_DTYPE_F32
+ *   lse     device out fp32 [B, n_q_heads], or NULL
+ *   workspace device, rptq_attend_paged_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim) bytes; nothing
+ *           in it has to be cleared or kept between calls; calls that overlap in time need one each
+ * Sums and softmax statistics are fp32 or exact integers; a sequence's last bits may depend on
+ * the other lengths of the call (they decide where sequences are split).  A NaN or infinity in q, or a
+ * score beyond fp32, makes its head's output NaN.
+ * pages_per_seq * page_size <= 2^30; strides (ld_*) are >= the row and, but for the page table's, multiples of 8.
+ *
+ * All three are asynchronous on `stream`, allocate nothing and may be recorded into a graph after the first
+ * call on the device.  Device pointers are 16-byte aligned, slots 8-byte, page_table and lens 4-byte.
+ */
+#define RPTQ_MIN_PAGE_SIZE 16
+#define RPTQ_MAX_PAGE_SIZE 4096
+size_t rptq_kv_page_bytes(int32_t d, int32_t page_size, int32_t bits);
+int32_t rptq_kv_quant_paged(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T, int32_t d,
+                            const void* k_table, const void* v_table, int32_t bits, const int64_t* slots,
+                            void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream);
+int32_t rptq_kv_dequant_paged(const void* k_pages, const void* v_pages, int64_t n_pages, int32_t page_size, int32_t bits,
+                              const int64_t* slots, int64_t T, int32_t d, const void* k_table, const void* v_table,
+                              void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream);
+size_t rptq_attend_paged_workspace_bytes(int32_t B, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
+int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                          float scale, const void* k_table, const void* v_table, int32_t bits, const void* k_pages,
+                          const void* v_pages, int64_t n_pages, int32_t page_size, const int32_t* page_table,
+                          int64_t ld_page_table, int32_t pages_per_seq, const int32_t* lens, void* out, int64_t ld_out,
+                          int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- helpers for verification (not on the timed path) ---------------------------- */
 
 /* The literal per-cluster integers Yq_i of App. A.4 from the same MFMA main loop:

@@ -8,7 +8,8 @@ What it covers (arXiv 2304.01089):
   two-number points for a tensor clustered alone (the value cache);
 * the key/value-cache codes of the W4A4KV / W4A3KV / W3A3KV settings (Sec. 5.1):
   per head, channels in cluster order, Eq. 1 with one Eq. 2 pair per cluster;
-* reading the cache back: x_hat = s (x_q - z), the line under Eq. 1.
+* reading the cache back: x_hat = s (x_q - z), the line under Eq. 1;
+* attention of one new token over cached codes, in float64.
 
 Only tests, the smoke check and the benchmark's CPU-baseline leg may import this
 module.  It shares no code with the HIP library and never calls it.
@@ -128,3 +129,29 @@ def kv_dequant(codes, hc: HeadClusters, tensor: int, original_order: bool = Fals
         out[:, hc.perm] = y
         return out
     return y
+
+
+def attend(q, k_codes, v_codes, hc_k: HeadClusters, tensor_k: int, hc_v: HeadClusters, tensor_v: int, n_q_heads: int,
+           scale: float):
+    """Attention of one new token over cached codes.  q [n_q_heads * d_head] in the original channel order,
+    k_codes / v_codes [tokens, D] in cluster order (D = key/value heads * d_head); query head h reads key/value head
+    h // (n_q_heads / key/value heads).  x_hat = s (code - z) is not rounded.  Returns (out [n_q_heads * d_head] in the
+    original channel order, lse [n_q_heads]) in float64; without tokens zeros and -infinity."""
+    H, dh = hc_k.n_heads, hc_k.d_head
+    share = n_q_heads // H
+    q = np.asarray(q, dtype=F64).reshape(n_q_heads, dh)
+    out, lse = np.zeros((n_q_heads, dh)), np.full(n_q_heads, -np.inf)
+    if len(k_codes) == 0:
+        return out.reshape(-1), lse
+    s_k, _, z_k = position_tables(hc_k, tensor_k)
+    s_v, _, z_v = position_tables(hc_v, tensor_v)
+    for h in range(n_q_heads):
+        kv = h // share
+        sl = slice(kv * dh, (kv + 1) * dh)
+        k_hat = s_k[sl].astype(F64) * (np.asarray(k_codes)[:, sl].astype(F64) - z_k[sl])
+        v_hat = s_v[sl].astype(F64) * (np.asarray(v_codes)[:, sl].astype(F64) - z_v[sl])
+        a = scale * (k_hat @ q[h][hc_k.perm[sl] - kv * dh])
+        p = np.exp(a - a.max())
+        lse[h] = a.max() + np.log(p.sum())
+        out[h][hc_v.perm[sl] - kv * dh] = p @ v_hat / p.sum()
+    return out.reshape(-1), lse

@@ -39,6 +39,11 @@ from .binding import (  # noqa: F401
     rptq_kv_tables,
     rptq_kv_quant,
     rptq_kv_dequant,
+    rptq_kv_page_bytes,
+    rptq_kv_quant_paged,
+    rptq_kv_dequant_paged,
+    rptq_attend_paged_workspace_bytes,
+    rptq_attend_paged,
     rptq_dequant_codes,
     rptq_dequant_weights,
     rptq_gemm_bf16,
@@ -50,4 +55,5 @@ from .binding import (  # noqa: F401
     DTYPE_F32,
 )
 from .layer import (Calibration, FoldedLinear, FoldedLinearCw, calibrate_site, identity_site, fold_linear, ln_quant,  # noqa: F401
-                    cluster_gemm, cluster_gemm_quant, fold_linear_cw, cluster_rowsums, cluster_gemm_cw)
+                    cluster_gemm, cluster_gemm_quant, fold_linear_cw, cluster_rowsums, cluster_gemm_cw, PagedCache, paged_cache, kv_quant_paged, kv_dequant_paged,
+                    attend_paged, attend_paged_workspace)

@@ -24,7 +24,8 @@ EXPORTED_SYMBOLS = (
     "rptq_cw_scale_bytes", "rptq_cw_cross_bytes", "rptq_cw_rowsum_bytes", "rptq_fold_reorder_cw", "rptq_cluster_rowsums",
     "rptq_cluster_gemm_cw", "rptq_cluster_gemm_partials_cw",
     "rptq_cluster_channels", "rptq_cluster_heads", "rptq_kv_table_bytes", "rptq_kv_tables", "rptq_kv_quant",
-    "rptq_kv_dequant", "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
+    "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
+    "rptq_attend_paged_workspace_bytes", "rptq_attend_paged", "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
 )
 
 _LIB = None
@@ -101,6 +102,12 @@ def load_library():
         "rptq_kv_tables": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]),
         "rptq_kv_quant": (i32, [vp, i64, i32, vp, i32, vp, vp]),
         "rptq_kv_dequant": (i32, [vp, i64, i32, vp, i32, vp, vp]),
+        "rptq_kv_page_bytes": (sz, [i32, i32, i32]),
+        "rptq_kv_quant_paged": (i32, [vp, i64, vp, i64, i64, i32, vp, vp, i32, vp, vp, vp, i64, i32, vp]),
+        "rptq_kv_dequant_paged": (i32, [vp, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp, i64, vp, i64, vp]),
+        "rptq_attend_paged_workspace_bytes": (sz, [i32, i32, i32, i32]),
+        "rptq_attend_paged": (i32, [vp, i64, i32, i32, i32, i32, f32, vp, vp, i32, vp, vp, i64, i32, vp, i64, i32, vp, vp, i64,
+                                    i32, vp, vp, sz, vp]),
         "rptq_device_info": (i32, [vp, vp, vp, vp]),
         "rptq_strerror": (C.c_char_p, [i32]),
         "rptq_last_hip_error": (i32, []),
@@ -594,6 +601,119 @@ def rptq_kv_dequant(codes, T: int, d: int, table, bits: int, out, stream=None):
         import torch
         st = load_library().rptq_kv_dequant(_dev(codes), T, d, _dev(table), bits, _dev(out, torch.bfloat16), _stream(stream))
     _check(st, "rptq_kv_dequant")
+
+
+# ---- the cache in pages: sizes come from the tensors, which may be rows of wider ones ------------------
+def _here(t, dtype, what: str):
+    """Address of a tensor of that type on the current device (the launch goes there)."""
+    import torch
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s: expected a tensor on the current device" % what)
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: expected dtype %s, got %s" % (what, dtype, t.dtype))
+    return t.data_ptr()
+
+
+def _whole(t, dtype, what: str, least: int):
+    """Address of a contiguous tensor of at least so many bytes."""
+    p = _here(t, dtype, what)
+    if not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous tensor" % what)
+    if t.numel() * t.element_size() < least:
+        raise ValueError("%s: %d bytes, %d needed" % (what, t.numel() * t.element_size(), least))
+    return p
+
+
+def _matrix(t, dtype, what: str, shape):
+    """(address, elements from row to row) of a two-dimensional tensor with contiguous rows."""
+    p = _here(t, dtype, what)
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: expected shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s: expected contiguous rows" % what)
+    return p, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _pages(k_pages, v_pages, d: int, page_size: int, bits: int):
+    """Addresses of both tensors' pages and their number."""
+    import torch
+    size = rptq_kv_page_bytes(d, page_size, bits)
+    if size == 0:
+        raise RptqError(-3 if bits not in (3, 4, 8) else -2, "rptq_kv_page_bytes")
+    if k_pages.numel() != v_pages.numel() or k_pages.numel() % size != 0:
+        raise ValueError("k_pages and v_pages: expected the same whole number of pages of %d bytes" % size)
+    return (_whole(k_pages, torch.uint8, "k_pages", size), _whole(v_pages, torch.uint8, "v_pages", size),
+            k_pages.numel() // size)
+
+
+def _tokens(k, v, slots):
+    """(T, d) of a call with keys and values of T tokens."""
+    import torch
+    if k.dim() != 2 or v.shape != k.shape:
+        raise ValueError("k and v: expected two tensors [T, d]")
+    if slots.dim() != 1 or slots.shape[0] != k.shape[0]:
+        raise ValueError("slots: expected one per row")
+    return k.shape[0], k.shape[1]
+
+
+def rptq_kv_page_bytes(d: int, page_size: int, bits: int) -> int:
+    return int(load_library().rptq_kv_page_bytes(d, page_size, bits))
+
+
+def rptq_kv_quant_paged(k, v, slots, k_table, v_table, bits: int, k_pages, v_pages, page_size: int, stream=None):
+    """k, v: bf16 [T, d], rows of any stride; slots: int64 [T]; pages: uint8, a whole number of pages."""
+    import torch
+    T, d = _tokens(k, v, slots)
+    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+    (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+    st = load_library().rptq_kv_quant_paged(
+        ka, ld_k, va, ld_v, T, d, _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), bits,
+        _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
+    _check(st, "rptq_kv_quant_paged")
+
+
+def rptq_kv_dequant_paged(k_pages, v_pages, page_size: int, bits: int, slots, k_table, v_table, k, v, stream=None):
+    """k, v: bf16 [T, d] out, rows of any stride; slots: int64 [T]."""
+    import torch
+    T, d = _tokens(k, v, slots)
+    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+    (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+    st = load_library().rptq_kv_dequant_paged(
+        kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
+        _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), ka, ld_k, va, ld_v,
+        _stream(stream)) if T else 0
+    _check(st, "rptq_kv_dequant_paged")
+
+
+def rptq_attend_paged_workspace_bytes(B: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(load_library().rptq_attend_paged_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim))
+
+
+def rptq_attend_paged(q, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, k_table, v_table, bits: int, k_pages,
+                      v_pages, page_size: int, page_table, lens, out, lse, workspace, stream=None):
+    """q, out: [B, n_q_heads * head_dim], rows of any stride; page_table: int32 [B, pages]; lens: int32 [B];
+    lse: fp32 [B, n_q_heads] or None."""
+    import torch
+    B, d = q.shape[0], n_kv_heads * head_dim
+    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+    if out.dtype == torch.float32:
+        out_dtype = DTYPE_F32
+    elif out.dtype == torch.bfloat16:
+        out_dtype = DTYPE_BF16
+    else:
+        raise ValueError("out must be bf16 or fp32")
+    if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != B:
+        raise ValueError("expected page_table [B, pages] and lens [B]")
+    qa, ld_q = _matrix(q, torch.bfloat16, "q", (B, n_q_heads * head_dim))
+    oa, ld_out = _matrix(out, None, "out", (B, n_q_heads * head_dim))
+    pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
+    la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
+    st = load_library().rptq_attend_paged(
+        qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _whole(k_table, None, "k_table", 16 * d),
+        _whole(v_table, None, "v_table", 16 * d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
+        _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
+        workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+    _check(st, "rptq_attend_paged")
 
 
 def rptq_unpack_codes(codes_packed, rows: int, cluster_off, bits: int, out, stream=None):

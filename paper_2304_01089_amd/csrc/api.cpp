@@ -332,6 +332,121 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
   return launch_kv_dequant(codes, T, d, static_cast<const KvPos*>(table), bits, out, static_cast<hipStream_t>(stream));
 }
 
+// ---- the cache in pages -----------------------------------------------------------------------------
+static bool page_size_ok(int32_t p) { return p >= RPTQ_MIN_PAGE_SIZE && p <= RPTQ_MAX_PAGE_SIZE && (p & (p - 1)) == 0; }
+
+static bool paged_channels_ok(int64_t d) { return d >= kPageBlock && d <= RPTQ_MAX_CHANNELS && d % kPageBlock == 0; }
+
+static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+static bool row_stride_ok(int64_t ld, int64_t row) { return ld >= row && ld % 8 == 0; }
+
+size_t rptq_kv_page_bytes(int32_t d, int32_t page_size, int32_t bits) {
+  if (!paged_channels_ok(d) || !page_size_ok(page_size) || check_bits(bits) != RPTQ_OK) return 0;
+  return static_cast<size_t>(d) * bits / 8 * page_size;
+}
+
+// What the three paged entry points have in common: the cache.
+static int32_t check_paged(int64_t d, int64_t n_pages, int32_t page_size, int32_t bits, PagedGeom* g) {
+  if (int32_t st = check_bits(bits)) return st;
+  if (!paged_channels_ok(d) || !page_size_ok(page_size) || n_pages < 1 || n_pages > INT32_MAX) return RPTQ_ERR_SHAPE;
+  *g = PagedGeom{static_cast<int32_t>(d), __builtin_ctz(static_cast<unsigned>(page_size)), n_pages};
+  return RPTQ_OK;
+}
+
+static int32_t check_kv_paged(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T, int32_t d,
+                              const void* k_table, const void* v_table, int32_t bits, const int64_t* slots,
+                              const void* k_pages, const void* v_pages, int64_t n_pages, int32_t page_size, PagedGeom* g) {
+  if (!k || !v || !k_table || !v_table || !slots || !k_pages || !v_pages) return RPTQ_ERR_NULL;
+  if (int32_t st = check_paged(d, n_pages, page_size, bits, g)) return st;
+  if (T < 0 || T > (INT64_C(1) << 40) || !row_stride_ok(ld_k, d) || !row_stride_ok(ld_v, d)) return RPTQ_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_table) || !aligned16(v_table) || !aligned_to(slots, 8) ||
+      !aligned16(k_pages) || !aligned16(v_pages))
+    return RPTQ_ERR_ALIGN;
+  return RPTQ_OK;
+}
+
+int32_t rptq_kv_quant_paged(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T, int32_t d,
+                            const void* k_table, const void* v_table, int32_t bits, const int64_t* slots,
+                            void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream) {
+  PagedGeom g;
+  if (int32_t st = check_kv_paged(k, ld_k, v, ld_v, T, d, k_table, v_table, bits, slots, k_pages, v_pages, n_pages, page_size, &g))
+    return st;
+  // (the kernel reads x only)
+  const PagedTensor kt{static_cast<const KvPos*>(k_table), static_cast<uint8_t*>(k_pages),
+                       const_cast<uint16_t*>(static_cast<const uint16_t*>(k)), ld_k};
+  const PagedTensor vt{static_cast<const KvPos*>(v_table), static_cast<uint8_t*>(v_pages),
+                       const_cast<uint16_t*>(static_cast<const uint16_t*>(v)), ld_v};
+  return launch_kv_quant_paged(kt, vt, slots, T, g, bits, static_cast<hipStream_t>(stream));
+}
+
+int32_t rptq_kv_dequant_paged(const void* k_pages, const void* v_pages, int64_t n_pages, int32_t page_size, int32_t bits,
+                              const int64_t* slots, int64_t T, int32_t d, const void* k_table, const void* v_table,
+                              void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream) {
+  PagedGeom g;
+  if (int32_t st = check_kv_paged(k, ld_k, v, ld_v, T, d, k_table, v_table, bits, slots, k_pages, v_pages, n_pages, page_size, &g))
+    return st;
+  // (the kernel reads the pages only)
+  const PagedTensor kt{static_cast<const KvPos*>(k_table), const_cast<uint8_t*>(static_cast<const uint8_t*>(k_pages)),
+                       static_cast<uint16_t*>(k), ld_k};
+  const PagedTensor vt{static_cast<const KvPos*>(v_table), const_cast<uint8_t*>(static_cast<const uint8_t*>(v_pages)),
+                       static_cast<uint16_t*>(v), ld_v};
+  return launch_kv_dequant_paged(kt, vt, slots, T, g, bits, static_cast<hipStream_t>(stream));
+}
+
+static bool attend_heads_ok(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
+  if (hd != 32 && hd != 64 && hd != 128 && hd != 256) return false;
+  if (B < 0 || B > (1 << 20) || n_kv < 1 || n_q < 1 || n_q % n_kv != 0) return false;
+  return paged_channels_ok(static_cast<int64_t>(n_kv) * hd) && static_cast<int64_t>(n_q) * hd <= RPTQ_MAX_CHANNELS;
+}
+
+size_t rptq_attend_paged_workspace_bytes(int32_t B, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (!attend_heads_ok(B, n_q_heads, n_kv_heads, head_dim)) return 0;
+  return attend_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim);
+}
+
+int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                          float scale, const void* k_table, const void* v_table, int32_t bits, const void* k_pages,
+                          const void* v_pages, int64_t n_pages, int32_t page_size, const int32_t* page_table,
+                          int64_t ld_page_table, int32_t pages_per_seq, const int32_t* lens, void* out, int64_t ld_out,
+                          int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k_table || !v_table || !k_pages || !v_pages || !page_table || !lens || !out || !workspace) return RPTQ_ERR_NULL;
+  if (int32_t st = check_bits(bits)) return st;
+  if (!attend_heads_ok(B, n_q_heads, n_kv_heads, head_dim)) return RPTQ_ERR_SHAPE;
+  AttendArgs a;
+  if (int32_t st = check_paged(static_cast<int64_t>(n_kv_heads) * head_dim, n_pages, page_size, bits, &a.g)) return st;
+  const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
+  if (!row_stride_ok(ld_q, row) || !row_stride_ok(ld_out, row)) return RPTQ_ERR_SHAPE;
+  if (pages_per_seq < 1 || ld_page_table < pages_per_seq) return RPTQ_ERR_SHAPE;
+  if (static_cast<int64_t>(pages_per_seq) * page_size > (INT64_C(1) << 30)) return RPTQ_ERR_SHAPE;
+  if (out_dtype != RPTQ_DTYPE_BF16 && out_dtype != RPTQ_DTYPE_F32) return RPTQ_ERR_SHAPE;
+  if (!std::isfinite(scale)) return RPTQ_ERR_RANGE;
+  if (workspace_bytes < attend_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim)) return RPTQ_ERR_WORKSPACE;
+  if (!aligned16(q) || !aligned16(k_table) || !aligned16(v_table) || !aligned16(k_pages) || !aligned16(v_pages) ||
+      !aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned16(out) || !aligned_to(lse, 4) || !aligned16(workspace))
+    return RPTQ_ERR_ALIGN;
+  a.q = static_cast<const uint16_t*>(q);
+  a.ld_q = ld_q;
+  a.B = B;
+  a.n_q = n_q_heads;
+  a.n_kv = n_kv_heads;
+  a.hd = head_dim;
+  a.scale = scale;
+  a.k_pos = static_cast<const KvPos*>(k_table);
+  a.v_pos = static_cast<const KvPos*>(v_table);
+  a.k_pages = static_cast<const uint8_t*>(k_pages);
+  a.v_pages = static_cast<const uint8_t*>(v_pages);
+  a.page_table = page_table;
+  a.ld_pt = ld_page_table;
+  a.pages_per_seq = pages_per_seq;
+  a.lens = lens;
+  a.out = out;
+  a.ld_out = ld_out;
+  a.lse = lse;
+  a.workspace = workspace;
+  return launch_attend_paged(a, bits, out_dtype, static_cast<hipStream_t>(stream));
+}
+
 int32_t rptq_cluster_gemm_partials(const void* codes_packed, int64_t M, int32_t bits,
                                    const void* Wq_packed, int32_t N, const int32_t* cluster_off, int32_t g,
                                    const int32_t* zX, const int32_t* zW, const int32_t* xsum,

@@ -11,27 +11,11 @@
 #include <hip/hip_runtime.h>
 
 #include "device_common.h"
+#include "kv_common.h"
 #include "pack_formats.h"
 #include "rptq_internal.h"
 
 namespace rptq {
-
-constexpr int kKvTile = 1024;                  // channels per wave tile
-constexpr int kKvLaneCodes = 16;               // codes per lane
-
-// position of local code e of a lane inside the wave tile
-template <int BITS>
-__device__ __forceinline__ int kv_local_pos(int lane, int e) {
-  if (BITS == 3) {
-    // lanes 2g, 2g+1 share the 32-code group g: lane 2g carries codes 0..7, 24..27, 16..19,
-    // lane 2g+1 codes 8..15, 28..31, 20..23 (so that each owns whole dwords of the group)
-    const int role = lane & 1, gbase = (lane >> 1) * kGroup;
-    if (e < 8) return gbase + role * 8 + e;
-    if (e < 12) return gbase + 24 + role * 4 + (e - 8);
-    return gbase + 16 + role * 4 + (e - 12);
-  }
-  return lane * kKvLaneCodes + e;
-}
 
 template <int BITS>
 __global__ void __launch_bounds__(256) kv_quant_kernel(const uint4* x, int64_t T, int32_t d, const KvPos* pos,
@@ -112,26 +96,7 @@ __global__ void __launch_bounds__(256) kv_quant_kernel(const uint4* x, int64_t T
     }
     wave_lds_fence();
     uint8_t* out = codes + row * out_row_bytes + out_tile;
-    if (BITS == 8) {
-      const uint4 o = make_uint4(D[0] ^ 0x80808080u, D[1] ^ 0x80808080u, D[2] ^ 0x80808080u, D[3] ^ 0x80808080u);
-      if (lane_ok) *reinterpret_cast<uint4*>(out + lane * 16) = o;
-    } else if (BITS == 4) {
-      uint2 o;
-      o.x = ((D[0] << 4) | D[1]) ^ 0x88888888u;
-      o.y = ((D[2] << 4) | D[3]) ^ 0x88888888u;
-      if (lane_ok) *reinterpret_cast<uint2*>(out + lane * 8) = o;
-    } else {
-      const int role = lane & 1;
-      const uint32_t w1 = ((D[0] << 5) | (D[1] << 2) | ((D[2] >> 1) & 0x03030303u)) ^ 0x80808080u ^ 0x10101010u ^ 0x02020202u;
-      const uint32_t mine = role ? (((D[3] << 2) ^ 0x10101010u) | ((D[2] & 0x01010101u) << 1))
-                                 : (((D[3] << 5) ^ 0x80808080u) | (D[2] & 0x01010101u));
-      const uint32_t other = __shfl_xor(mine, 1, kWave);
-      if (lane_ok) {
-        uint32_t* p = reinterpret_cast<uint32_t*>(out + (lane >> 1) * 12 + role * 4);
-        p[0] = w1;
-        if (role) p[1] = mine | other;
-      }
-    }
+    kv_store_codes<BITS>(out + (BITS == 3 ? (lane >> 1) * 12 : lane * 2 * BITS), lane, lane_ok, D[0], D[1], D[2], D[3]);
   }
 }
 

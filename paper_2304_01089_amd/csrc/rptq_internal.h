@@ -145,6 +145,42 @@ int32_t launch_gemm_bf16(const void* xh, const void* wh, int64_t M, int32_t N, i
                          hipStream_t st);
 int32_t launch_kv_quant(const void* x, int64_t T, int32_t d, const KvPos* pos, int32_t bits, void* codes, hipStream_t st);
 int32_t launch_kv_dequant(const void* codes, int64_t T, int32_t d, const KvPos* pos, int32_t bits, void* out, hipStream_t st);
+// kv_paged.hip, attend_paged.hip: the cache in pages.  One tensor (keys or values) of it:
+struct PagedTensor {
+  const KvPos* pos;
+  uint8_t* pages;
+  uint16_t* x;                             // rows of the dense side (quantize: read, de-quantize: written)
+  int64_t ld;                              // elements between them
+};
+struct PagedGeom {
+  int32_t d;                               // channels, a multiple of 128
+  int32_t page_shift;                      // log2 of the tokens of a page
+  int64_t n_pages;
+};
+constexpr int kPageBlock = 128;            // positions of one row of a page's block
+int32_t launch_kv_quant_paged(const PagedTensor& k, const PagedTensor& v, const int64_t* slots, int64_t T,
+                              const PagedGeom& g, int32_t bits, hipStream_t st);
+int32_t launch_kv_dequant_paged(const PagedTensor& k, const PagedTensor& v, const int64_t* slots, int64_t T,
+                                const PagedGeom& g, int32_t bits, hipStream_t st);
+struct AttendArgs {
+  const uint16_t* q;
+  int64_t ld_q;
+  int32_t B, n_q, n_kv, hd;
+  float scale;
+  const KvPos *k_pos, *v_pos;
+  const uint8_t *k_pages, *v_pages;
+  PagedGeom g;
+  const int32_t* page_table;
+  int64_t ld_pt;
+  int32_t pages_per_seq;
+  const int32_t* lens;
+  void* out;
+  int64_t ld_out;
+  float* lse;
+  void* workspace;
+};
+size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd);
+int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype, hipStream_t st);
 // Per-head clustering (host.cpp), exposed through rptq_cluster_heads.
 int32_t cluster_heads(const float* const* ch_min, const float* const* ch_max, int32_t n_tensors, int32_t d,
                       int32_t n_heads, int32_t g, int32_t bits, uint64_t seed, int32_t max_iter, int32_t* assign,

@@ -186,3 +186,71 @@ def cluster_gemm_cw(cal: Calibration, lin: FoldedLinearCw, codes, rowsums, M, y=
     B.rptq_cluster_gemm_cw(codes, M, cal.bits, lin.Wq, lin.N, cal.cluster_off, lin.scale_tab, lin.cross_tab, lin.colterm,
                            rowsums, y)
     return y
+
+
+# ---- the key/value cache in pages ------------------------------------------------------------------
+@dataclass
+class PagedCache:
+    """Keys and values of one layer: pages of codes, and the position tables (rptq_kv_tables) they are written and read by."""
+    n_heads: int
+    head_dim: int
+    bits: int
+    page_size: int
+    k_pages: object       # uint8 [n_pages, d / 128, page_size, 16 * bits]
+    v_pages: object
+    k_table: object
+    v_table: object
+
+
+def paged_cache(n_pages: int, page_size: int, n_heads: int, head_dim: int, bits: int, k_table, v_table) -> PagedCache:
+    """A cache with room for n_pages * page_size tokens.  (What no token was written to holds no values: no call reads it but
+    for a token that a page table and a length claim.)"""
+    import torch
+    d = n_heads * head_dim
+    if B.rptq_kv_page_bytes(d, page_size, bits) == 0:
+        raise B.RptqError(-3 if bits not in (3, 4, 8) else -2, "rptq_kv_page_bytes")
+    pages = [torch.zeros((n_pages, d // 128, page_size, 16 * bits), dtype=torch.uint8, device=k_table.device) for _ in range(2)]
+    return PagedCache(n_heads, head_dim, bits, page_size, pages[0], pages[1], k_table, v_table)
+
+
+def kv_quant_paged(cache: PagedCache, k, v, slots):
+    """Keys and values [T, d] of new tokens into the cache; a negative slot: that row is stored nowhere."""
+    B.rptq_kv_quant_paged(k, v, slots, cache.k_table, cache.v_table, cache.bits, cache.k_pages, cache.v_pages, cache.page_size)
+
+
+def kv_dequant_paged(cache: PagedCache, slots, k=None, v=None):
+    """The rows at these slots, bf16 in the original channel order; where a slot is none, zeros, or what a given tensor held."""
+    if k is None or v is None:
+        import torch
+        shape = (slots.shape[0], cache.n_heads * cache.head_dim)
+        if k is None:
+            k = torch.zeros(shape, dtype=torch.bfloat16, device=slots.device)
+        if v is None:
+            v = torch.zeros(shape, dtype=torch.bfloat16, device=slots.device)
+    B.rptq_kv_dequant_paged(cache.k_pages, cache.v_pages, cache.page_size, cache.bits, slots, cache.k_table, cache.v_table, k, v)
+    return k, v
+
+
+def attend_paged_workspace(cache: PagedCache, batch: int, n_q_heads: int):
+    """Device memory for attend_paged calls of that many sequences, one call at a time."""
+    import torch
+    return torch.empty(max(16, B.rptq_attend_paged_workspace_bytes(batch, n_q_heads, cache.n_heads, cache.head_dim)),
+                       dtype=torch.uint8, device=cache.k_pages.device)
+
+
+def attend_paged(cache: PagedCache, q, page_table, lens, scale=None, out=None, lse=None, want_lse=False, workspace=None):
+    """Attention of one new token of every sequence over the cache.  q: [B, n_q_heads * head_dim]; scale: 1 / sqrt(head_dim)
+    unless given.  Returns (out, lse); lse is None unless given or wanted."""
+    n_q_heads = q.shape[1] // cache.head_dim
+    if out is None or (lse is None and want_lse) or workspace is None:
+        import torch
+        if out is None:
+            out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=q.device)
+        if lse is None and want_lse:
+            lse = torch.empty((q.shape[0], n_q_heads), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = attend_paged_workspace(cache, q.shape[0], n_q_heads)
+    B.rptq_attend_paged(q, n_q_heads, cache.n_heads, cache.head_dim, cache.head_dim ** -0.5 if scale is None else scale,
+                        cache.k_table, cache.v_table, cache.bits, cache.k_pages, cache.v_pages, cache.page_size, page_table,
+                        lens, out, lse, workspace)
+    return out, lse
