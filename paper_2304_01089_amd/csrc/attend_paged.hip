@@ -1,126 +1,583 @@
-// Attention of one new token per sequence over the paged cache, on the codes.  With q'_j = scale q[src_j] s^K_j,
-//   a_t = sum_j q'_j k_tj - sum_j q'_j z^K_j,   out_j = s^V_j (sum_t p_t v_tj / sum_t p_t - z^V_j),   p_t = exp(a_t - max a):
+// Attention of one new token per sequence over the paged cache, on the codes.  With q'_j = scale log2(e) q[src_j] s^K_j,
+//   a_t = sum_j q'_j k_tj - sum_j q'_j z^K_j,   out_j = s^V_j (sum_t p_t v_tj / sum_t p_t - z^V_j),   p_t = 2^(a_t - max a):
 // the zero points of the keys add one number to every score of a head, which the softmax does not see (only lse does), and
 // those of the values come off the weighted mean.
 //
-// A workgroup takes one query head of one sequence through all of its tokens, 256 at a time, a token per thread for the
-// scores and a channel per thread for the sums.
+// Both sums run on the int8 matrix cores, exactly.  A query's q' and a tile's weights p are written in fixed point, 31 bits
+// below the head's largest |q'| and 30 below the tile's largest weight, as four signed digits to the base 256; a digit is a
+// row of the matrix product, so four heads fill its 16 rows (one query head on a key/value head uses four of them: rows cost
+// nothing here, the product is bound by the bytes of the cache).  Codes are the other operand as they are stored, one shift
+// and one mask per four of them.  The digits' sums meet again in one lane.  What is rounded: q' once per factor, the sum of a
+// tile of 64 tokens once to fp32.
+//
+// A workgroup takes a part of one sequence for the heads that read one block of 128 positions (two for heads 256 wide), a
+// wave every fourth tile of 64 tokens.  How sequences are cut in parts follows their lengths, which the kernel reads: parts
+// of equal length over the whole batch, as many as fill the chip.  Parts leave (max, sum, weighted codes), a second kernel
+// joins them; sequences of one part are finished at once.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device_common.h"
-#include "pack_formats.h"
 #include "rptq_internal.h"
 
 namespace rptq {
 
+typedef int v4i __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNone = -3.402823466e38f;      // below every score
+constexpr int kTile = 64;                      // tokens of a wave's tile
+constexpr int kLeastTiles = 4;                 // of a part: one per wave
+constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
-template <int BITS, bool F32>
-__global__ void __launch_bounds__(256) attend_paged_kernel(AttendArgs a) {
-  constexpr int GB = 4 * BITS;                         // bytes of 32 codes
-  __shared__ float qs[256], p[256], red[8];
-  __shared__ double redd[4];
-  __shared__ int64_t vrow[256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.x % a.n_q, b = blockIdx.x / a.n_q;
-  const int kvh = h / (a.n_q / a.n_kv);
-  const int page_size = 1 << a.g.page_shift;
-  const int len = static_cast<int>(min<int64_t>(max(a.lens[b], 0), static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift));
-  auto sum_all = [&](float v) {
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m, kWave);
-    __syncthreads();
-    if (lane == 0) red[wave] = v;
-    __syncthreads();
-    return red[0] + red[1] + red[2] + red[3];
-  };
-  auto max_all = [&](float v) {
-    for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, kWave));
-    __syncthreads();
-    if (lane == 0) red[wave] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  };
-  double zterm = 0.0;
-  if (tid < a.hd) {
-    const KvPos kp = a.k_pos[kvh * a.hd + tid];
-    const float x = __uint_as_float(static_cast<uint32_t>(a.q[b * a.ld_q + h * a.hd + (kp.src & (a.hd - 1))]) << 16);
-    qs[tid] = x * kp.s * (a.scale * kLog2e);
-    zterm = static_cast<double>(qs[tid]) * kp.z;
-  }
-  for (int m = 32; m; m >>= 1) zterm += __shfl_xor(zterm, m, kWave);
-  if (lane == 0) redd[wave] = zterm;
-  __syncthreads();
-  zterm = redd[0] + redd[1] + redd[2] + redd[3];
-  float m_run = -1e30f, l_run = 0.0f, acc = 0.0f;
-  const int block = kvh * a.hd / kPageBlock, first = kvh * a.hd % kPageBlock;
-  auto row_at = [&](int page, int blk, int r) {
-    return (((static_cast<int64_t>(page) * (a.g.d / kPageBlock) + blk) << a.g.page_shift) + r) * (16 * BITS);
-  };
-  for (int t0 = 0; t0 < len; t0 += 256) {
-    const int t = t0 + tid;
-    const int page = t < len ? a.page_table[b * a.ld_pt + (t >> a.g.page_shift)] : -1;
-    const bool here = page >= 0 && page < a.g.n_pages;
-    float score = -1e30f;
-    if (here) {
-      score = 0.0f;
-      for (int j0 = 0; j0 < a.hd; j0 += 32) {
-        const int at = first + j0;
-        const uint8_t* src = a.k_pages + row_at(page, block + at / kPageBlock, t & (page_size - 1)) + at % kPageBlock / 32 * GB;
-        uint32_t w[GB / 4];
-        int c[32];
-        for (int k = 0; k < GB / 4; ++k) w[k] = reinterpret_cast<const uint32_t*>(src)[k];
-        decode_group<BITS>(w, c);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) score = fmaf(qs[j0 + j], static_cast<float>(c[j]), score);
-      }
-    }
-    const float m_new = fmaxf(m_run, max_all(score));
-    const float e = here ? __builtin_amdgcn_exp2f(score - m_new) : 0.0f;
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    l_run = l_run * alpha + sum_all(e);
-    p[tid] = e;
-    vrow[tid] = here ? row_at(page, block, t & (page_size - 1)) : -1;
-    __syncthreads();
-    if (tid < a.hd) {
-      const int at = first + tid;
-      const int64_t off = static_cast<int64_t>(at / kPageBlock) * (static_cast<int64_t>(page_size) * 16 * BITS) + at % kPageBlock / 32 * GB;
-      acc *= alpha;
-      for (int i = 0; i < 256; ++i) {
-        if (vrow[i] < 0) continue;
-        uint32_t w[GB / 4];
-        int c[32];
-        for (int k = 0; k < GB / 4; ++k) w[k] = reinterpret_cast<const uint32_t*>(a.v_pages + vrow[i] + off)[k];
-        decode_group<BITS>(w, c);
-        int mine = 0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) mine = (at & 31) == j ? c[j] : mine;
-        acc = fmaf(p[i], static_cast<float>(mine), acc);
-      }
-    }
-    m_run = m_new;
-    __syncthreads();
-  }
-  if (tid < a.hd) {
-    const KvPos vp = a.v_pos[kvh * a.hd + tid];
-    const float y = l_run != 0.0f ? vp.s * (acc / l_run - static_cast<float>(vp.z)) : 0.0f;
-    const int64_t at = b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1));
-    if (F32) static_cast<float*>(a.out)[at] = y;
-    else static_cast<__bf16*>(a.out)[at] = static_cast<__bf16>(y);
-  }
-  if (a.lse && tid == 0)
-    a.lse[static_cast<int64_t>(b) * a.n_q + h] = l_run != 0.0f ? kLn2 * static_cast<float>(m_run + log2f(l_run) - zterm) : -__builtin_huge_valf();
+// Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
+__host__ __device__ constexpr int most_row_tiles(int blocks) { return blocks == 2 ? 2 : 4; }
+
+// How a call is laid out; from sizes alone, so that the workspace's is known before the lengths are.
+struct AttendPlan {
+  int32_t units;                               // blocks of positions (heads 256 wide: pairs of blocks)
+  int32_t unit_heads;                          // query heads that read a unit
+  int32_t chunks, chunk_heads;                 // these heads in equal groups, each a workgroup's
+  int32_t parts;                               // parts that the tokens of the batch are cut in (one more per sequence, from rounding up)
+  int32_t slots;                               // parts + B
+};
+
+static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
+  constexpr int kWorkgroups = 1024;            // four per compute unit of 256
+  AttendPlan p;
+  const int unit = hd > kPageBlock ? hd : kPageBlock;
+  p.units = n_kv * hd / unit;
+  p.unit_heads = n_q / p.units;
+  const int most = kRowHeads * most_row_tiles(unit / kPageBlock);
+  p.chunks = (p.unit_heads + most - 1) / most;
+  p.chunk_heads = (p.unit_heads + p.chunks - 1) / p.chunks;
+  const int each = p.units * p.chunks;
+  p.parts = std::max(1, (kWorkgroups + each - 1) / each);
+  p.slots = p.parts + B;
+  return p;
 }
 
-size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) { return 16; }
+// Workspace: [slots][n_q] {max, sum, the keys' zero-point term}, [slots][n_q][hd] weighted codes, [B] {first slot, parts}.
+struct PartHead {
+  float m, l, zterm, unused;
+};
+
+size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
+  const AttendPlan p = attend_plan(B, n_q, n_kv, hd);
+  const size_t rows = static_cast<size_t>(p.slots) * n_q;
+  return rows * sizeof(PartHead) + rows * hd * sizeof(float) + ((static_cast<size_t>(B) + 1) / 2) * 16;
+}
+
+struct PartBuffers {
+  PartHead* heads;
+  float* acc;
+  int2* where;
+};
+
+__device__ __forceinline__ PartBuffers part_buffers(const AttendArgs& a, const AttendPlan& p) {
+  const size_t rows = static_cast<size_t>(p.slots) * a.n_q;
+  PartBuffers b;
+  b.heads = static_cast<PartHead*>(a.workspace);
+  b.acc = reinterpret_cast<float*>(b.heads + rows);
+  b.where = reinterpret_cast<int2*>(b.acc + rows * a.hd);
+  return b;
+}
+
+// ---- lane arithmetic ------------------------------------------------------------------------------------
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_row(uint32_t v) {                // a permutation inside a row of 16 lanes
+  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_row(float v) { return __uint_as_float(dpp_row<CTRL>(__float_as_uint(v))); }
+
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, dpp_row<0xB1>(v));
+  v = fmaxf(v, dpp_row<0x4E>(v));
+  v = fmaxf(v, dpp_row<0x141>(v));
+  return fmaxf(v, dpp_row<0x140>(v));
+}
+__device__ __forceinline__ float row16_add(float v) {
+  v += dpp_row<0xB1>(v);
+  v += dpp_row<0x4E>(v);
+  v += dpp_row<0x141>(v);
+  return v + dpp_row<0x140>(v);
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = row16_max(v);
+  auto row = [&](int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); };
+  return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_plus(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_prefix(int v) {                      // inclusive
+  v = dpp_plus<0x111, 0xf>(v);
+  v = dpp_plus<0x112, 0xf>(v);
+  v = dpp_plus<0x114, 0xf>(v);
+  v = dpp_plus<0x118, 0xf>(v);
+  v = dpp_plus<0x142, 0xa>(v);
+  return dpp_plus<0x143, 0xc>(v);
+}
+
+// Four lanes' four bytes transposed: lane i's byte b becomes lane b's byte i.  (Two exchanges, of neighbours and of pairs.)
+struct QuadSel {
+  uint32_t s0, s1;
+};
+__device__ __forceinline__ QuadSel quad_sel(int lane) {
+  return {lane & 1 ? 0x03070105u : 0x06020400u, lane & 2 ? 0x03020706u : 0x05040100u};
+}
+__device__ __forceinline__ uint32_t quad_transpose(uint32_t x, const QuadSel& s) {
+  x = __builtin_amdgcn_perm(dpp_row<0xB1>(x), x, s.s0);
+  return __builtin_amdgcn_perm(dpp_row<0x4E>(x), x, s.s1);
+}
+
+// A number of up to 31 bits as four signed digits to the base 256, lowest in the lowest byte.
+__device__ __forceinline__ uint32_t digits(int v) { return (static_cast<uint32_t>(v) + 0x80808080u) ^ 0x80808080u; }
+
+// The digits' sums, lowest first, as one fp32 number (the products of two digits' sums with the base are exact).
+__device__ __forceinline__ float undigit(const v4i& c) {
+  return fmaf(static_cast<float>(c[3] * 256 + c[2]), 65536.0f, static_cast<float>(c[1] * 256 + c[0]));
+}
+
+// 32 packed codes (of one token; or, after quad_transpose, byte b of four tokens) -> operand bytes code << kShift, codes 4e..4e+3 in w[e]
+template <int BITS>
+__device__ __forceinline__ void expand(const uint32_t (&x)[BITS], uint32_t (&w)[8]) {
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = x[e];
+  } else if constexpr (BITS == 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      w[2 * u] = x[u] & 0xf0f0f0f0u;
+      w[2 * u + 1] = (x[u] << 4) & 0xf0f0f0f0u;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      w[2 * u] = x[u] & 0xe0e0e0e0u;
+      w[2 * u + 1] = (x[u] << 3) & 0xe0e0e0e0u;
+    }
+    w[6] = ((x[0] << 6) & 0xc0c0c0c0u) | ((x[2] << 5) & 0x20202020u);
+    w[7] = ((x[1] << 6) & 0xc0c0c0c0u) | ((x[2] << 4) & 0x20202020u);
+  }
+}
+
+// ---- which tokens a workgroup takes ------------------------------------------------------------------------
+struct Part {
+  int b, len, index, count, first_tile, end_tile;
+};
+
+// The part that slot number `slot` holds; false: none.  Every sequence has at least one.
+__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, double per_part, int slot, int lane, Part* out) {
+  const int cap = a.pages_per_seq << a.g.page_shift;
+  auto len_of = [&](int i) { return i < a.B ? min(max(a.lens[i], 0), cap) : 0; };
+  auto tiles_of = [](int n) { return (n + kTile - 1) / kTile; };
+  const int len0 = len_of(lane);
+  double total = tiles_of(len0);
+  for (int i = 64 + lane; i < a.B + lane; i += 64) total += tiles_of(len_of(i));
+  // tiles of a part: all tiles over the number of parts, rounded up (per_part is a little more than its reciprocal)
+  const int most = max(kLeastTiles, __builtin_amdgcn_readfirstlane(static_cast<int>((wave_sum(total) - 1.0) * per_part)) + 1);
+  int before = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    const int i = base + lane;
+    const int len = base == 0 ? len0 : len_of(i);
+    const int n = i < a.B ? max(1, (tiles_of(len) + most - 1) / most) : 0;
+    const int upto = wave_prefix(n);
+    const uint64_t hit = __ballot(slot >= before + upto - n && slot < before + upto);
+    if (hit != 0) {
+      const int l = __builtin_ctzll(hit);
+      out->b = base + l;
+      out->len = __builtin_amdgcn_readlane(len, l);
+      out->count = __builtin_amdgcn_readlane(n, l);
+      out->index = slot - before - __builtin_amdgcn_readlane(upto, l) + out->count;
+      const int tiles = tiles_of(out->len), each = (tiles + out->count - 1) / out->count;
+      out->first_tile = out->index * each;
+      out->end_tile = min(out->first_tile + each, tiles);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+__device__ __forceinline__ void store_out(const AttendArgs& a, bool f32, int64_t at, float y) {
+  if (f32) static_cast<float*>(a.out)[at] = y;
+  else static_cast<__bf16*>(a.out)[at] = static_cast<__bf16>(y);
+}
+
+// What a head's (max, sum) and weighted codes give: no tokens, zeros.
+__device__ __forceinline__ float finish(float acc, float l, const KvPos& v) {
+  return l != 0.0f ? v.s * (acc / l - static_cast<float>(v.z)) : 0.0f;
+}
+__device__ __forceinline__ float finish_lse(float m, float l, float zterm) {
+  return l != 0.0f ? kLn2 * ((m - 30.0f - zterm) + __log2f(l)) : -__builtin_huge_valf();
+}
+
+// ---- the parts ---------------------------------------------------------------------------------------------
+// NB: blocks of a unit; RT: row tiles (of four heads)
+template <int BITS, int NB, int RT>
+__global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, AttendPlan plan, double per_part, bool f32) {
+  constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
+  constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
+  constexpr int P = NB * kPageBlock;                       // positions of the unit
+  constexpr int kQBytes = RT * 16 * P, kPBytes = 4 * RT * 1024, kMergeBytes = 4 * kRowHeads * P * 4;
+  constexpr int kFront = kQBytes + kPBytes > kMergeBytes ? kQBytes + kPBytes : kMergeBytes;
+  __shared__ __align__(16) unsigned char smem[kFront];
+  __shared__ float h_scale[RT * kRowHeads], h_z[RT * kRowHeads];
+  __shared__ float2 w_ml[4][RT * kRowHeads];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n16 = lane & 15, g4 = lane >> 4;
+
+  // chunks of one unit's heads run on one XCD (workgroups are dealt to the eight in turn): they read the same pages
+  const int cells = plan.slots * plan.units;
+  const int chunk = static_cast<int>(blockIdx.x >> 3) % plan.chunks;
+  const int cell = static_cast<int>(blockIdx.x >> 3) / plan.chunks * 8 + static_cast<int>(blockIdx.x & 7);
+  if (cell >= cells) return;
+  const int unit = cell % plan.units, slot = cell / plan.units;
+
+  // (requested first: they depend on nothing)
+  const KvPos* kt = a.k_pos + unit * P;
+  KvPos kp[2 * NB];
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i) kp[i] = kt[i * 64 + lane];
+  const KvPos vp = a.v_pos[unit * P + tid % P];
+  Part part;
+  if (!find_part(a, plan, per_part, slot, lane, &part)) return;
+
+  // ---- pages of this wave's tiles: lane 4k + i holds the page of its k-th tile's i-th 16 tokens, or -1 ---------
+  const int32_t* pt = a.page_table + part.b * a.ld_pt;
+  const int my_tiles = max(0, (part.end_tile - part.first_tile - wave + 3) >> 2);
+  auto token_of = [&](int k) { return (part.first_tile + wave + 4 * k) * kTile; };
+  const int last_page = max(part.len - 1, 0) >> a.g.page_shift;
+  auto pages_from = [&](int k) {
+    const int t = token_of(k + (lane >> 2)) + (lane & 3) * 16;
+    const int id = pt[min(t >> a.g.page_shift, last_page)];
+    return t < part.len && id >= 0 && id < a.g.n_pages ? id : -1;
+  };
+  int ids = my_tiles > 0 ? pages_from(0) : -1, ids_next = my_tiles > 16 ? pages_from(16) : -1;
+
+  // K and V of a tile: lane (token n16, group g4) of every 16 tokens' keys; lane (group n16 / 4, token 4 g4 + n16 % 4) of the values
+  const uint32_t k_off = n16 * kRow + g4 * (4 * BITS);
+  const uint32_t v_off = (4 * g4 + (n16 & 3)) * kRow + (n16 >> 2) * (4 * BITS);
+  const int64_t block_rows = static_cast<int64_t>(1) << a.g.page_shift;
+  const int64_t page_rows = static_cast<int64_t>(a.g.d / kPageBlock) << a.g.page_shift;
+  auto row_of = [&](int k, int r) {                        // bytes to 16 tokens' rows in the unit's first block (uniform)
+    const int id = max(__builtin_amdgcn_readlane(ids, (k & 15) * 4 + r), 0);
+    const int t = (token_of(k) + r * 16) & static_cast<int>(block_rows - 1);
+    return (id * page_rows + unit * NB * block_rows + t) * kRow;
+  };
+  auto load = [&](const uint8_t* p, uint32_t off, uint32_t (&x)[BITS]) {
+    const uint8_t* s = p + off;
+    if constexpr (BITS == 3) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) x[k] = reinterpret_cast<const uint32_t*>(s)[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < BITS / 4; ++k) {
+        const v4i v = reinterpret_cast<const v4i*>(s)[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * k + e] = static_cast<uint32_t>(v[e]);
+      }
+    }
+  };
+  uint32_t kr[4][NB][BITS], vr[4][NB][BITS];
+  auto load_tile = [&](int k, const uint8_t* pages, uint32_t off, uint32_t (&x)[4][NB][BITS]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t row = row_of(k, r);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) load(pages + row + nb * block_rows * kRow, off, x[r][nb]);
+    }
+  };
+  if (my_tiles > 0) {
+    load_tile(0, a.k_pages, k_off, kr);
+    load_tile(0, a.v_pages, v_off, vr);
+  }
+
+  // ---- queries to digits: wave w takes head w of every row tile ------------------------------------------------
+  const int share = a.n_q / a.n_kv;
+  const int first_head = chunk * plan.chunk_heads;
+  const int heads = min(plan.chunk_heads, plan.unit_heads - first_head);       // of this workgroup
+  const int q_head = unit * plan.unit_heads + first_head;                      // the first of them
+  auto own = [&](int hh, int pos) { return NB == 2 || pos / a.hd == (first_head + hh) / share; };
+  unsigned char* q_dig = smem;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int hh = rt * kRowHeads + wave;
+    float x[2 * NB], top = 0.0f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+      x[i] = 0.0f;
+      if (hh < heads && own(hh, i * 64 + lane)) {
+        const uint16_t h = a.q[part.b * a.ld_q + (q_head + hh) * a.hd + (kp[i].src & (a.hd - 1))];
+        x[i] = __uint_as_float(static_cast<uint32_t>(h) << 16) * kp[i].s * (a.scale * kLog2e);
+      }
+      top = fmaxf(top, fabsf(x[i]));
+      bad = bad || !(fabsf(x[i]) < __builtin_huge_valf());
+    }
+    top = wave_max(top);
+    const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;           // top < 2^e
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+      const uint32_t d = digits(static_cast<int>(rintf(ldexpf(x[i], 30 - e))));
+#pragma unroll
+      for (int b = 0; b < 4; ++b) q_dig[(rt * 16 + wave * 4 + b) * P + i * 64 + lane] = static_cast<unsigned char>(d >> (8 * b));
+    }
+    float z = 0.0f;
+    if (a.lse) {
+      double zs = 0.0;
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) zs += static_cast<double>(x[i]) * kp[i].z;
+      z = static_cast<float>(wave_sum(zs));
+    }
+    const bool any_bad = __ballot(bad) != 0;
+    if (lane == 0) {
+      h_scale[hh] = any_bad ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);
+      h_z[hh] = z;
+    }
+  }
+  __syncthreads();
+  v4i qa[RT][NB][2];
+  float scale[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        qa[rt][nb][s] = *reinterpret_cast<const v4i*>(q_dig + (rt * 16 + n16) * P + nb * kPageBlock + g4 * 32 + s * 16);
+    scale[rt] = h_scale[rt * kRowHeads + g4];
+  }
+
+  // ---- the tiles -----------------------------------------------------------------------------------------------
+  unsigned char* p_buf = smem + kQBytes + wave * (RT * 1024);
+  const QuadSel sel = quad_sel(lane);
+  float m_run[RT], l_run[RT], acc[RT][NB][8];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m_run[rt] = kNone;
+    l_run[rt] = 0.0f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[rt][nb][e] = 0.0f;
+  }
+  for (int k = 0; k < my_tiles; ++k) {
+    v4i c[RT][4];
+    bool ok[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      ok[r] = token_of(k) + r * 16 + n16 < part.len && __builtin_amdgcn_readlane(ids, (k & 15) * 4 + r) >= 0;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) c[rt][r] = v4i{0, 0, 0, 0};
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        uint32_t w[8];
+        expand<BITS>(kr[r][nb], w);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const v4i kb = {static_cast<int>(w[4 * s]), static_cast<int>(w[4 * s + 1]), static_cast<int>(w[4 * s + 2]), static_cast<int>(w[4 * s + 3])};
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) c[rt][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[rt][nb][s], kb, c[rt][r], 0, 0, 0);
+        }
+      }
+    }
+    const bool more = k + 1 < my_tiles;
+    if (more && ((k + 1) & 15) == 0) {
+      ids = ids_next;
+      ids_next = k + 17 < my_tiles ? pages_from(k + 17) : -1;
+    }
+    if (more) load_tile(k + 1, a.k_pages, k_off, kr);
+
+    // weights of the tile, relative to its largest, as digits: lane (head g4, token n16 of every 16) -> operand lane (row n16, tokens of g4)
+    float alpha[RT], beta[RT];
+    v4i pa[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float s[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[r] = ok[r] ? undigit(c[rt][r]) * scale[rt] : kNone;
+      const float top = row16_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+      const float m_new = fmaxf(m_run[rt], top);
+      alpha[rt] = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+      beta[rt] = __builtin_amdgcn_exp2f(top - m_new);
+      float sum = 0.0f;
+      v4i d;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float e = ok[r] ? __builtin_amdgcn_exp2f((s[r] - top) + 30.0f) : 0.0f;
+        sum += e;
+        d[r] = static_cast<int>(quad_transpose(digits(static_cast<int>(e)), sel));
+      }
+      l_run[rt] = fmaf(l_run[rt], alpha[rt], sum * beta[rt]);
+      m_run[rt] = m_new;
+      *reinterpret_cast<v4i*>(p_buf + rt * 1024 + (g4 * 4 + (n16 & 3)) * 64 + (n16 >> 2) * 16) = d;
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) pa[rt] = *reinterpret_cast<const v4i*>(p_buf + rt * 1024 + n16 * 64 + g4 * 16);
+    wave_lds_fence();
+
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      uint32_t w[4][8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint32_t t[BITS];
+#pragma unroll
+        for (int i = 0; i < BITS; ++i) t[i] = quad_transpose(vr[r][nb][i], sel);
+        expand<BITS>(t, w[r]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const v4i vb = {static_cast<int>(w[0][e]), static_cast<int>(w[1][e]), static_cast<int>(w[2][e]), static_cast<int>(w[3][e])};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const v4i o = __builtin_amdgcn_mfma_i32_16x16x64_i8(pa[rt], vb, v4i{0, 0, 0, 0}, 0, 0, 0);
+          acc[rt][nb][e] = fmaf(acc[rt][nb][e], alpha[rt], undigit(o) * beta[rt]);
+        }
+      }
+    }
+    if (more) load_tile(k + 1, a.v_pages, v_off, vr);
+  }
+
+  // ---- the waves' sums together ------------------------------------------------------------------------------------
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float l = row16_add(l_run[rt]);
+    if (n16 == 0) w_ml[wave][rt * kRowHeads + g4] = make_float2(m_run[rt], l);
+  }
+  const PartBuffers buf = part_buffers(a, plan);
+  const bool whole = part.count == 1;
+  if (part.index == 0 && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
+  float* merge = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    __syncthreads();                                       // (everybody is done with what lies there)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        merge[(wave * kRowHeads + g4) * P + nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+      const int pos = tid % P, g = (i * 256 + tid) / P, hh = rt * kRowHeads + g;
+      if (hh >= heads || !own(hh, pos)) continue;
+      float m = kNone, l = 0.0f, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, w_ml[w][hh].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(w_ml[w][hh].x - m);
+        l = fmaf(w_ml[w][hh].y, f, l);
+        sum = fmaf(merge[(w * kRowHeads + g) * P + pos], f, sum);
+      }
+      sum *= 1.0f / (1 << kShift);
+      const int h = q_head + hh, at = NB == 2 ? pos : pos & (a.hd - 1);
+      if (whole) {
+        store_out(a, f32, part.b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
+        if (a.lse && at == 0) a.lse[static_cast<int64_t>(part.b) * a.n_q + h] = finish_lse(m, l, h_z[hh]);
+      } else {
+        const int64_t row = static_cast<int64_t>(slot) * a.n_q + h;
+        buf.acc[row * a.hd + at] = sum;
+        if (at == 0) buf.heads[row] = PartHead{m, l, h_z[hh], 0.0f};
+      }
+    }
+  }
+}
+
+// ---- the parts of a sequence together: a workgroup per (sequence, query head) ------------------------------------
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPlan plan, bool f32) {
+  __shared__ float weight[256], red[8], merge[256 * 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x % a.n_q, b = blockIdx.x / a.n_q;
+  const PartBuffers buf = part_buffers(a, plan);
+  const int2 where = buf.where[b];
+  if (where.y <= 1) return;
+  const PartHead* heads = buf.heads + static_cast<int64_t>(where.x) * a.n_q + h;
+  float m = kNone;
+  for (int i = tid; i < where.y; i += 256) m = fmaxf(m, heads[static_cast<int64_t>(i) * a.n_q].m);
+  m = wave_max(m);
+  if (lane == 0) red[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  // a thread: channels c, c + 64.. of the head in every (256 / lanes)-th part
+  const int per = min(a.hd, 64), c = tid % per, p0 = tid / per, step = 256 / per, n_c = a.hd / per;
+  float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int base = 0; base < where.y; base += 256) {
+    const int n = min(256, where.y - base);
+    __syncthreads();
+    if (tid < n) {
+      const PartHead ph = heads[static_cast<int64_t>(base + tid) * a.n_q];
+      weight[tid] = __builtin_amdgcn_exp2f(ph.m - m);
+      l = fmaf(ph.l, weight[tid], l);
+    }
+    __syncthreads();
+    const float* src = buf.acc + ((static_cast<int64_t>(where.x) + base) * a.n_q + h) * a.hd;
+#pragma unroll 4
+    for (int i = p0; i < n; i += step) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < n_c) acc[j] = fmaf(src[static_cast<int64_t>(i) * a.n_q * a.hd + j * per + c], weight[i], acc[j]);
+    }
+  }
+  l = row16_add(l);
+  auto row = [&](int at) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), at)); };
+  l = (row(0) + row(16)) + (row(32) + row(48));
+  if (lane == 0) red[4 + wave] = l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) merge[j * 256 + tid] = acc[j];
+  __syncthreads();
+  l = (red[4] + red[5]) + (red[6] + red[7]);
+  if (tid < a.hd) {
+    const int kvh = h / (a.n_q / a.n_kv);
+    const KvPos vp = a.v_pos[kvh * a.hd + tid];
+    float sum = 0.0f;
+    for (int i = 0; i < step; ++i) sum += merge[tid / per * 256 + i * per + tid % per];
+    store_out(a, f32, b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
+    if (a.lse && tid == 0) a.lse[static_cast<int64_t>(b) * a.n_q + h] = finish_lse(m, l, heads[0].zterm);
+  }
+}
+
+template <int BITS, int NB, int RT>
+static void launch_parts(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
+  const int64_t cells = (static_cast<int64_t>(p.slots) * p.units + 7) / 8 * 8 * p.chunks;
+  const double per_part = 1.0 / p.parts * (1.0 + 0x1p-50);
+  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), dim3(static_cast<unsigned>(cells)), dim3(256), 0, st, a, p, per_part, f32);
+}
+
+template <int BITS>
+static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
+  const int tiles = (p.chunk_heads + kRowHeads - 1) / kRowHeads;
+  if (a.hd > kPageBlock) {
+    if (tiles <= 1) launch_parts<BITS, 2, 1>(a, p, f32, st);
+    else launch_parts<BITS, 2, 2>(a, p, f32, st);
+  } else {
+    if (tiles <= 1) launch_parts<BITS, 1, 1>(a, p, f32, st);
+    else if (tiles == 2) launch_parts<BITS, 1, 2>(a, p, f32, st);
+    else launch_parts<BITS, 1, 4>(a, p, f32, st);
+  }
+}
 
 int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype, hipStream_t st) {
   if (a.B == 0) return RPTQ_OK;
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(a.B) * a.n_q), dim3(256), 0, st, a); };
   const bool f32 = out_dtype == RPTQ_DTYPE_F32;
-  if (bits == 3) f32 ? go(attend_paged_kernel<3, true>) : go(attend_paged_kernel<3, false>);
-  else if (bits == 4) f32 ? go(attend_paged_kernel<4, true>) : go(attend_paged_kernel<4, false>);
-  else f32 ? go(attend_paged_kernel<8, true>) : go(attend_paged_kernel<8, false>);
+  const AttendPlan p = attend_plan(a.B, a.n_q, a.n_kv, a.hd);
+  if (bits == 3) launch_bits<3>(a, p, f32, st);
+  else if (bits == 4) launch_bits<4>(a, p, f32, st);
+  else launch_bits<8>(a, p, f32, st);
+  RPTQ_HIP(hipGetLastError());
+  // (a sequence that cannot be longer than the shortest part is never cut)
+  if ((static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift) <= kLeastTiles * kTile) return RPTQ_OK;
+  hipLaunchKernelGGL(attend_join_kernel, dim3(static_cast<unsigned>(a.B) * a.n_q), dim3(256), 0, st, a, p, f32);
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;
 }
