@@ -131,12 +131,14 @@ def _set_up_calls(lib):
     try:
         import torch
         from . import _calls
-        objects = dict(bfloat16=torch.bfloat16, float32=torch.float32, int32=torch.int32, get_device=torch._C._cuda_getDevice,
+        objects = dict(bfloat16=torch.bfloat16, float32=torch.float32, int32=torch.int32, int64=torch.int64,
+                       uint8=torch.uint8, get_device=torch._C._cuda_getDevice,
                        get_stream=torch._C._cuda_getCurrentRawStream)
     except (ImportError, AttributeError):
         return
     names = ("rptq_ln_quant", "rptq_cluster_gemm", "rptq_cluster_gemm_quant", "rptq_cluster_rowsums", "rptq_cluster_gemm_cw",
-             "rptq_kv_quant", "rptq_kv_dequant")
+             "rptq_kv_quant", "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
+             "rptq_attend_paged")
     _calls.setup({n: C.cast(getattr(lib, n), C.c_void_p).value for n in names}, objects)
     _CALLS = _calls
 
@@ -662,26 +664,30 @@ def rptq_kv_page_bytes(d: int, page_size: int, bits: int) -> int:
 
 def rptq_kv_quant_paged(k, v, slots, k_table, v_table, bits: int, k_pages, v_pages, page_size: int, stream=None):
     """k, v: bf16 [T, d], rows of any stride; slots: int64 [T]; pages: uint8, a whole number of pages."""
-    import torch
-    T, d = _tokens(k, v, slots)
-    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-    (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
-    st = load_library().rptq_kv_quant_paged(
-        ka, ld_k, va, ld_v, T, d, _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), bits,
-        _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
+    st = None if _CALLS is None else _CALLS.kv_quant_paged(k, v, slots, k_table, v_table, bits, k_pages, v_pages, page_size, stream)
+    if st is None:
+        import torch
+        T, d = _tokens(k, v, slots)
+        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+        st = load_library().rptq_kv_quant_paged(
+            ka, ld_k, va, ld_v, T, d, _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), bits,
+            _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
     _check(st, "rptq_kv_quant_paged")
 
 
 def rptq_kv_dequant_paged(k_pages, v_pages, page_size: int, bits: int, slots, k_table, v_table, k, v, stream=None):
     """k, v: bf16 [T, d] out, rows of any stride; slots: int64 [T]."""
-    import torch
-    T, d = _tokens(k, v, slots)
-    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-    (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
-    st = load_library().rptq_kv_dequant_paged(
-        kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
-        _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), ka, ld_k, va, ld_v,
-        _stream(stream)) if T else 0
+    st = None if _CALLS is None else _CALLS.kv_dequant_paged(k_pages, v_pages, page_size, bits, slots, k_table, v_table, k, v, stream)
+    if st is None:
+        import torch
+        T, d = _tokens(k, v, slots)
+        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+        st = load_library().rptq_kv_dequant_paged(
+            kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
+            _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), ka, ld_k, va, ld_v,
+            _stream(stream)) if T else 0
     _check(st, "rptq_kv_dequant_paged")
 
 
@@ -693,26 +699,30 @@ def rptq_attend_paged(q, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: 
                       v_pages, page_size: int, page_table, lens, out, lse, workspace, stream=None):
     """q, out: [B, n_q_heads * head_dim], rows of any stride; page_table: int32 [B, pages]; lens: int32 [B];
     lse: fp32 [B, n_q_heads] or None."""
-    import torch
-    B, d = q.shape[0], n_kv_heads * head_dim
-    kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-    if out.dtype == torch.float32:
-        out_dtype = DTYPE_F32
-    elif out.dtype == torch.bfloat16:
-        out_dtype = DTYPE_BF16
-    else:
-        raise ValueError("out must be bf16 or fp32")
-    if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != B:
-        raise ValueError("expected page_table [B, pages] and lens [B]")
-    qa, ld_q = _matrix(q, torch.bfloat16, "q", (B, n_q_heads * head_dim))
-    oa, ld_out = _matrix(out, None, "out", (B, n_q_heads * head_dim))
-    pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
-    la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
-    st = load_library().rptq_attend_paged(
-        qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _whole(k_table, None, "k_table", 16 * d),
-        _whole(v_table, None, "v_table", 16 * d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
-        _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
-        workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+    st = None if _CALLS is None else _CALLS.attend_paged(
+        q, n_q_heads, n_kv_heads, head_dim, scale, k_table, v_table, bits, k_pages, v_pages, page_size, page_table, lens, out, lse,
+        workspace, stream)
+    if st is None:
+        import torch
+        B, d = q.shape[0], n_kv_heads * head_dim
+        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+        if out.dtype == torch.float32:
+            out_dtype = DTYPE_F32
+        elif out.dtype == torch.bfloat16:
+            out_dtype = DTYPE_BF16
+        else:
+            raise ValueError("out must be bf16 or fp32")
+        if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != B:
+            raise ValueError("expected page_table [B, pages] and lens [B]")
+        qa, ld_q = _matrix(q, torch.bfloat16, "q", (B, n_q_heads * head_dim))
+        oa, ld_out = _matrix(out, None, "out", (B, n_q_heads * head_dim))
+        pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
+        la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
+        st = load_library().rptq_attend_paged(
+            qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _whole(k_table, None, "k_table", 16 * d),
+            _whole(v_table, None, "v_table", 16 * d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
+            _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
+            workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_paged")
 
 

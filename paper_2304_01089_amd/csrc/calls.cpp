@@ -21,9 +21,13 @@ decltype(&rptq_cluster_rowsums) f_cluster_rowsums;
 decltype(&rptq_cluster_gemm_cw) f_cluster_gemm_cw;
 decltype(&rptq_kv_quant) f_kv_quant;
 decltype(&rptq_kv_dequant) f_kv_dequant;
+decltype(&rptq_kv_page_bytes) f_kv_page_bytes;
+decltype(&rptq_kv_quant_paged) f_kv_quant_paged;
+decltype(&rptq_kv_dequant_paged) f_kv_dequant_paged;
+decltype(&rptq_attend_paged) f_attend_paged;
 
-PyObject *n_is_cuda, *n_is_contiguous, *n_dtype, *n_data_ptr, *n_nbytes;     // attribute names
-PyObject *t_bf16, *t_f32, *t_i32, *get_device, *get_stream;         // torch's objects
+PyObject *n_is_cuda, *n_is_contiguous, *n_dtype, *n_data_ptr, *n_nbytes, *n_get_device, *n_shape, *n_stride;     // attribute names
+PyObject *t_bf16, *t_f32, *t_i32, *t_i64, *t_u8, *get_device, *get_stream;         // torch's objects
 
 // Each getter returns false, with no Python error set, where the ordinary case does not apply.
 bool no_error() {
@@ -257,6 +261,150 @@ PyObject* kv_call(PyObject* const* a, Py_ssize_t n, bool quant) {
 PyObject* kv_quant(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_call(a, n, true); }
 PyObject* kv_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_call(a, n, false); }
 
+// ---- the cache in pages: tensors whose sizes, strides and device count ----------------------------------
+// The current device and its current stream.
+bool get_place(PyObject* stream, int64_t* device, void** out) {
+  if (stream != Py_None) return false;
+  PyObject* d = PyObject_CallNoArgs(get_device);
+  if (d == nullptr) return no_error();
+  PyObject* s = PyObject_CallOneArg(get_stream, d);
+  const bool ok = s != nullptr && PyLong_Check(s) && get_i64(d, device);
+  *out = ok ? PyLong_AsVoidPtr(s) : nullptr;
+  Py_DECREF(d);
+  Py_XDECREF(s);
+  return (ok && !PyErr_Occurred()) || no_error();
+}
+
+bool int_of(PyObject* owned, int64_t* out) {
+  if (owned == nullptr) return no_error();
+  const bool ok = get_i64(owned, out);
+  Py_DECREF(owned);
+  return ok;
+}
+
+// Address of a tensor of that dtype (any if NULL) on that device.
+template <typename T>
+bool get_on(PyObject* t, PyObject* dtype, int64_t device, T** out) {
+  int64_t at;
+  if (!int_of(PyObject_CallMethodNoArgs(t, n_get_device), &at) || at != device || at < 0) return false;
+  if (dtype != nullptr && dtype_of(t) != dtype) return false;
+  PyObject* p = PyObject_CallMethodNoArgs(t, n_data_ptr);
+  if (p == nullptr) return no_error();
+  *out = static_cast<T*>(PyLong_Check(p) ? PyLong_AsVoidPtr(p) : nullptr);
+  Py_DECREF(p);
+  return !PyErr_Occurred() || no_error();
+}
+
+// The same of a contiguous one with `bytes` bytes.
+template <typename T>
+bool get_whole(PyObject* t, PyObject* dtype, int64_t device, T** out, int64_t* bytes) {
+  return get_on(t, dtype, device, out) && is_true(PyObject_CallMethodNoArgs(t, n_is_contiguous)) && get_bytes(t, bytes);
+}
+
+// The first `n` entries of a tuple of exactly so many.
+bool get_sizes(PyObject* owned, int n, int64_t* out) {
+  if (owned == nullptr) return no_error();
+  bool ok = PyTuple_Check(owned) && PyTuple_GET_SIZE(owned) == n;
+  for (int i = 0; ok && i < n; ++i) ok = get_i64(PyTuple_GET_ITEM(owned, i), out + i);
+  Py_DECREF(owned);
+  return ok;
+}
+
+// A two-dimensional tensor with contiguous rows, at least one of them.
+struct Rows {
+  void* at;
+  int64_t rows, cols, ld;
+  bool get(PyObject* t, PyObject* dtype, int64_t device) {
+    int64_t size[2], step[2];
+    if (!get_on(t, dtype, device, &at) || !get_sizes(PyObject_GetAttr(t, n_shape), 2, size) ||
+        !get_sizes(PyObject_CallMethodNoArgs(t, n_stride), 2, step))
+      return false;
+    rows = size[0], cols = size[1];
+    ld = rows > 1 ? step[0] : cols;
+    return rows >= 1 && cols > 1 && cols <= INT32_MAX && step[1] == 1;
+  }
+};
+
+// Both tensors' pages and tables: the same whole number of pages, and a record for each of d positions.
+struct Pages {
+  uint8_t *k, *v;
+  void *k_table, *v_table;
+  int64_t n;
+  bool get(PyObject* kp, PyObject* vp, PyObject* kt, PyObject* vt, int64_t device, int64_t d, int32_t page_size, int32_t bits) {
+    int64_t kb, vb, ktb, vtb;
+    if (d < 1 || d > RPTQ_MAX_CHANNELS) return false;
+    const int64_t size = static_cast<int64_t>(f_kv_page_bytes(static_cast<int32_t>(d), page_size, bits));
+    if (size == 0 || !get_whole(kp, t_u8, device, &k, &kb) || !get_whole(vp, t_u8, device, &v, &vb) || kb != vb || kb < size || kb % size != 0)
+      return false;
+    n = kb / size;
+    return get_whole(kt, nullptr, device, &k_table, &ktb) && get_whole(vt, nullptr, device, &v_table, &vtb) && ktb >= 16 * d && vtb >= 16 * d;
+  }
+};
+
+bool get_slots(PyObject* t, int64_t device, int64_t rows, int64_t** out) {
+  int64_t bytes, size;
+  return get_whole(t, t_i64, device, out, &bytes) && get_sizes(PyObject_GetAttr(t, n_shape), 1, &size) && size == rows;
+}
+
+// (k, v, slots, k_table, v_table, bits, k_pages, v_pages, page_size, stream)
+PyObject* kv_quant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows k, v;
+  Pages p;
+  int64_t device, *slots;
+  int32_t bits, page_size;
+  void* stream;
+  if (n != 10 || f_kv_quant_paged == nullptr || !get_place(a[9], &device, &stream) || !get_i32(a[5], &bits) || !get_i32(a[8], &page_size) ||
+      !k.get(a[0], t_bf16, device) || !v.get(a[1], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !get_slots(a[2], device, k.rows, &slots) || !p.get(a[6], a[7], a[3], a[4], device, k.cols, page_size, bits))
+    Py_RETURN_NONE;
+  return run([&] {
+    return f_kv_quant_paged(k.at, k.ld, v.at, v.ld, k.rows, static_cast<int32_t>(k.cols), p.k_table, p.v_table, bits, slots, p.k, p.v, p.n,
+                            page_size, stream);
+  });
+}
+
+// (k_pages, v_pages, page_size, bits, slots, k_table, v_table, k, v, stream)
+PyObject* kv_dequant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows k, v;
+  Pages p;
+  int64_t device, *slots;
+  int32_t bits, page_size;
+  void* stream;
+  if (n != 10 || f_kv_dequant_paged == nullptr || !get_place(a[9], &device, &stream) || !get_i32(a[3], &bits) || !get_i32(a[2], &page_size) ||
+      !k.get(a[7], t_bf16, device) || !v.get(a[8], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !get_slots(a[4], device, k.rows, &slots) || !p.get(a[0], a[1], a[5], a[6], device, k.cols, page_size, bits))
+    Py_RETURN_NONE;
+  return run([&] {
+    return f_kv_dequant_paged(p.k, p.v, p.n, page_size, bits, slots, k.rows, static_cast<int32_t>(k.cols), p.k_table, p.v_table, k.at, k.ld,
+                              v.at, v.ld, stream);
+  });
+}
+
+// (q, n_q_heads, n_kv_heads, head_dim, scale, k_table, v_table, bits, k_pages, v_pages, page_size, page_table, lens, out, lse, workspace, stream)
+PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows q, table, out;
+  Pages p;
+  int64_t device, lens_bytes, lse_bytes = 0, ws_bytes, b;
+  int32_t n_q, n_kv, hd, bits, page_size, *lens, out_dtype;
+  float scale, *lse = nullptr;
+  void *workspace, *stream;
+  if (n != 17 || f_attend_paged == nullptr || !get_place(a[16], &device, &stream) || !get_i32(a[1], &n_q) || !get_i32(a[2], &n_kv) ||
+      !get_i32(a[3], &hd) || !get_f32(a[4], &scale) || !get_i32(a[7], &bits) || !get_i32(a[10], &page_size) || n_q < 1 || n_kv < 1 || hd < 1 ||
+      !q.get(a[0], t_bf16, device) || q.cols != static_cast<int64_t>(n_q) * hd || q.rows > INT32_MAX)
+    Py_RETURN_NONE;
+  if (!p.get(a[8], a[9], a[5], a[6], device, static_cast<int64_t>(n_kv) * hd, page_size, bits) || !get_y_dtype(a[13], &out_dtype) ||
+      !out.get(a[13], nullptr, device) || out.rows != q.rows || out.cols != q.cols || !table.get(a[11], t_i32, device) ||
+      table.rows != q.rows || !get_whole(a[12], t_i32, device, &lens, &lens_bytes) ||
+      !get_sizes(PyObject_GetAttr(a[12], n_shape), 1, &b) || b != q.rows || !get_whole(a[15], nullptr, device, &workspace, &ws_bytes))
+    Py_RETURN_NONE;
+  if (a[14] != Py_None && (!get_whole(a[14], t_f32, device, &lse, &lse_bytes) || lse_bytes < 4 * q.rows * n_q)) Py_RETURN_NONE;
+  return run([&] {
+    return f_attend_paged(q.at, q.ld, static_cast<int32_t>(q.rows), n_q, n_kv, hd, scale, p.k_table, p.v_table, bits, p.k, p.v, p.n,
+                          page_size, static_cast<int32_t*>(table.at), table.ld, static_cast<int32_t>(table.cols), lens, out.at, out.ld,
+                          out_dtype, lse, workspace, static_cast<size_t>(ws_bytes), stream);
+  });
+}
+
 template <typename F>
 bool set_entry(PyObject* addresses, const char* name, F* f) {
   PyObject* o = PyDict_GetItemString(addresses, name);   // (borrowed)
@@ -274,7 +422,7 @@ PyObject* setup(PyObject*, PyObject* args) {
   PyObject *addresses, *objects;
   if (!PyArg_ParseTuple(args, "O!O!", &PyDict_Type, &addresses, &PyDict_Type, &objects)) return nullptr;
   const struct { const char* name; PyObject** at; } wanted[] = {
-      {"bfloat16", &t_bf16}, {"float32", &t_f32}, {"int32", &t_i32}, {"get_device", &get_device}, {"get_stream", &get_stream}};
+      {"bfloat16", &t_bf16}, {"float32", &t_f32}, {"int32", &t_i32}, {"int64", &t_i64}, {"uint8", &t_u8}, {"get_device", &get_device}, {"get_stream", &get_stream}};
   for (const auto& w : wanted) {
     PyObject* o = PyDict_GetItemString(objects, w.name);
     if (o == nullptr) return PyErr_Format(PyExc_KeyError, "%s", w.name);
@@ -285,7 +433,9 @@ PyObject* setup(PyObject*, PyObject* args) {
       !set_entry(addresses, "rptq_cluster_gemm_quant", &f_cluster_gemm_quant) ||
       !set_entry(addresses, "rptq_cluster_rowsums", &f_cluster_rowsums) ||
       !set_entry(addresses, "rptq_cluster_gemm_cw", &f_cluster_gemm_cw) || !set_entry(addresses, "rptq_kv_quant", &f_kv_quant) ||
-      !set_entry(addresses, "rptq_kv_dequant", &f_kv_dequant))
+      !set_entry(addresses, "rptq_kv_dequant", &f_kv_dequant) || !set_entry(addresses, "rptq_kv_page_bytes", &f_kv_page_bytes) ||
+      !set_entry(addresses, "rptq_kv_quant_paged", &f_kv_quant_paged) ||
+      !set_entry(addresses, "rptq_kv_dequant_paged", &f_kv_dequant_paged) || !set_entry(addresses, "rptq_attend_paged", &f_attend_paged))
     return nullptr;
   Py_RETURN_NONE;
 }
@@ -293,7 +443,8 @@ PyObject* setup(PyObject*, PyObject* args) {
 #define RPTQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RPTQ_METHOD(ln_quant), RPTQ_METHOD(cluster_gemm), RPTQ_METHOD(cluster_gemm_quant),
                          RPTQ_METHOD(cluster_rowsums), RPTQ_METHOD(cluster_gemm_cw), RPTQ_METHOD(kv_quant),
-                         RPTQ_METHOD(kv_dequant), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         RPTQ_METHOD(kv_dequant), RPTQ_METHOD(kv_quant_paged), RPTQ_METHOD(kv_dequant_paged),
+                         RPTQ_METHOD(attend_paged), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -304,6 +455,9 @@ PyMODINIT_FUNC PyInit__calls(void) {
   n_dtype = PyUnicode_InternFromString("dtype");
   n_data_ptr = PyUnicode_InternFromString("data_ptr");
   n_nbytes = PyUnicode_InternFromString("nbytes");
-  if (!n_is_cuda || !n_is_contiguous || !n_dtype || !n_data_ptr || !n_nbytes) return nullptr;
+  n_get_device = PyUnicode_InternFromString("get_device");
+  n_shape = PyUnicode_InternFromString("shape");
+  n_stride = PyUnicode_InternFromString("stride");
+  if (!n_is_cuda || !n_is_contiguous || !n_dtype || !n_data_ptr || !n_nbytes || !n_get_device || !n_shape || !n_stride) return nullptr;
   return PyModule_Create(&module);
 }

@@ -545,3 +545,63 @@ def test_calls_of_nothing(rp):
     assert k.shape == v.shape == (0, 128) and torch.equal(b.cache.k_pages, before)
     out, lse = rp.attend_paged(b.cache, x, b.page_table[:0], b.dev_lens[:0], want_lse=True)
     assert out.shape == (0, 128) and lse.shape == (0, 2)
+
+
+def test_native_and_python_marshalling(rp, monkeypatch):
+    """Ordinary arguments are taken natively, with the results that the Python marshalling leads to; an argument out of the
+    ordinary, whichever it is, is not (None, and nothing written)."""
+    from paper_2304_01089_amd import binding
+    b = Batch(rp, [100, 37], 2, 64, 4, 16)
+    c, gen = b.cache, torch.Generator(device="cuda").manual_seed(1)
+    wide = torch.randn(3, 400, generator=gen, device="cuda").bfloat16()
+    k, v, slots = wide[:, :128], wide[:, 128:256], torch.tensor([3, 70, -1], device="cuda")
+    pages = c.k_pages.clone(), c.v_pages.clone()
+    back = torch.zeros(2, 3, 128, dtype=torch.bfloat16, device="cuda")
+    q, out, lse = wide[:2, 136:392], torch.zeros(2, 256, device="cuda"), torch.zeros(2, 4, device="cuda")
+    ws = rp.attend_paged_workspace(c, 2, 4)
+    calls = [
+        ("kv_quant_paged", (k, v, slots, c.k_table, c.v_table, 4) + pages + (16, None), pages),
+        ("kv_dequant_paged", pages + (16, 4, slots, c.k_table, c.v_table, back[0], back[1], None), (back,)),
+        ("attend_paged", (q, 4, 2, 64, 0.125, c.k_table, c.v_table, 4, c.k_pages, c.v_pages, 16, b.page_table, b.dev_lens, out, lse, ws, None),
+         (out, lse)),
+        ("attend_paged", (q, 4, 2, 64, 0.125, c.k_table, c.v_table, 4, c.k_pages, c.v_pages, 16, b.page_table, b.dev_lens, out.bfloat16(), None,
+                          ws, None), ()),
+    ]
+    for name, args, outs in calls:
+        native, entry = getattr(binding._CALLS, name), getattr(rp, "rptq_" + name)
+        start = [t.clone() for t in outs]
+        assert native(*args) == 0, name
+        got = [t.clone() for t in outs]
+        assert not outs or any(not torch.equal(a, s) for a, s in zip(got, start))
+        for t, s in zip(outs, start):
+            t.copy_(s)
+        with monkeypatch.context() as m:
+            m.setattr(binding, "_CALLS", None)
+            m.setattr(binding, "_CALLS_SOUGHT", True)
+            entry(*args)
+        assert all(torch.equal(a, t) for a, t in zip(got, outs)), name
+        for t in outs:
+            t.view(torch.uint8).fill_(0x3c)
+        torch.cuda.synchronize()
+        for i, a in enumerate(args):
+            if isinstance(a, torch.Tensor):
+                odd = [a.cpu(), a.to(torch.float64 if a.dtype != torch.float64 else torch.int8), 1, a[None], a.reshape(-1)[:1]]
+                if a is not lse:
+                    odd.append(None)
+                if a is ws or a is c.k_table or a is c.v_table:            # (bytes of any type, as long as there are enough)
+                    odd = [a.cpu(), 1, None] + ([a.reshape(-1)[:8]] if a is not ws else [])
+                elif a is lse or a.dtype == torch.uint8:                   # (any shape)
+                    odd = odd[:3] + odd[4:]
+                if a is pages[0] or a is pages[1] or a is c.k_pages or a is c.v_pages:
+                    odd.append(a[:-1])
+            elif a is None:
+                odd = [torch.cuda.current_stream()] if i == len(args) - 1 else [1]
+            elif isinstance(a, float):
+                odd = [1, np.float32(0.1)]
+            else:
+                odd = [float(a), np.int64(a), 1 << 80, 0, -a]
+            for o in odd:
+                assert native(*args[:i], o, *args[i + 1:]) is None, (name, i, o)
+        assert native(*args[:-1]) is None and native(*args, None) is None, name
+        torch.cuda.synchronize()
+        assert all((t.view(torch.uint8) == 0x3c).all() for t in outs), name
