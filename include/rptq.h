@@ -454,7 +454,7 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
  * Sums and softmax statistics are fp32 or exact integers; a sequence's last bits may depend on
  * the other lengths of the call (they decide where sequences are split).  A NaN or infinity in q, or a
  * score beyond fp32, makes its head's output NaN.
- * pages_per_seq * page_size <= 2^30; strides (ld_*) are >= the row and, but for the page table's, multiples of 8.
+ * pages_per_seq * page_size <= 2^29; strides (ld_*) are >= the row and, but for the page table's, multiples of 8.
  *
  * All three are asynchronous on `stream`, allocate nothing and may be recorded into a graph after the first
  * call on the device.  Device pointers are 16-byte aligned, slots 8-byte, page_table and lens 4-byte.

@@ -418,7 +418,7 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
   const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
   if (!row_stride_ok(ld_q, row) || !row_stride_ok(ld_out, row)) return RPTQ_ERR_SHAPE;
   if (pages_per_seq < 1 || ld_page_table < pages_per_seq) return RPTQ_ERR_SHAPE;
-  if (static_cast<int64_t>(pages_per_seq) * page_size > (INT64_C(1) << 30)) return RPTQ_ERR_SHAPE;
+  if (static_cast<int64_t>(pages_per_seq) * page_size > (INT64_C(1) << 29)) return RPTQ_ERR_SHAPE;
   if (out_dtype != RPTQ_DTYPE_BF16 && out_dtype != RPTQ_DTYPE_F32) return RPTQ_ERR_SHAPE;
   if (!std::isfinite(scale)) return RPTQ_ERR_RANGE;
   if (workspace_bytes < attend_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim)) return RPTQ_ERR_WORKSPACE;

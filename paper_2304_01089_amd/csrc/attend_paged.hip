@@ -29,23 +29,27 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
 constexpr int kTile = 64;                      // tokens of a wave's tile
-constexpr int kLeastTiles = 4;                 // of a part: one per wave
+constexpr int kMidTiles = 16;                  // of a part: four per wave
+constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
 __host__ __device__ constexpr int most_row_tiles(int blocks) { return blocks == 2 ? 2 : 4; }
+
+__host__ __device__ constexpr int row_tiles(int heads) { return (heads + kRowHeads - 1) / kRowHeads; }
 
 // How a call is laid out; from sizes alone, so that the workspace's is known before the lengths are.
 struct AttendPlan {
   int32_t units;                               // blocks of positions (heads 256 wide: pairs of blocks)
   int32_t unit_heads;                          // query heads that read a unit
   int32_t chunks, chunk_heads;                 // these heads in equal groups, each a workgroup's
-  int32_t parts;                               // parts that the tokens of the batch are cut in (one more per sequence, from rounding up)
-  int32_t slots;                               // parts + B
+  int32_t least;                               // tiles of a part at least
+  bool join;                                   // whether a sequence may be cut
+  double per_few, per_many;                    // 1 / parts, a little more, where the tokens of the batch are cut in few, and in many
+  int32_t slots;                               // parts that there may be: one more per sequence, from rounding up
 };
 
-static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
-  constexpr int kWorkgroups = 1024;            // four per compute unit of 256
+static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, int64_t most_tokens) {
   AttendPlan p;
   const int unit = hd > kPageBlock ? hd : kPageBlock;
   p.units = n_kv * hd / unit;
@@ -54,8 +58,17 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) 
   p.chunks = (p.unit_heads + most - 1) / most;
   p.chunk_heads = (p.unit_heads + p.chunks - 1) / p.chunks;
   const int each = p.units * p.chunks;
-  p.parts = std::max(1, (kWorkgroups + each - 1) / each);
-  p.slots = p.parts + B;
+  auto parts = [&](int workgroups) { return std::max(1, (workgroups + each - 1) / each); };
+  p.per_few = 1.0 / parts(kFewWorkgroups) * (1.0 + 0x1p-50);
+  p.per_many = 1.0 / parts(kManyWorkgroups) * (1.0 + 0x1p-50);
+  // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch: 4 us, as long as a wave
+  // takes for three tiles of one block and one row tile.
+  const int whole = std::max(4, 16 / (unit / kPageBlock * row_tiles(p.chunk_heads)));
+  p.least = most_tokens <= whole * kTile ? whole : 1;
+  p.join = p.least == 1;
+  // (a sequence is cut in no more parts than its pages hold)
+  const int64_t per_seq = (most_tokens + p.least * kTile - 1) / (p.least * kTile);
+  p.slots = static_cast<int32_t>(std::min<int64_t>(parts(kManyWorkgroups) + static_cast<int64_t>(B), B * per_seq));
   return p;
 }
 
@@ -65,7 +78,7 @@ struct PartHead {
 };
 
 size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
-  const AttendPlan p = attend_plan(B, n_q, n_kv, hd);
+  const AttendPlan p = attend_plan(B, n_q, n_kv, hd, INT64_C(1) << 30);
   const size_t rows = static_cast<size_t>(p.slots) * n_q;
   return rows * sizeof(PartHead) + rows * hd * sizeof(float) + ((static_cast<size_t>(B) + 1) / 2) * 16;
 }
@@ -173,20 +186,30 @@ struct Part {
 };
 
 // The part that slot number `slot` holds; false: none.  Every sequence has at least one.
-__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, double per_part, int slot, int lane, Part* out) {
+__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int slot, int lane, Part* out) {
   const int cap = a.pages_per_seq << a.g.page_shift;
   auto len_of = [&](int i) { return i < a.B ? min(max(a.lens[i], 0), cap) : 0; };
   auto tiles_of = [](int n) { return (n + kTile - 1) / kTile; };
+  auto parts_of = [](int tiles, int n) {       // rounded up; (24 bits, which is all there is: a division by float)
+    return ((static_cast<uint32_t>(tiles) + n - 1) & 0xffffffu) / (static_cast<uint32_t>(n) & 0xffffffu);
+  };
   const int len0 = len_of(lane);
-  double total = tiles_of(len0);
-  for (int i = 64 + lane; i < a.B + lane; i += 64) total += tiles_of(len_of(i));
-  // tiles of a part: all tiles over the number of parts, rounded up (per_part is a little more than its reciprocal)
-  const int most = max(kLeastTiles, __builtin_amdgcn_readfirstlane(static_cast<int>((wave_sum(total) - 1.0) * per_part)) + 1);
+  double total;
+  if (a.B <= 64) {
+    total = __builtin_amdgcn_readlane(wave_prefix(tiles_of(len0)), 63);
+  } else {
+    total = tiles_of(len0);
+    for (int i = 64; i < a.B; i += 64) total += tiles_of(len_of(i + lane));
+    total = wave_sum(total);
+  }
+  // tiles of a part: all tiles over the number of parts, rounded up
+  auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>((total - 1.0) * per)) + 1; };
+  const int most = max(p.least, max(min(each_of(p.per_few), kMidTiles), each_of(p.per_many)));
   int before = 0;
   for (int base = 0; base < a.B; base += 64) {
     const int i = base + lane;
     const int len = base == 0 ? len0 : len_of(i);
-    const int n = i < a.B ? max(1, (tiles_of(len) + most - 1) / most) : 0;
+    const int n = i < a.B ? max<int>(1, parts_of(tiles_of(len), most)) : 0;
     const int upto = wave_prefix(n);
     const uint64_t hit = __ballot(slot >= before + upto - n && slot < before + upto);
     if (hit != 0) {
@@ -195,7 +218,7 @@ __device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan&
       out->len = __builtin_amdgcn_readlane(len, l);
       out->count = __builtin_amdgcn_readlane(n, l);
       out->index = slot - before - __builtin_amdgcn_readlane(upto, l) + out->count;
-      const int tiles = tiles_of(out->len), each = (tiles + out->count - 1) / out->count;
+      const int tiles = tiles_of(out->len), each = parts_of(tiles, out->count);
       out->first_tile = out->index * each;
       out->end_tile = min(out->first_tile + each, tiles);
       return true;
@@ -221,13 +244,13 @@ __device__ __forceinline__ float finish_lse(float m, float l, float zterm) {
 // ---- the parts ---------------------------------------------------------------------------------------------
 // NB: blocks of a unit; RT: row tiles (of four heads)
 template <int BITS, int NB, int RT>
-__global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, AttendPlan plan, double per_part, bool f32) {
+__global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_kernel(AttendArgs a, AttendPlan plan, bool f32) {
   constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
-  constexpr int kQBytes = RT * 16 * P, kPBytes = 4 * RT * 1024, kMergeBytes = 4 * kRowHeads * P * 4;
-  constexpr int kFront = kQBytes + kPBytes > kMergeBytes ? kQBytes + kPBytes : kMergeBytes;
-  __shared__ __align__(16) unsigned char smem[kFront];
+  constexpr int kQBytes = RT * 16 * P, kPBytes = 4 * RT * 1024;
+  __shared__ __align__(16) unsigned char smem[kQBytes + kPBytes];
+  __shared__ float merge[RT][4][kRowHeads][P];
   __shared__ float h_scale[RT * kRowHeads], h_z[RT * kRowHeads];
   __shared__ float2 w_ml[4][RT * kRowHeads];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -248,7 +271,7 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
   for (int i = 0; i < 2 * NB; ++i) kp[i] = kt[i * 64 + lane];
   const KvPos vp = a.v_pos[unit * P + tid % P];
   Part part;
-  if (!find_part(a, plan, per_part, slot, lane, &part)) return;
+  if (!find_part(a, plan, slot, lane, &part)) return;
 
   // ---- pages of this wave's tiles: lane 4k + i holds the page of its k-th tile's i-th 16 tokens, or -1 ---------
   const int32_t* pt = a.page_table + part.b * a.ld_pt;
@@ -261,6 +284,19 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
     return t < part.len && id >= 0 && id < a.g.n_pages ? id : -1;
   };
   int ids = my_tiles > 0 ? pages_from(0) : -1, ids_next = my_tiles > 16 ? pages_from(16) : -1;
+
+  const int share = a.n_q / a.n_kv;
+  const int first_head = chunk * plan.chunk_heads;
+  const int heads = min(plan.chunk_heads, plan.unit_heads - first_head);       // of this workgroup
+  const int q_head = unit * plan.unit_heads + first_head;                      // the first of them
+  auto own = [&](int hh, int pos) { return NB == 2 || pos / a.hd == (first_head + hh) / share; };
+  // (the queries, before the tiles: loads come back in order)
+  uint16_t q_raw[RT][2 * NB];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i)
+      q_raw[rt][i] = a.q[part.b * a.ld_q + (q_head + min(rt * kRowHeads + wave, heads - 1)) * a.hd + (kp[i].src & (a.hd - 1))];
 
   // K and V of a tile: lane (token n16, group g4) of every 16 tokens' keys; lane (group n16 / 4, token 4 g4 + n16 % 4) of the values
   const uint32_t k_off = n16 * kRow + g4 * (4 * BITS);
@@ -301,11 +337,6 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
   }
 
   // ---- queries to digits: wave w takes head w of every row tile ------------------------------------------------
-  const int share = a.n_q / a.n_kv;
-  const int first_head = chunk * plan.chunk_heads;
-  const int heads = min(plan.chunk_heads, plan.unit_heads - first_head);       // of this workgroup
-  const int q_head = unit * plan.unit_heads + first_head;                      // the first of them
-  auto own = [&](int hh, int pos) { return NB == 2 || pos / a.hd == (first_head + hh) / share; };
   unsigned char* q_dig = smem;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -314,11 +345,8 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) {
-      x[i] = 0.0f;
-      if (hh < heads && own(hh, i * 64 + lane)) {
-        const uint16_t h = a.q[part.b * a.ld_q + (q_head + hh) * a.hd + (kp[i].src & (a.hd - 1))];
-        x[i] = __uint_as_float(static_cast<uint32_t>(h) << 16) * kp[i].s * (a.scale * kLog2e);
-      }
+      x[i] = __uint_as_float(static_cast<uint32_t>(q_raw[rt][i]) << 16) * kp[i].s * (a.scale * kLog2e);
+      if (hh >= heads || !own(hh, i * 64 + lane)) x[i] = 0.0f;
       top = fmaxf(top, fabsf(x[i]));
       bad = bad || !(fabsf(x[i]) < __builtin_huge_valf());
     }
@@ -457,16 +485,15 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
   const PartBuffers buf = part_buffers(a, plan);
   const bool whole = part.count == 1;
   if (part.index == 0 && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
-  float* merge = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    __syncthreads();                                       // (everybody is done with what lies there)
+  for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        merge[(wave * kRowHeads + g4) * P + nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e];
-    __syncthreads();
+      for (int e = 0; e < 8; ++e) merge[rt][wave][g4][nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e];
+  __syncthreads();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) {
       const int pos = tid % P, g = (i * 256 + tid) / P, hh = rt * kRowHeads + g;
@@ -478,7 +505,7 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
       for (int w = 0; w < 4; ++w) {
         const float f = __builtin_amdgcn_exp2f(w_ml[w][hh].x - m);
         l = fmaf(w_ml[w][hh].y, f, l);
-        sum = fmaf(merge[(w * kRowHeads + g) * P + pos], f, sum);
+        sum = fmaf(merge[rt][w][g][pos], f, sum);
       }
       sum *= 1.0f / (1 << kShift);
       const int h = q_head + hh, at = NB == 2 ? pos : pos & (a.hd - 1);
@@ -495,53 +522,69 @@ __global__ void __launch_bounds__(256, 2) attend_part_kernel(AttendArgs a, Atten
 }
 
 // ---- the parts of a sequence together: a workgroup per (sequence, query head) ------------------------------------
+// A thread takes four channels of every (1024 / hd)-th part.
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPlan plan, bool f32) {
-  __shared__ float weight[256], red[8], merge[256 * 4];
+  __shared__ float weight[256], red[8];
+  __shared__ __align__(16) float merge[256 * 4];
+  typedef float f4 __attribute__((ext_vector_type(4)));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.x % a.n_q, b = blockIdx.x / a.n_q;
   const PartBuffers buf = part_buffers(a, plan);
   const int2 where = buf.where[b];
   if (where.y <= 1) return;
   const PartHead* heads = buf.heads + static_cast<int64_t>(where.x) * a.n_q + h;
-  float m = kNone;
-  for (int i = tid; i < where.y; i += 256) m = fmaxf(m, heads[static_cast<int64_t>(i) * a.n_q].m);
-  m = wave_max(m);
-  if (lane == 0) red[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  // a thread: channels c, c + 64.. of the head in every (256 / lanes)-th part
-  const int per = min(a.hd, 64), c = tid % per, p0 = tid / per, step = 256 / per, n_c = a.hd / per;
-  float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int per = a.hd / 4, c = tid % per, p0 = tid / per, step = 256 / per;
+  const f4* src = reinterpret_cast<const f4*>(buf.acc + (static_cast<int64_t>(where.x) * a.n_q + h) * a.hd) + c;
+  const int64_t row_f4 = static_cast<int64_t>(a.n_q) * per;
+  // (everything that a short join reads is requested before anything is waited for)
+  constexpr int kAhead = 4;
+  f4 first[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) first[k] = src[min(p0 + k * step, where.y - 1) * row_f4];
+  const KvPos vp = a.v_pos[h / (a.n_q / a.n_kv) * a.hd + min(tid, a.hd - 1)];
+  float m = kNone, l = 0.0f;
+  f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int base = 0; base < where.y; base += 256) {
     const int n = min(256, where.y - base);
+    const PartHead ph = heads[static_cast<int64_t>(base + min(tid, n - 1)) * a.n_q];
+    __syncthreads();                                          // (the weights of the 256 before have been read)
+    const float top = wave_max(ph.m);
+    if (lane == 0) red[wave] = top;
     __syncthreads();
-    if (tid < n) {
-      const PartHead ph = heads[static_cast<int64_t>(base + tid) * a.n_q];
-      weight[tid] = __builtin_amdgcn_exp2f(ph.m - m);
-      l = fmaf(ph.l, weight[tid], l);
-    }
-    __syncthreads();
-    const float* src = buf.acc + ((static_cast<int64_t>(where.x) + base) * a.n_q + h) * a.hd;
-#pragma unroll 4
-    for (int i = p0; i < n; i += step) {
+    const float m_new = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new), f = __builtin_amdgcn_exp2f(ph.m - m_new);
+    weight[tid] = f;
+    l = fmaf(l, alpha, tid < n ? ph.l * f : 0.0f);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j < n_c) acc[j] = fmaf(src[static_cast<int64_t>(i) * a.n_q * a.hd + j * per + c], weight[i], acc[j]);
+    for (int j = 0; j < 4; ++j) acc[j] *= alpha;
+    m = m_new;
+    __syncthreads();
+    int i = p0;
+    if (base == 0) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k, i += step)
+        if (i < n) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = fmaf(first[k][j], weight[i], acc[j]);
+        }
+    }
+#pragma unroll 8
+    for (; i < n; i += step) {
+      const f4 v = src[(base + i) * row_f4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = fmaf(v[j], weight[i], acc[j]);
     }
   }
   l = row16_add(l);
   auto row = [&](int at) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), at)); };
   l = (row(0) + row(16)) + (row(32) + row(48));
   if (lane == 0) red[4 + wave] = l;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) merge[j * 256 + tid] = acc[j];
+  *reinterpret_cast<f4*>(merge + tid * 4) = acc;              // [part % step][channel]
   __syncthreads();
   l = (red[4] + red[5]) + (red[6] + red[7]);
   if (tid < a.hd) {
-    const int kvh = h / (a.n_q / a.n_kv);
-    const KvPos vp = a.v_pos[kvh * a.hd + tid];
     float sum = 0.0f;
-    for (int i = 0; i < step; ++i) sum += merge[tid / per * 256 + i * per + tid % per];
+    for (int i = 0; i < step; ++i) sum += merge[i * a.hd + tid];
     store_out(a, f32, b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
     if (a.lse && tid == 0) a.lse[static_cast<int64_t>(b) * a.n_q + h] = finish_lse(m, l, heads[0].zterm);
   }
@@ -550,13 +593,12 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPl
 template <int BITS, int NB, int RT>
 static void launch_parts(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
   const int64_t cells = (static_cast<int64_t>(p.slots) * p.units + 7) / 8 * 8 * p.chunks;
-  const double per_part = 1.0 / p.parts * (1.0 + 0x1p-50);
-  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), dim3(static_cast<unsigned>(cells)), dim3(256), 0, st, a, p, per_part, f32);
+  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), dim3(static_cast<unsigned>(cells)), dim3(256), 0, st, a, p, f32);
 }
 
 template <int BITS>
 static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
-  const int tiles = (p.chunk_heads + kRowHeads - 1) / kRowHeads;
+  const int tiles = row_tiles(p.chunk_heads);
   if (a.hd > kPageBlock) {
     if (tiles <= 1) launch_parts<BITS, 2, 1>(a, p, f32, st);
     else launch_parts<BITS, 2, 2>(a, p, f32, st);
@@ -570,13 +612,13 @@ static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, hipS
 int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype, hipStream_t st) {
   if (a.B == 0) return RPTQ_OK;
   const bool f32 = out_dtype == RPTQ_DTYPE_F32;
-  const AttendPlan p = attend_plan(a.B, a.n_q, a.n_kv, a.hd);
+  const int64_t most_tokens = static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift;
+  const AttendPlan p = attend_plan(a.B, a.n_q, a.n_kv, a.hd, most_tokens);
   if (bits == 3) launch_bits<3>(a, p, f32, st);
   else if (bits == 4) launch_bits<4>(a, p, f32, st);
   else launch_bits<8>(a, p, f32, st);
   RPTQ_HIP(hipGetLastError());
-  // (a sequence that cannot be longer than the shortest part is never cut)
-  if ((static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift) <= kLeastTiles * kTile) return RPTQ_OK;
+  if (!p.join) return RPTQ_OK;
   hipLaunchKernelGGL(attend_join_kernel, dim3(static_cast<unsigned>(a.B) * a.n_q), dim3(256), 0, st, a, p, f32);
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;

@@ -74,7 +74,7 @@ def test_attention_refused(lib, name, value, status):
 
 
 def test_tokens_of_a_sequence_fit_32_bits(lib):
-    assert attend(lib, dict(ATTEND, page_size=4096, per_seq=(1 << 18) + 1, ld_pt=1 << 20)) == SHAPE
+    assert attend(lib, dict(ATTEND, page_size=4096, per_seq=(1 << 17) + 1, ld_pt=1 << 20)) == SHAPE
 
 
 def test_tensors_that_are_not_on_the_device_are_refused():
