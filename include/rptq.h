@@ -443,7 +443,8 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
  * of page page_table[b, t / page_size], and a number outside 0 .. n_pages - 1 stands for a page
  * that is not there (its tokens take no part).  lens[b] below 0 counts as 0, beyond
  * pages_per_seq * page_size as that.  A sequence without tokens gets zeros, and -infinity as lse.
- *   q       device bf16 [B, n_q_heads * head_dim], original channel order, rows ld_q apart
+ *   q       device bf16 [B, n_q_heads * head_dim], original channel order, rows ld_q apart;
+ *           B <= RPTQ_MAX_SEQUENCES
  *   head_dim  32, 64, 128 or 256; n_q_heads a multiple of n_kv_heads
  *   page_table device int32 [B, pages_per_seq], rows ld_page_table apart;  lens device int32 [B]
  *   out     device out [B, n_q_heads * head_dim], original channel order, rows ld_out apart,
@@ -461,6 +462,7 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
  */
 #define RPTQ_MIN_PAGE_SIZE 16
 #define RPTQ_MAX_PAGE_SIZE 4096
+#define RPTQ_MAX_SEQUENCES 32768
 size_t rptq_kv_page_bytes(int32_t d, int32_t page_size, int32_t bits);
 int32_t rptq_kv_quant_paged(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T, int32_t d,
                             const void* k_table, const void* v_table, int32_t bits, const int64_t* slots,

@@ -396,7 +396,7 @@ int32_t rptq_kv_dequant_paged(const void* k_pages, const void* v_pages, int64_t 
 
 static bool attend_heads_ok(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
   if (hd != 32 && hd != 64 && hd != 128 && hd != 256) return false;
-  if (B < 0 || B > (1 << 20) || n_kv < 1 || n_q < 1 || n_q % n_kv != 0) return false;
+  if (B < 0 || B > RPTQ_MAX_SEQUENCES || n_kv < 1 || n_q < 1 || n_q % n_kv != 0) return false;
   return paged_channels_ok(static_cast<int64_t>(n_kv) * hd) && static_cast<int64_t>(n_q) * hd <= RPTQ_MAX_CHANNELS;
 }
 

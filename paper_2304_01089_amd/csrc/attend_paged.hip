@@ -241,10 +241,17 @@ __device__ __forceinline__ float finish_lse(float m, float l, float zterm) {
   return l != 0.0f ? kLn2 * ((m - 30.0f - zterm) + __log2f(l)) : -__builtin_huge_valf();
 }
 
+// Waves per SIMD that the registers are shared out for: what is fastest, with few spills or none.
+__host__ __device__ constexpr int part_waves(int bits, int blocks, int tiles) {
+  if (blocks == 2) return bits == 8 && tiles > 1 ? 1 : 2;
+  if (bits == 8) return tiles == 1 ? 3 : 2;
+  return tiles == 1 ? 4 : (tiles < 4 ? 3 : 2);
+}
+
 // ---- the parts ---------------------------------------------------------------------------------------------
 // NB: blocks of a unit; RT: row tiles (of four heads)
 template <int BITS, int NB, int RT>
-__global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_kernel(AttendArgs a, AttendPlan plan, bool f32) {
+__global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_kernel(AttendArgs a, AttendPlan plan, bool f32) {
   constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
@@ -252,17 +259,20 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
   __shared__ __align__(16) unsigned char smem[kQBytes + kPBytes];
   __shared__ float merge[RT][4][kRowHeads][P];
   __shared__ float h_scale[RT * kRowHeads], h_z[RT * kRowHeads];
-  __shared__ float2 w_ml[4][RT * kRowHeads];
+  __shared__ float w_m[4][RT * kRowHeads], w_l[4][RT * kRowHeads];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g4 = lane >> 4;
 
-  // chunks of one unit's heads run on one XCD (workgroups are dealt to the eight in turn): they read the same pages
-  const int cells = plan.slots * plan.units;
-  const int chunk = static_cast<int>(blockIdx.x >> 3) % plan.chunks;
-  const int cell = static_cast<int>(blockIdx.x >> 3) / plan.chunks * 8 + static_cast<int>(blockIdx.x & 7);
-  if (cell >= cells) return;
-  const int unit = cell % plan.units, slot = cell / plan.units;
+  // (unit, slot); with chunks, (8 chunks x 8 slots, unit, slot / 8), so that the chunks of a unit's heads, which read the
+  // same pages, run next to each other on one XCD (workgroups are dealt to the eight in turn)
+  int unit = blockIdx.x, slot = blockIdx.y, chunk = 0;
+  if (plan.chunks > 1) {
+    unit = blockIdx.y;
+    slot = static_cast<int>(blockIdx.z) * 8 + static_cast<int>(blockIdx.x & 7);
+    chunk = static_cast<int>(blockIdx.x >> 3);
+    if (slot >= plan.slots) return;
+  }
 
   // (requested first: they depend on nothing)
   const KvPos* kt = a.k_pos + unit * P;
@@ -289,7 +299,11 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
   const int first_head = chunk * plan.chunk_heads;
   const int heads = min(plan.chunk_heads, plan.unit_heads - first_head);       // of this workgroup
   const int q_head = unit * plan.unit_heads + first_head;                      // the first of them
-  auto own = [&](int hh, int pos) { return NB == 2 || pos / a.hd == (first_head + hh) / share; };
+  // whether a position belongs to the key/value head that head hh of the workgroup reads
+  const int hd_shift = __builtin_ctz(a.hd);
+  auto own = [&](int hh, int pos) {
+    return NB == 2 || static_cast<unsigned>(first_head + hh - (pos >> hd_shift) * share) < static_cast<unsigned>(share);
+  };
   // (the queries, before the tiles: loads come back in order)
   uint16_t q_raw[RT][2 * NB];
 #pragma unroll
@@ -308,27 +322,31 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
     const int t = (token_of(k) + r * 16) & static_cast<int>(block_rows - 1);
     return (id * page_rows + unit * NB * block_rows + t) * kRow;
   };
-  auto load = [&](const uint8_t* p, uint32_t off, uint32_t (&x)[BITS]) {
-    const uint8_t* s = p + off;
-    if constexpr (BITS == 3) {
-#pragma unroll
-      for (int k = 0; k < 3; ++k) x[k] = reinterpret_cast<const uint32_t*>(s)[k];
-    } else {
-#pragma unroll
-      for (int k = 0; k < BITS / 4; ++k) {
-        const v4i v = reinterpret_cast<const v4i*>(s)[k];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * k + e] = static_cast<uint32_t>(v[e]);
-      }
-    }
-  };
+  // (buffer loads: a descriptor of the rows in scalar registers, a lane's offset in one register)
   uint32_t kr[4][NB][BITS], vr[4][NB][BITS];
+  const int block_bytes = static_cast<int>(block_rows) * kRow;
   auto load_tile = [&](int k, const uint8_t* pages, uint32_t off, uint32_t (&x)[4][NB][BITS]) {
+    typedef unsigned u3v __attribute__((ext_vector_type(3)));
+    typedef unsigned u4v __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t row = row_of(k, r);
+      const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>(pages) + row_of(k, r), 0, (NB - 1) * block_bytes + 16 * kRow, 0x00020000);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) load(pages + row + nb * block_rows * kRow, off, x[r][nb]);
+      for (int nb = 0; nb < NB; ++nb) {
+        if constexpr (BITS == 3) {
+          const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rows, off, nb * block_bytes, 0);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) x[r][nb][e] = v[e];
+        } else {
+#pragma unroll
+          for (int h = 0; h < BITS / 4; ++h) {
+            const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rows, off + 16 * h, nb * block_bytes, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[r][nb][4 * h + e] = v[e];
+          }
+        }
+      }
     }
   };
   if (my_tiles > 0) {
@@ -358,31 +376,20 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
 #pragma unroll
       for (int b = 0; b < 4; ++b) q_dig[(rt * 16 + wave * 4 + b) * P + i * 64 + lane] = static_cast<unsigned char>(d >> (8 * b));
     }
-    float z = 0.0f;
-    if (a.lse) {
-      double zs = 0.0;
-#pragma unroll
-      for (int i = 0; i < 2 * NB; ++i) zs += static_cast<double>(x[i]) * kp[i].z;
-      z = static_cast<float>(wave_sum(zs));
-    }
     const bool any_bad = __ballot(bad) != 0;
-    if (lane == 0) {
-      h_scale[hh] = any_bad ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);
-      h_z[hh] = z;
-    }
+    if (lane == 0) h_scale[hh] = any_bad ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);
   }
   __syncthreads();
-  v4i qa[RT][NB][2];
+  // One row tile's operands stay in registers, more are read again for every tile.
+  auto q_operand = [&](int rt, int nb, int s) {
+    return *reinterpret_cast<const v4i*>(q_dig + (rt * 16 + n16) * P + nb * kPageBlock + g4 * 32 + s * 16);
+  };
+  constexpr bool kHeld = RT * NB == 1;
+  v4i held[2];
   float scale[RT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-        qa[rt][nb][s] = *reinterpret_cast<const v4i*>(q_dig + (rt * 16 + n16) * P + nb * kPageBlock + g4 * 32 + s * 16);
-    scale[rt] = h_scale[rt * kRowHeads + g4];
-  }
+  for (int rt = 0; rt < RT; ++rt) scale[rt] = h_scale[rt * kRowHeads + g4];
+  if (kHeld) held[0] = q_operand(0, 0, 0), held[1] = q_operand(0, 0, 1);
 
   // ---- the tiles -----------------------------------------------------------------------------------------------
   unsigned char* p_buf = smem + kQBytes + wave * (RT * 1024);
@@ -398,55 +405,84 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
       for (int e = 0; e < 8; ++e) acc[rt][nb][e] = 0.0f;
   }
   for (int k = 0; k < my_tiles; ++k) {
-    v4i c[RT][4];
-    bool ok[4];
+    // (a score's upper bound: below every score where there is no token.  Its weight is then 0 by itself, but for a tile
+    // without any, whose sums are taken 0 times)
+    float most[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      ok[r] = token_of(k) + r * 16 + n16 < part.len && __builtin_amdgcn_readlane(ids, (k & 15) * 4 + r) >= 0;
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) c[rt][r] = v4i{0, 0, 0, 0};
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        uint32_t w[8];
-        expand<BITS>(kr[r][nb], w);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const v4i kb = {static_cast<int>(w[4 * s]), static_cast<int>(w[4 * s + 1]), static_cast<int>(w[4 * s + 2]), static_cast<int>(w[4 * s + 3])};
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) c[rt][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[rt][nb][s], kb, c[rt][r], 0, 0, 0);
-        }
-      }
+      const int left = __builtin_amdgcn_readlane(ids, (k & 15) * 4 + r) >= 0 ? part.len - token_of(k) - r * 16 : 0;
+      most[r] = n16 < left ? __builtin_huge_valf() : kNone;
     }
     const bool more = k + 1 < my_tiles;
-    if (more && ((k + 1) & 15) == 0) {
-      ids = ids_next;
-      ids_next = k + 17 < my_tiles ? pages_from(k + 17) : -1;
+    auto next_keys = [&] {                                 // (once the keys' registers are free)
+      if (more && ((k + 1) & 15) == 0) {
+        ids = ids_next;
+        ids_next = k + 17 < my_tiles ? pages_from(k + 17) : -1;
+      }
+      if (more) load_tile(k + 1, a.k_pages, k_off, kr);
+    };
+    auto operand = [](const uint32_t (&w)[8], int s) {
+      return v4i{static_cast<int>(w[4 * s]), static_cast<int>(w[4 * s + 1]), static_cast<int>(w[4 * s + 2]), static_cast<int>(w[4 * s + 3])};
+    };
+    // One or two row tiles: their sums side by side, a block of codes expanded at a time.  More: the tile's codes stay
+    // expanded and the row tiles go one after the other, which is fewer registers.
+    constexpr bool kWide = NB == 1 && RT > 2;
+    v4i c[kWide ? 1 : RT][4];
+    uint32_t kw[kWide ? 4 : 1][8];
+    if constexpr (kWide) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) expand<BITS>(kr[r][0], kw[r]);
+      next_keys();
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) c[rt][r] = v4i{0, 0, 0, 0};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          expand<BITS>(kr[r][nb], kw[0]);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              c[rt][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kHeld ? held[s] : q_operand(rt, nb, s), operand(kw[0], s), c[rt][r], 0, 0, 0);
+        }
+      }
+      next_keys();
     }
-    if (more) load_tile(k + 1, a.k_pages, k_off, kr);
 
     // weights of the tile, relative to its largest, as digits: lane (head g4, token n16 of every 16) -> operand lane (row n16, tokens of g4)
     float alpha[RT], beta[RT];
     v4i pa[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+      if constexpr (kWide) {
+        const v4i q0 = q_operand(rt, 0, 0), q1 = q_operand(rt, 0, 1);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          c[0][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q0, operand(kw[r], 0), v4i{0, 0, 0, 0}, 0, 0, 0);
+          c[0][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q1, operand(kw[r], 1), c[0][r], 0, 0, 0);
+        }
+      }
       float s[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[r] = ok[r] ? undigit(c[rt][r]) * scale[rt] : kNone;
+      for (int r = 0; r < 4; ++r) s[r] = fminf(undigit(c[kWide ? 0 : rt][r]) * scale[rt], most[r]);
       const float top = row16_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
       const float m_new = fmaxf(m_run[rt], top);
       alpha[rt] = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
-      beta[rt] = __builtin_amdgcn_exp2f(top - m_new);
+      beta[rt] = top > kNone ? __builtin_amdgcn_exp2f(top - m_new) : 0.0f;
       float sum = 0.0f;
       v4i d;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float e = ok[r] ? __builtin_amdgcn_exp2f((s[r] - top) + 30.0f) : 0.0f;
+        const float e = __builtin_amdgcn_exp2f((s[r] - top) + 30.0f);
         sum += e;
         d[r] = static_cast<int>(quad_transpose(digits(static_cast<int>(e)), sel));
       }
       l_run[rt] = fmaf(l_run[rt], alpha[rt], sum * beta[rt]);
       m_run[rt] = m_new;
       *reinterpret_cast<v4i*>(p_buf + rt * 1024 + (g4 * 4 + (n16 & 3)) * 64 + (n16 >> 2) * 16) = d;
+      if (kWide) __builtin_amdgcn_sched_barrier(0);       // (one row tile after the other: the scheduler would keep all their sums)
     }
     wave_lds_fence();
 #pragma unroll
@@ -471,52 +507,70 @@ __global__ void __launch_bounds__(256, NB == 2 || RT == 4 ? 1 : 2) attend_part_k
           const v4i o = __builtin_amdgcn_mfma_i32_16x16x64_i8(pa[rt], vb, v4i{0, 0, 0, 0}, 0, 0, 0);
           acc[rt][nb][e] = fmaf(acc[rt][nb][e], alpha[rt], undigit(o) * beta[rt]);
         }
+        // (about eight products under way at a time: the scheduler would take registers for all of them)
+        if (RT > 1 && (e + 1) % (8 / RT) == 0)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) asm volatile("" : "+v"(acc[rt][nb][e]), "+v"(pa[rt]));
       }
     }
     if (more) load_tile(k + 1, a.v_pages, v_off, vr);
   }
 
   // ---- the waves' sums together ------------------------------------------------------------------------------------
+  // (what the zero points of the keys add to a head's scores: lse alone sees it)
+  if (a.lse && part.index == 0) {
+#pragma unroll 1
+    for (int hh = wave; hh < heads; hh += 4) {
+      double z = 0.0;
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) {
+        const KvPos k = kt[i * 64 + lane];
+        const uint32_t h = a.q[part.b * a.ld_q + (q_head + hh) * a.hd + (k.src & (a.hd - 1))];
+        const float x = __uint_as_float(h << 16) * k.s * (a.scale * kLog2e);
+        z += own(hh, i * 64 + lane) ? static_cast<double>(x) * k.z : 0.0;
+      }
+      z = wave_sum(z);
+      if (lane == 0) h_z[hh] = static_cast<float>(z);
+    }
+  }
+  // (first the largest scores, so that every wave scales its own sums once)
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+    if (n16 == 0) w_m[wave][rt * kRowHeads + g4] = m_run[rt];
+  __syncthreads();
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const float l = row16_add(l_run[rt]);
-    if (n16 == 0) w_ml[wave][rt * kRowHeads + g4] = make_float2(m_run[rt], l);
+    const int hh = rt * kRowHeads + g4;
+    const float m = fmaxf(fmaxf(w_m[0][hh], w_m[1][hh]), fmaxf(w_m[2][hh], w_m[3][hh]));
+    const float f = __builtin_amdgcn_exp2f(m_run[rt] - m), l = row16_add(l_run[rt]) * f;
+    if (n16 == 0) w_l[wave][hh] = l;
+    const float fs = f * (1.0f / (1 << kShift));
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) merge[rt][wave][g4][nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e] * fs;
   }
   const PartBuffers buf = part_buffers(a, plan);
   const bool whole = part.count == 1;
   if (part.index == 0 && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) merge[rt][wave][g4][nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e];
   __syncthreads();
+  const int pos = tid % P, at = NB == 2 ? pos : pos & (a.hd - 1);
+#pragma unroll 1
+  for (int hh = tid / P; hh < heads; hh += 256 / P) {
+    if (!own(hh, pos)) continue;
+    float l = 0.0f, sum = 0.0f;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) {
-      const int pos = tid % P, g = (i * 256 + tid) / P, hh = rt * kRowHeads + g;
-      if (hh >= heads || !own(hh, pos)) continue;
-      float m = kNone, l = 0.0f, sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, w_ml[w][hh].x);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(w_ml[w][hh].x - m);
-        l = fmaf(w_ml[w][hh].y, f, l);
-        sum = fmaf(merge[rt][w][g][pos], f, sum);
-      }
-      sum *= 1.0f / (1 << kShift);
-      const int h = q_head + hh, at = NB == 2 ? pos : pos & (a.hd - 1);
-      if (whole) {
-        store_out(a, f32, part.b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
-        if (a.lse && at == 0) a.lse[static_cast<int64_t>(part.b) * a.n_q + h] = finish_lse(m, l, h_z[hh]);
-      } else {
-        const int64_t row = static_cast<int64_t>(slot) * a.n_q + h;
-        buf.acc[row * a.hd + at] = sum;
-        if (at == 0) buf.heads[row] = PartHead{m, l, h_z[hh], 0.0f};
-      }
+    for (int w = 0; w < 4; ++w) {
+      l += w_l[w][hh];
+      sum += merge[hh / kRowHeads][w][hh % kRowHeads][pos];
+    }
+    const int64_t h = q_head + hh, row = static_cast<int64_t>(slot) * a.n_q + h;
+    if (whole) store_out(a, f32, part.b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
+    else buf.acc[row * a.hd + at] = sum;
+    if (at == 0 && (a.lse || !whole)) {
+      const float m = fmaxf(fmaxf(w_m[0][hh], w_m[1][hh]), fmaxf(w_m[2][hh], w_m[3][hh]));
+      if (!whole) buf.heads[row] = PartHead{m, l, h_z[hh], 0.0f};
+      else a.lse[static_cast<int64_t>(part.b) * a.n_q + h] = finish_lse(m, l, h_z[hh]);
     }
   }
 }
@@ -592,8 +646,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPl
 
 template <int BITS, int NB, int RT>
 static void launch_parts(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
-  const int64_t cells = (static_cast<int64_t>(p.slots) * p.units + 7) / 8 * 8 * p.chunks;
-  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), dim3(static_cast<unsigned>(cells)), dim3(256), 0, st, a, p, f32);
+  const dim3 grid = p.chunks == 1 ? dim3(p.units, p.slots) : dim3(8 * p.chunks, p.units, (p.slots + 7) / 8);
+  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), grid, dim3(256), 0, st, a, p, f32);
 }
 
 template <int BITS>
@@ -605,6 +659,7 @@ static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, hipS
   } else {
     if (tiles <= 1) launch_parts<BITS, 1, 1>(a, p, f32, st);
     else if (tiles == 2) launch_parts<BITS, 1, 2>(a, p, f32, st);
+    else if (tiles == 3) launch_parts<BITS, 1, 3>(a, p, f32, st);
     else launch_parts<BITS, 1, 4>(a, p, f32, st);
   }
 }
