@@ -29,8 +29,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
 constexpr int kTile = 64;                      // tokens of a wave's tile
-constexpr int kMidTiles = 16;                  // of a part: four per wave
 constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
+constexpr int kLongTiles = 64;                 // of a part, where there are few
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
@@ -59,7 +59,8 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   p.chunk_heads = (p.unit_heads + p.chunks - 1) / p.chunks;
   const int each = p.units * p.chunks;
   auto parts = [&](int workgroups) { return std::max(1, (workgroups + each - 1) / each); };
-  p.per_few = 1.0 / parts(kFewWorkgroups) * (1.0 + 0x1p-50);
+  // (rounding up adds half a part per sequence)
+  p.per_few = 1.0 / parts(kFewWorkgroups - static_cast<int>(std::min<int64_t>(static_cast<int64_t>(B) * each / 2, kFewWorkgroups - 1))) * (1.0 + 0x1p-50);
   p.per_many = 1.0 / parts(kManyWorkgroups) * (1.0 + 0x1p-50);
   // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch: 4 us, as long as a wave
   // takes for three tiles of one block and one row tile.
@@ -204,7 +205,7 @@ __device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan&
   }
   // tiles of a part: all tiles over the number of parts, rounded up
   auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>((total - 1.0) * per)) + 1; };
-  const int most = max(p.least, max(min(each_of(p.per_few), kMidTiles), each_of(p.per_many)));
+  const int few = each_of(p.per_few), most = max(p.least, few <= kLongTiles ? few : each_of(p.per_many));
   int before = 0;
   for (int base = 0; base < a.B; base += 64) {
     const int i = base + lane;
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   constexpr int P = NB * kPageBlock;                       // positions of the unit
   constexpr int kQBytes = RT * 16 * P, kPBytes = 4 * RT * 1024;
   __shared__ __align__(16) unsigned char smem[kQBytes + kPBytes];
-  __shared__ float merge[RT][4][kRowHeads][P];
+  __shared__ float merge[RT][4][kRowHeads][P + 16];       // [..][block][code 4e..][lane of 16]; (the 16 more: other banks)
   __shared__ float h_scale[RT * kRowHeads], h_z[RT * kRowHeads];
   __shared__ float w_m[4][RT * kRowHeads], w_l[4][RT * kRowHeads];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -548,30 +549,38 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) merge[rt][wave][g4][nb * kPageBlock + (n16 >> 2) * 32 + e * 4 + (n16 & 3)] = acc[rt][nb][e] * fs;
+      for (int e = 0; e < 8; ++e) merge[rt][wave][g4][nb * kPageBlock + e * 16 + n16] = acc[rt][nb][e] * fs;
   }
   const PartBuffers buf = part_buffers(a, plan);
   const bool whole = part.count == 1;
   if (part.index == 0 && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
   __syncthreads();
   const int pos = tid % P, at = NB == 2 ? pos : pos & (a.hd - 1);
-#pragma unroll 1
-  for (int hh = tid / P; hh < heads; hh += 256 / P) {
-    if (!own(hh, pos)) continue;
-    float l = 0.0f, sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      l += w_l[w][hh];
-      sum += merge[hh / kRowHeads][w][hh % kRowHeads][pos];
+  const int from = (pos & ~(kPageBlock - 1)) + (pos >> 2 & 7) * 16 + (pos >> 5 & 3) * 4 + (pos & 3);
+  auto sum_of = [&](int hh) {
+    const int rt = hh / kRowHeads, g = hh % kRowHeads;
+    return (merge[rt][0][g][from] + merge[rt][1][g][from]) + (merge[rt][2][g][from] + merge[rt][3][g][from]);
+  };
+  auto weight_of = [&](int hh) { return (w_l[0][hh] + w_l[1][hh]) + (w_l[2][hh] + w_l[3][hh]); };
+  auto top_of = [&](int hh) { return fmaxf(fmaxf(w_m[0][hh], w_m[1][hh]), fmaxf(w_m[2][hh], w_m[3][hh])); };
+  if (whole) {
+#pragma unroll 2
+    for (int hh = tid / P; hh < heads; hh += 256 / P) {
+      const float y = finish(sum_of(hh), weight_of(hh), vp);
+      if (!own(hh, pos)) continue;
+      store_out(a, f32, part.b * a.ld_out + static_cast<int64_t>(q_head + hh) * a.hd + (vp.src & (a.hd - 1)), y);
     }
-    const int64_t h = q_head + hh, row = static_cast<int64_t>(slot) * a.n_q + h;
-    if (whole) store_out(a, f32, part.b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
-    else buf.acc[row * a.hd + at] = sum;
-    if (at == 0 && (a.lse || !whole)) {
-      const float m = fmaxf(fmaxf(w_m[0][hh], w_m[1][hh]), fmaxf(w_m[2][hh], w_m[3][hh]));
-      if (!whole) buf.heads[row] = PartHead{m, l, h_z[hh], 0.0f};
-      else a.lse[static_cast<int64_t>(part.b) * a.n_q + h] = finish_lse(m, l, h_z[hh]);
+    if (a.lse && tid < heads)
+      a.lse[static_cast<int64_t>(part.b) * a.n_q + q_head + tid] = finish_lse(top_of(tid), weight_of(tid), h_z[tid]);
+  } else {
+    const int64_t row = static_cast<int64_t>(slot) * a.n_q + q_head;
+    float* dst = buf.acc + row * a.hd + at;
+#pragma unroll 4
+    for (int hh = tid / P; hh < heads; hh += 256 / P) {
+      const float sum = sum_of(hh);
+      if (own(hh, pos)) dst[hh * a.hd] = sum;
     }
+    if (tid < heads) buf.heads[row + tid] = PartHead{top_of(tid), weight_of(tid), h_z[tid], 0.0f};
   }
 }
 
