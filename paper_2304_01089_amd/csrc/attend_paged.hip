@@ -30,7 +30,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
 constexpr int kTile = 64;                      // tokens of a wave's tile
 constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
-constexpr int kLongTiles = 64;                 // of a part, where there are few
+constexpr int kLongTiles = 64;                 // of a part at most where there are few,
+constexpr int kShortTiles = 16;                // and at least where there are many
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
@@ -186,30 +187,32 @@ struct Part {
   int b, len, index, count, first_tile, end_tile;
 };
 
-// The part that slot number `slot` holds; false: none.  Every sequence has at least one.
-__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int slot, int lane, Part* out) {
+// The part that slot number `slot` holds; false: none.  first_len: lane i's is that of sequence i (or the last's).  Every sequence has at least one.
+__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int first_len, int slot, int lane, Part* out) {
   const int cap = a.pages_per_seq << a.g.page_shift;
-  auto len_of = [&](int i) { return i < a.B ? min(max(a.lens[i], 0), cap) : 0; };
+  auto clamped = [&](int i, int len) { return i < a.B ? min(max(len, 0), cap) : 0; };
+  auto len_of = [&](int i) { return clamped(i, a.lens[min(i, a.B - 1)]); };
   auto tiles_of = [](int n) { return (n + kTile - 1) / kTile; };
   auto parts_of = [](int tiles, int n) {       // rounded up; (24 bits, which is all there is: a division by float)
     return ((static_cast<uint32_t>(tiles) + n - 1) & 0xffffffu) / (static_cast<uint32_t>(n) & 0xffffffu);
   };
-  const int len0 = len_of(lane);
+  const int len0 = clamped(lane, first_len);
   double total;
   if (a.B <= 64) {
     total = __builtin_amdgcn_readlane(wave_prefix(tiles_of(len0)), 63);
   } else {
     total = tiles_of(len0);
+#pragma unroll 4
     for (int i = 64; i < a.B; i += 64) total += tiles_of(len_of(i + lane));
     total = wave_sum(total);
   }
   // tiles of a part: all tiles over the number of parts, rounded up
   auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>((total - 1.0) * per)) + 1; };
-  const int few = each_of(p.per_few), most = max(p.least, few <= kLongTiles ? few : each_of(p.per_many));
-  int before = 0;
+  const int few = each_of(p.per_few), most = max(p.least, few <= kLongTiles ? few : max(kShortTiles, each_of(p.per_many)));
+  int before = 0, next_len = len0;
   for (int base = 0; base < a.B; base += 64) {
-    const int i = base + lane;
-    const int len = base == 0 ? len0 : len_of(i);
+    const int i = base + lane, len = next_len;
+    if (base + 64 < a.B) next_len = len_of(i + 64);
     const int n = i < a.B ? max<int>(1, parts_of(tiles_of(len), most)) : 0;
     const int upto = wave_prefix(n);
     const uint64_t hit = __ballot(slot >= before + upto - n && slot < before + upto);
@@ -275,26 +278,42 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     if (slot >= plan.slots) return;
   }
 
-  // (requested first: they depend on nothing)
+  // (requested first: they depend on nothing, and the lengths are waited for first)
+  const int first_len = a.lens[min(lane, a.B - 1)];
+  // (one argument of every 64 bytes of them, so that all are fetched at once and not one after the other)
+  asm volatile("" ::"s"(a.q), "s"(a.v_pos), "s"(a.page_table), "s"(a.workspace), "s"(plan.per_few));
+  __builtin_amdgcn_sched_barrier(0);
   const KvPos* kt = a.k_pos + unit * P;
   KvPos kp[2 * NB];
 #pragma unroll
   for (int i = 0; i < 2 * NB; ++i) kp[i] = kt[i * 64 + lane];
   const KvPos vp = a.v_pos[unit * P + tid % P];
   Part part;
-  if (!find_part(a, plan, slot, lane, &part)) return;
+  if (!find_part(a, plan, first_len, slot, lane, &part)) return;
 
-  // ---- pages of this wave's tiles: lane 4k + i holds the page of its k-th tile's i-th 16 tokens, or -1 ---------
+  // ---- rows of this wave's tiles: lane 4k + i holds where its k-th tile's i-th 16 tokens lie, in bytes to the unit's first
+  // block, and whether their page is there (else 0, the first page); sixteen tiles at a time, the next requested ahead ------
   const int32_t* pt = a.page_table + part.b * a.ld_pt;
   const int my_tiles = max(0, (part.end_tile - part.first_tile - wave + 3) >> 2);
   auto token_of = [&](int k) { return (part.first_tile + wave + 4 * k) * kTile; };
   const int last_page = max(part.len - 1, 0) >> a.g.page_shift;
-  auto pages_from = [&](int k) {
+  const int block_rows = 1 << a.g.page_shift;
+  auto page_of = [&](int k) {                              // -1: none
     const int t = token_of(k + (lane >> 2)) + (lane & 3) * 16;
     const int id = pt[min(t >> a.g.page_shift, last_page)];
     return t < part.len && id >= 0 && id < a.g.n_pages ? id : -1;
   };
-  int ids = my_tiles > 0 ? pages_from(0) : -1, ids_next = my_tiles > 16 ? pages_from(16) : -1;
+  struct Rows {
+    uint32_t lo, hi;
+    uint64_t there;
+  };
+  auto rows_of = [&](int k, int id) {
+    const int t = (token_of(k + (lane >> 2)) + (lane & 3) * 16) & (block_rows - 1);
+    const uint64_t row = (static_cast<uint64_t>(max(id, 0)) * (a.g.d / kPageBlock) + unit * NB) * block_rows + t;
+    return Rows{static_cast<uint32_t>(row * kRow), static_cast<uint32_t>(row * kRow >> 32), __ballot(id >= 0)};
+  };
+  const int first_page = my_tiles > 0 ? page_of(0) : -1;
+  int next_page = my_tiles > 16 ? page_of(16) : -1;
 
   const int share = a.n_q / a.n_kv;
   const int first_head = chunk * plan.chunk_heads;
@@ -316,23 +335,19 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   // K and V of a tile: lane (token n16, group g4) of every 16 tokens' keys; lane (group n16 / 4, token 4 g4 + n16 % 4) of the values
   const uint32_t k_off = n16 * kRow + g4 * (4 * BITS);
   const uint32_t v_off = (4 * g4 + (n16 & 3)) * kRow + (n16 >> 2) * (4 * BITS);
-  const int64_t block_rows = static_cast<int64_t>(1) << a.g.page_shift;
-  const int64_t page_rows = static_cast<int64_t>(a.g.d / kPageBlock) << a.g.page_shift;
-  auto row_of = [&](int k, int r) {                        // bytes to 16 tokens' rows in the unit's first block (uniform)
-    const int id = max(__builtin_amdgcn_readlane(ids, (k & 15) * 4 + r), 0);
-    const int t = (token_of(k) + r * 16) & static_cast<int>(block_rows - 1);
-    return (id * page_rows + unit * NB * block_rows + t) * kRow;
-  };
+  Rows rows_at = rows_of(0, first_page);
   // (buffer loads: a descriptor of the rows in scalar registers, a lane's offset in one register)
   uint32_t kr[4][NB][BITS], vr[4][NB][BITS];
-  const int block_bytes = static_cast<int>(block_rows) * kRow;
+  const int block_bytes = block_rows * kRow;
   auto load_tile = [&](int k, const uint8_t* pages, uint32_t off, uint32_t (&x)[4][NB][BITS]) {
     typedef unsigned u3v __attribute__((ext_vector_type(3)));
     typedef unsigned u4v __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
+      const int at = (k & 15) * 4 + r;
+      const uint64_t row = static_cast<uint64_t>(__builtin_amdgcn_readlane(rows_at.hi, at)) << 32 | __builtin_amdgcn_readlane(rows_at.lo, at);
       const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(pages) + row_of(k, r), 0, (NB - 1) * block_bytes + 16 * kRow, 0x00020000);
+          const_cast<uint8_t*>(pages) + row, 0, (NB - 1) * block_bytes + 16 * kRow, 0x00020000);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if constexpr (BITS == 3) {
@@ -411,14 +426,14 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     float most[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int left = __builtin_amdgcn_readlane(ids, (k & 15) * 4 + r) >= 0 ? part.len - token_of(k) - r * 16 : 0;
+      const int left = rows_at.there >> ((k & 15) * 4 + r) & 1 ? part.len - token_of(k) - r * 16 : 0;
       most[r] = n16 < left ? __builtin_huge_valf() : kNone;
     }
     const bool more = k + 1 < my_tiles;
     auto next_keys = [&] {                                 // (once the keys' registers are free)
       if (more && ((k + 1) & 15) == 0) {
-        ids = ids_next;
-        ids_next = k + 17 < my_tiles ? pages_from(k + 17) : -1;
+        rows_at = rows_of(k + 1, next_page);
+        next_page = k + 17 < my_tiles ? page_of(k + 17) : -1;
       }
       if (more) load_tile(k + 1, a.k_pages, k_off, kr);
     };
