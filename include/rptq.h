@@ -449,7 +449,7 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
  *   page_table device int32 [B, pages_per_seq], rows ld_page_table apart;  lens device int32 [B]
  *   out     device out [B, n_q_heads * head_dim], original channel order, rows ld_out apart,
  *           out_dtype RPTQ_DTYPE_BF16 or RPTQ_DTYPE_F32
- *   lse     device out fp32 [B, n_q_heads], or NULL
+ *   lse     device out fp32 [B, n_q_heads], or NULL  (nothing that is written may overlap anything that is read)
  *   workspace device, rptq_attend_paged_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim) bytes; nothing
  *           in it has to be cleared or kept between calls; calls that overlap in time need one each
  * Sums and softmax statistics are fp32 or exact integers; a sequence's last bits may depend on

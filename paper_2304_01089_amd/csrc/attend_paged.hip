@@ -32,6 +32,7 @@ constexpr int kTile = 64;                      // tokens of a wave's tile
 constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
 constexpr int kLongTiles = 64;                 // of a part at most where there are few,
 constexpr int kShortTiles = 16;                // and at least where there are many
+constexpr int kMostTiles = 1 << 23;            // of a sequence
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
@@ -70,7 +71,7 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   p.join = p.least == 1;
   // (a sequence is cut in no more parts than its pages hold)
   const int64_t per_seq = (most_tokens + p.least * kTile - 1) / (p.least * kTile);
-  p.slots = static_cast<int32_t>(std::min<int64_t>(parts(kManyWorkgroups) + static_cast<int64_t>(B), B * per_seq));
+  p.slots = static_cast<int32_t>(std::min<int64_t>(parts(kManyWorkgroups) + static_cast<int64_t>(B), B * per_seq));   // (not cut: B)
   return p;
 }
 
@@ -187,7 +188,8 @@ struct Part {
   int b, len, index, count, first_tile, end_tile;
 };
 
-// The part that slot number `slot` holds; false: none.  first_len: lane i's is that of sequence i (or the last's).  Every sequence has at least one.
+// The part that slot number `slot` holds; false: none.  Every sequence has at least one.  first_len: lane i's is that of
+// sequence i (or the last's); where sequences are not cut, that of sequence number `slot`, whose only part it is.
 __device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int first_len, int slot, int lane, Part* out) {
   const int cap = a.pages_per_seq << a.g.page_shift;
   auto clamped = [&](int i, int len) { return i < a.B ? min(max(len, 0), cap) : 0; };
@@ -196,6 +198,14 @@ __device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan&
   auto parts_of = [](int tiles, int n) {       // rounded up; (24 bits, which is all there is: a division by float)
     return ((static_cast<uint32_t>(tiles) + n - 1) & 0xffffffu) / (static_cast<uint32_t>(n) & 0xffffffu);
   };
+  if (!p.join) {
+    out->b = slot;
+    out->len = __builtin_amdgcn_readfirstlane(clamped(slot, first_len));
+    out->index = out->first_tile = 0;
+    out->count = 1;
+    out->end_tile = tiles_of(out->len);
+    return true;
+  }
   const int len0 = clamped(lane, first_len);
   double total;
   if (a.B <= 64) {
@@ -206,8 +216,8 @@ __device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan&
     for (int i = 64; i < a.B; i += 64) total += tiles_of(len_of(i + lane));
     total = wave_sum(total);
   }
-  // tiles of a part: all tiles over the number of parts, rounded up
-  auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>((total - 1.0) * per)) + 1; };
+  // tiles of a part: all tiles over the number of parts, rounded up; no more than a sequence of 2^29 tokens has
+  auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>(fmin((total - 1.0) * per, kMostTiles - 1.0))) + 1; };
   const int few = each_of(p.per_few), most = max(p.least, few <= kLongTiles ? few : max(kShortTiles, each_of(p.per_many)));
   int before = 0, next_len = len0;
   for (int base = 0; base < a.B; base += 64) {
@@ -279,7 +289,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   }
 
   // (requested first: they depend on nothing, and the lengths are waited for first)
-  const int first_len = a.lens[min(lane, a.B - 1)];
+  const int first_len = a.lens[min(plan.join ? lane : slot, a.B - 1)];
   // (one argument of every 64 bytes of them, so that all are fetched at once and not one after the other)
   asm volatile("" ::"s"(a.q), "s"(a.v_pos), "s"(a.page_table), "s"(a.workspace), "s"(plan.per_few));
   __builtin_amdgcn_sched_barrier(0);
@@ -606,7 +616,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPl
   __shared__ __align__(16) float merge[256 * 4];
   typedef float f4 __attribute__((ext_vector_type(4)));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.x % a.n_q, b = blockIdx.x / a.n_q;
+  const int h = blockIdx.x, b = blockIdx.y;
   const PartBuffers buf = part_buffers(a, plan);
   const int2 where = buf.where[b];
   if (where.y <= 1) return;
@@ -698,7 +708,7 @@ int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype
   else launch_bits<8>(a, p, f32, st);
   RPTQ_HIP(hipGetLastError());
   if (!p.join) return RPTQ_OK;
-  hipLaunchKernelGGL(attend_join_kernel, dim3(static_cast<unsigned>(a.B) * a.n_q), dim3(256), 0, st, a, p, f32);
+  hipLaunchKernelGGL(attend_join_kernel, dim3(a.n_q, a.B), dim3(256), 0, st, a, p, f32);
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;
 }

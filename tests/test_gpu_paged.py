@@ -274,6 +274,51 @@ def test_many_sequences(rp):
     b.check(q, 2, 64 ** -0.5, out, lse)
 
 
+def test_more_tiles_than_32_bits_count(rp):
+    """Sequences of 2^27 tokens whose pages are there at the start and the end only: 2^31 tiles of 64 in the batch."""
+    B, page, n_q = 1040, 4096, 2
+    b = Batch(rp, [4 * page], 1, 128, 4, page, extra_pages=0)
+    ids = b.table[0]
+    q1 = b.queries(n_q)
+    lens = (1 << 27) - 1000 * np.arange(B)
+    width = (1 << 27) // page
+    assert ((lens + 63) // 64).sum() > 1 << 31
+    table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    last = (lens - 1) // page
+    first_id, last_id = ids[np.arange(B) % 3], ids[3]
+    table[:, 0] = dev(first_id, np.int32)
+    table[torch.arange(B, device="cuda"), dev(last, np.int64)] = int(last_id)
+    b.page_table, b.dev_lens = table, dev(lens, np.int32)
+    q = np.tile(q1, (B, 1))
+    out, lse = run(rp, b, q, n_q)
+    at = {int(i): n for n, i in enumerate(ids)}                # where a page's codes are in the sequence of four pages
+    for row in (0, 1, 2, 500, 1038, 1039):
+        tail = int(lens[row]) - int(last[row]) * page
+        tokens = np.r_[at[int(first_id[row])] * page + np.arange(page), at[int(last_id)] * page + np.arange(tail)]
+        k, v = b.k[0][tokens], b.v[0][tokens]
+        want, wl = kvo.attend(q[row], k, v, b.hk, 0, b.hv, 0, n_q, 128 ** -0.5)
+        tol, tl = paged.attend_bounds(q[row], k, b.hk, b.hv, n_q, 128 ** -0.5, 4, want, wl)
+        assert (np.abs(out[row].double().cpu().numpy() - want) <= tol).all(), row
+        assert (np.abs(lse[row].double().cpu().numpy() - wl) <= tl).all(), row
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+def test_the_largest_batch(rp):
+    """As many sequences and query heads as there may be at once."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough free memory")
+    B, n_q, hd = 32768, 1024, 32
+    b = Batch(rp, [300, 2, 0, 65], 4, hd, 4, 16)
+    few = b.queries(n_q)
+    kind = torch.arange(B, device="cuda") % 4
+    q = dev_bf16(few)[kind]
+    out = torch.full((B, n_q * hd), float("nan"), dtype=torch.bfloat16, device="cuda")
+    _, lse = rp.attend_paged(b.cache, q, b.page_table[kind], b.dev_lens[kind], out=out, want_lse=True)
+    b.check(few, n_q, hd ** -0.5, out[:4], lse[:4])
+    assert torch.equal(out.view(-1, 4, n_q * hd), out[:4].expand(B // 4, -1, -1))
+    assert torch.equal(lse.view(-1, 4, n_q), lse[:4].expand(B // 4, -1, -1))
+
+
 @pytest.mark.parametrize("page,holes", [(16, (0,)), (16, (1, 2, 3, 5)), (64, (0, 2)), (32, tuple(range(64))), (16, tuple(range(0, 80, 3)))])
 def test_pages_that_are_not_there(rp, page, holes):
     """Tokens of a page that is not there take no part, wherever it lies, and a sequence may lose all of its pages."""
