@@ -32,6 +32,7 @@ constexpr int kTile = 64;                      // tokens of a wave's tile
 constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
 constexpr int kLongTiles = 64;                 // of a part at most where there are few,
 constexpr int kShortTiles = 16;                // and at least where there are many
+constexpr int kLeastTiles = 2;                 // of a part of a sequence that is cut (1 | 2 | 4, us: 7 x 1531 of 16 on 2 x 256 at 4 bits 12.3 | 10.9 | 11.5, at 8 12.5 | 12.3 | 14.0)
 constexpr int kMostTiles = 1 << 23;            // of a sequence
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
@@ -67,8 +68,8 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch: 4 us, as long as a wave
   // takes for three tiles of one block and one row tile.
   const int whole = std::max(4, 16 / (unit / kPageBlock * row_tiles(p.chunk_heads)));
-  p.least = most_tokens <= whole * kTile ? whole : 1;
-  p.join = p.least == 1;
+  p.join = most_tokens > whole * kTile;
+  p.least = p.join ? kLeastTiles : whole;
   // (a sequence is cut in no more parts than its pages hold)
   const int64_t per_seq = (most_tokens + p.least * kTile - 1) / (p.least * kTile);
   p.slots = static_cast<int32_t>(std::min<int64_t>(parts(kManyWorkgroups) + static_cast<int64_t>(B), B * per_seq));   // (not cut: B)
@@ -293,6 +294,10 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   // (one argument of every 64 bytes of them, so that all are fetched at once and not one after the other)
   asm volatile("" ::"s"(a.q), "s"(a.v_pos), "s"(a.page_table), "s"(a.workspace), "s"(plan.per_few));
   __builtin_amdgcn_sched_barrier(0);
+  // (a sequence that is not cut: its first pages' numbers as well, before its length is there to say which of them count)
+  int early_page = 0;
+  if (!plan.join)
+    early_page = a.page_table[slot * a.ld_pt + min(((wave + 4 * (lane >> 2)) * kTile + (lane & 3) * 16) >> a.g.page_shift, a.pages_per_seq - 1)];
   const KvPos* kt = a.k_pos + unit * P;
   KvPos kp[2 * NB];
 #pragma unroll
@@ -308,21 +313,19 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   auto token_of = [&](int k) { return (part.first_tile + wave + 4 * k) * kTile; };
   const int last_page = max(part.len - 1, 0) >> a.g.page_shift;
   const int block_rows = 1 << a.g.page_shift;
-  auto page_of = [&](int k) {                              // -1: none
-    const int t = token_of(k + (lane >> 2)) + (lane & 3) * 16;
-    const int id = pt[min(t >> a.g.page_shift, last_page)];
-    return t < part.len && id >= 0 && id < a.g.n_pages ? id : -1;
-  };
+  auto tokens_of = [&](int k) { return token_of(k + (lane >> 2)) + (lane & 3) * 16; };
+  auto checked = [&](int k, int id) { return tokens_of(k) < part.len && id >= 0 && id < a.g.n_pages ? id : -1; };        // -1: none
+  auto page_of = [&](int k) { return checked(k, pt[min(tokens_of(k) >> a.g.page_shift, last_page)]); };
   struct Rows {
     uint32_t lo, hi;
     uint64_t there;
   };
   auto rows_of = [&](int k, int id) {
-    const int t = (token_of(k + (lane >> 2)) + (lane & 3) * 16) & (block_rows - 1);
+    const int t = tokens_of(k) & (block_rows - 1);
     const uint64_t row = (static_cast<uint64_t>(max(id, 0)) * (a.g.d / kPageBlock) + unit * NB) * block_rows + t;
     return Rows{static_cast<uint32_t>(row * kRow), static_cast<uint32_t>(row * kRow >> 32), __ballot(id >= 0)};
   };
-  const int first_page = my_tiles > 0 ? page_of(0) : -1;
+  const int first_page = !plan.join ? checked(0, early_page) : (my_tiles > 0 ? page_of(0) : -1);
   int next_page = my_tiles > 16 ? page_of(16) : -1;
 
   const int share = a.n_q / a.n_kv;
