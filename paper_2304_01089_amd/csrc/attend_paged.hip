@@ -33,7 +33,9 @@ constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight 
 constexpr int kLongTiles = 64;                 // of a part at most where there are few,
 constexpr int kShortTiles = 16;                // and at least where there are many
 constexpr int kLeastTiles = 2;                 // of a part of a sequence that is cut (1 | 2 | 4, us: 7 x 1531 of 16 on 2 x 256 at 4 bits 12.3 | 10.9 | 11.5, at 8 12.5 | 12.3 | 14.0)
+constexpr int kWholeTiles = 48;                // of a sequence that is never cut at most (one such among short ones keeps the others waiting)
 constexpr int kMostTiles = 1 << 23;            // of a sequence
+constexpr int kJoinWorkgroups = 2048;          // that join parts, about: more take several heads each (512 x 1500 of 64 on 8 x 128: 136 | 127 us)
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
@@ -65,9 +67,13 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   // (rounding up adds half a part per sequence)
   p.per_few = 1.0 / parts(kFewWorkgroups - static_cast<int>(std::min<int64_t>(static_cast<int64_t>(B) * each / 2, kFewWorkgroups - 1))) * (1.0 + 0x1p-50);
   p.per_many = 1.0 / parts(kManyWorkgroups) * (1.0 + 0x1p-50);
-  // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch: 4 us, as long as a wave
-  // takes for three tiles of one block and one row tile.
-  const int whole = std::max(4, 16 / (unit / kPageBlock * row_tiles(p.chunk_heads)));
+  // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch (4 us, as long as a wave
+  // takes for three tiles of one block and one row tile) and the search for a workgroup's part.  The more sequences there are,
+  // the less cutting gives: cut | not, us, at 10, 20, 32, 48 tiles of 128 wide heads and 4 bits: 48 workgroups 8.3 9.1 9.6 10.3
+  // | 6.9 9.3 12.5 17.1, 144: 9.8 10.7 13.7 15.0 | 7.0 9.3 13.9 18.4, 256: 10.5 13.8 15.8 18.4 | 7.1 11.0 14.4 19.4, 512:
+  // 12.7 16.6 20.7 26.4 | 10.1 13.6 17.9 23.9; 16 heads on 2 256 wide at 8 bits, 144: 25.6 32.6 43.5 48.2 | 18.7 26.8 36.9 50.9.
+  const int alone = std::max(4, 16 / (unit / kPageBlock * row_tiles(p.chunk_heads)));
+  const int whole = std::max(alone, static_cast<int>(std::min<int64_t>(static_cast<int64_t>(B) * each / 6, kWholeTiles)));
   p.join = most_tokens > whole * kTile;
   p.least = p.join ? kLeastTiles : whole;
   // (a sequence is cut in no more parts than its pages hold)
@@ -76,7 +82,7 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   return p;
 }
 
-// Workspace: [slots][n_q] {max, sum, the keys' zero-point term}, [slots][n_q][hd] weighted codes, [B] {first slot, parts}.
+// Workspace: [slots][n_q] {max, sum, the keys' zero-point term}, [slots][n_q][hd] weighted codes, [B] {slot of the second part, parts}.
 struct PartHead {
   float m, l, zterm, unused;
 };
@@ -189,58 +195,70 @@ struct Part {
   int b, len, index, count, first_tile, end_tile;
 };
 
-// The part that slot number `slot` holds; false: none.  Every sequence has at least one.  first_len: lane i's is that of
-// sequence i (or the last's); where sequences are not cut, that of sequence number `slot`, whose only part it is.
-__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int first_len, int slot, int lane, Part* out) {
+// The part that slot number `slot` holds; false: none.  A sequence's first part is in the slot of its own number, the others,
+// sequence after sequence, in those behind.  own_len: the length of sequence number `slot`; first_len: lane i's is that of sequence
+// i (or the last's), where sequences may be cut.
+__device__ __forceinline__ bool find_part(const AttendArgs& a, const AttendPlan& p, int first_len, int own_len, int slot, int lane, Part* out) {
   const int cap = a.pages_per_seq << a.g.page_shift;
-  auto clamped = [&](int i, int len) { return i < a.B ? min(max(len, 0), cap) : 0; };
-  auto len_of = [&](int i) { return clamped(i, a.lens[min(i, a.B - 1)]); };
+  auto clamped = [&](int len) { return min(max(len, 0), cap); };
+  auto len_of = [&](int i) { return i < a.B ? clamped(a.lens[min(i, a.B - 1)]) : 0; };
   auto tiles_of = [](int n) { return (n + kTile - 1) / kTile; };
   auto parts_of = [](int tiles, int n) {       // rounded up; (24 bits, which is all there is: a division by float)
     return ((static_cast<uint32_t>(tiles) + n - 1) & 0xffffffu) / (static_cast<uint32_t>(n) & 0xffffffu);
   };
   if (!p.join) {
     out->b = slot;
-    out->len = __builtin_amdgcn_readfirstlane(clamped(slot, first_len));
+    out->len = __builtin_amdgcn_readfirstlane(clamped(own_len));
     out->index = out->first_tile = 0;
     out->count = 1;
     out->end_tile = tiles_of(out->len);
     return true;
   }
-  const int len0 = clamped(lane, first_len);
+  const int len0 = lane < a.B ? clamped(first_len) : 0;
   double total;
   if (a.B <= 64) {
     total = __builtin_amdgcn_readlane(wave_prefix(tiles_of(len0)), 63);
   } else {
     total = tiles_of(len0);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 64; i < a.B; i += 64) total += tiles_of(len_of(i + lane));
     total = wave_sum(total);
   }
   // tiles of a part: all tiles over the number of parts, rounded up; no more than a sequence of 2^29 tokens has
   auto each_of = [&](double per) { return __builtin_amdgcn_readfirstlane(static_cast<int>(fmin((total - 1.0) * per, kMostTiles - 1.0))) + 1; };
   const int few = each_of(p.per_few), most = max(p.least, few <= kLongTiles ? few : max(kShortTiles, each_of(p.per_many)));
-  int before = 0, next_len = len0;
-  for (int base = 0; base < a.B; base += 64) {
-    const int i = base + lane, len = next_len;
-    if (base + 64 < a.B) next_len = len_of(i + 64);
-    const int n = i < a.B ? max<int>(1, parts_of(tiles_of(len), most)) : 0;
-    const int upto = wave_prefix(n);
-    const uint64_t hit = __ballot(slot >= before + upto - n && slot < before + upto);
-    if (hit != 0) {
-      const int l = __builtin_ctzll(hit);
-      out->b = base + l;
-      out->len = __builtin_amdgcn_readlane(len, l);
-      out->count = __builtin_amdgcn_readlane(n, l);
-      out->index = slot - before - __builtin_amdgcn_readlane(upto, l) + out->count;
-      const int tiles = tiles_of(out->len), each = parts_of(tiles, out->count);
-      out->first_tile = out->index * each;
-      out->end_tile = min(out->first_tile + each, tiles);
-      return true;
+  if (slot < a.B) {
+    out->b = slot;
+    out->len = __builtin_amdgcn_readfirstlane(clamped(own_len));
+    out->index = 0;
+    out->count = max<int>(1, parts_of(tiles_of(out->len), most));
+  } else {
+    // (a sequence of t tiles has at most (t - 1) / most further parts)
+    const int rank = slot - a.B;
+    if (__builtin_amdgcn_readfirstlane(total <= (rank + 1.0) * most)) return false;
+    int before = 0, next_len = len0;
+    for (int base = 0;; base += 64) {
+      if (base >= a.B) return false;
+      const int len = next_len;
+      if (base + 64 < a.B) next_len = len_of(base + 64 + lane);
+      const int n = max<int>(1, parts_of(tiles_of(len), most)) - 1;
+      const int upto = wave_prefix(n);
+      const uint64_t hit = __ballot(rank >= before + upto - n && rank < before + upto);
+      if (hit != 0) {
+        const int l = __builtin_ctzll(hit);
+        out->b = base + l;
+        out->len = __builtin_amdgcn_readlane(len, l);
+        out->count = __builtin_amdgcn_readlane(n, l) + 1;
+        out->index = rank - before - __builtin_amdgcn_readlane(upto, l) + out->count;
+        break;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
   }
-  return false;
+  const int tiles = tiles_of(out->len), each = parts_of(tiles, out->count);
+  out->first_tile = out->index * each;
+  out->end_tile = min(out->first_tile + each, tiles);
+  return true;
 }
 
 __device__ __forceinline__ void store_out(const AttendArgs& a, bool f32, int64_t at, float y) {
@@ -290,13 +308,15 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   }
 
   // (requested first: they depend on nothing, and the lengths are waited for first)
-  const int first_len = a.lens[min(plan.join ? lane : slot, a.B - 1)];
+  const int own_len = a.lens[min(slot, a.B - 1)];
+  int first_len = 0;
+  if (plan.join) first_len = a.lens[min(lane, a.B - 1)];
   // (one argument of every 64 bytes of them, so that all are fetched at once and not one after the other)
   asm volatile("" ::"s"(a.q), "s"(a.v_pos), "s"(a.page_table), "s"(a.workspace), "s"(plan.per_few));
   __builtin_amdgcn_sched_barrier(0);
-  // (a sequence that is not cut: its first pages' numbers as well, before its length is there to say which of them count)
+  // (a sequence's first part: its first pages' numbers as well, before the lengths are there to say which of them count)
   int early_page = 0;
-  if (!plan.join)
+  if (slot < a.B)
     early_page = a.page_table[slot * a.ld_pt + min(((wave + 4 * (lane >> 2)) * kTile + (lane & 3) * 16) >> a.g.page_shift, a.pages_per_seq - 1)];
   const KvPos* kt = a.k_pos + unit * P;
   KvPos kp[2 * NB];
@@ -304,7 +324,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   for (int i = 0; i < 2 * NB; ++i) kp[i] = kt[i * 64 + lane];
   const KvPos vp = a.v_pos[unit * P + tid % P];
   Part part;
-  if (!find_part(a, plan, first_len, slot, lane, &part)) return;
+  if (!find_part(a, plan, first_len, own_len, slot, lane, &part)) return;
 
   // ---- rows of this wave's tiles: lane 4k + i holds where its k-th tile's i-th 16 tokens lie, in bytes to the unit's first
   // block, and whether their page is there (else 0, the first page); sixteen tiles at a time, the next requested ahead ------
@@ -325,7 +345,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     const uint64_t row = (static_cast<uint64_t>(max(id, 0)) * (a.g.d / kPageBlock) + unit * NB) * block_rows + t;
     return Rows{static_cast<uint32_t>(row * kRow), static_cast<uint32_t>(row * kRow >> 32), __ballot(id >= 0)};
   };
-  const int first_page = !plan.join ? checked(0, early_page) : (my_tiles > 0 ? page_of(0) : -1);
+  const int first_page = part.index == 0 ? checked(0, early_page) : (my_tiles > 0 ? page_of(0) : -1);
   int next_page = my_tiles > 16 ? page_of(16) : -1;
 
   const int share = a.n_q / a.n_kv;
@@ -581,7 +601,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   }
   const PartBuffers buf = part_buffers(a, plan);
   const bool whole = part.count == 1;
-  if (part.index == 0 && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
+  if (part.index == (whole ? 0 : 1) && unit == 0 && chunk == 0 && tid == 0) buf.where[part.b] = make_int2(slot, part.count);
   __syncthreads();
   const int pos = tid % P, at = NB == 2 ? pos : pos & (a.hd - 1);
   const int from = (pos & ~(kPageBlock - 1)) + (pos >> 2 & 7) * 16 + (pos >> 5 & 3) * 4 + (pos & 3);
@@ -612,73 +632,78 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   }
 }
 
-// ---- the parts of a sequence together: a workgroup per (sequence, query head) ------------------------------------
+// ---- the parts of a sequence together: a workgroup per (sequence, `each` query heads) ------------------------------
 // A thread takes four channels of every (1024 / hd)-th part.
-__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPlan plan, bool f32) {
+template <bool SEVERAL>
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPlan plan, bool f32, int each) {
   __shared__ float weight[256], red[8];
   __shared__ __align__(16) float merge[256 * 4];
   typedef float f4 __attribute__((ext_vector_type(4)));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.x, b = blockIdx.y;
+  const int b = blockIdx.y;
   const PartBuffers buf = part_buffers(a, plan);
   const int2 where = buf.where[b];
   if (where.y <= 1) return;
-  const PartHead* heads = buf.heads + static_cast<int64_t>(where.x) * a.n_q + h;
-  const int per = a.hd / 4, c = tid % per, p0 = tid / per, step = 256 / per;
-  const f4* src = reinterpret_cast<const f4*>(buf.acc + (static_cast<int64_t>(where.x) * a.n_q + h) * a.hd) + c;
-  const int64_t row_f4 = static_cast<int64_t>(a.n_q) * per;
-  // (everything that a short join reads is requested before anything is waited for)
-  constexpr int kAhead = 4;
-  f4 first[kAhead];
+  int h = SEVERAL ? blockIdx.x * each : blockIdx.x;
+  const int end = SEVERAL ? min(h + each, a.n_q) : 0;
+  do {
+    auto row_of = [&](int part) { return static_cast<int64_t>(part == 0 ? b : where.x + part - 1) * a.n_q + h; };
+    const int per = a.hd / 4, c = tid % per, p0 = tid / per, step = 256 / per;
+    const f4* src = reinterpret_cast<const f4*>(buf.acc) + c;
+    // (everything that a short join reads is requested before anything is waited for)
+    constexpr int kAhead = 4;
+    f4 first[kAhead];
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) first[k] = src[min(p0 + k * step, where.y - 1) * row_f4];
-  const KvPos vp = a.v_pos[h / (a.n_q / a.n_kv) * a.hd + min(tid, a.hd - 1)];
-  float m = kNone, l = 0.0f;
-  f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int base = 0; base < where.y; base += 256) {
-    const int n = min(256, where.y - base);
-    const PartHead ph = heads[static_cast<int64_t>(base + min(tid, n - 1)) * a.n_q];
-    __syncthreads();                                          // (the weights of the 256 before have been read)
-    const float top = wave_max(ph.m);
-    if (lane == 0) red[wave] = top;
-    __syncthreads();
-    const float m_new = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float alpha = __builtin_amdgcn_exp2f(m - m_new), f = __builtin_amdgcn_exp2f(ph.m - m_new);
-    weight[tid] = f;
-    l = fmaf(l, alpha, tid < n ? ph.l * f : 0.0f);
+    for (int k = 0; k < kAhead; ++k) first[k] = src[row_of(min(p0 + k * step, where.y - 1)) * per];
+    const KvPos vp = a.v_pos[h / (a.n_q / a.n_kv) * a.hd + min(tid, a.hd - 1)];
+    float m = kNone, l = 0.0f;
+    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int base = 0; base < where.y; base += 256) {
+      const int n = min(256, where.y - base);
+      const PartHead ph = buf.heads[row_of(base + min(tid, n - 1))];
+      __syncthreads();                                          // (the weights of the 256 before have been read)
+      const float top = wave_max(ph.m);
+      if (lane == 0) red[wave] = top;
+      __syncthreads();
+      const float m_new = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new), f = __builtin_amdgcn_exp2f(ph.m - m_new);
+      weight[tid] = f;
+      l = fmaf(l, alpha, tid < n ? ph.l * f : 0.0f);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] *= alpha;
-    m = m_new;
-    __syncthreads();
-    int i = p0;
-    if (base == 0) {
+      for (int j = 0; j < 4; ++j) acc[j] *= alpha;
+      m = m_new;
+      __syncthreads();
+      int i = p0;
+      if (base == 0) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k, i += step)
-        if (i < n) {
+        for (int k = 0; k < kAhead; ++k, i += step)
+          if (i < n) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = fmaf(first[k][j], weight[i], acc[j]);
-        }
-    }
+            for (int j = 0; j < 4; ++j) acc[j] = fmaf(first[k][j], weight[i], acc[j]);
+          }
+      }
 #pragma unroll 8
-    for (; i < n; i += step) {
-      const f4 v = src[(base + i) * row_f4];
+      for (; i < n; i += step) {
+        const f4 v = src[row_of(base + i) * per];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = fmaf(v[j], weight[i], acc[j]);
+        for (int j = 0; j < 4; ++j) acc[j] = fmaf(v[j], weight[i], acc[j]);
+      }
     }
-  }
-  l = row16_add(l);
-  auto row = [&](int at) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), at)); };
-  l = (row(0) + row(16)) + (row(32) + row(48));
-  if (lane == 0) red[4 + wave] = l;
-  *reinterpret_cast<f4*>(merge + tid * 4) = acc;              // [part % step][channel]
-  __syncthreads();
-  l = (red[4] + red[5]) + (red[6] + red[7]);
-  if (tid < a.hd) {
-    float sum = 0.0f;
-    for (int i = 0; i < step; ++i) sum += merge[i * a.hd + tid];
-    store_out(a, f32, b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
-    if (a.lse && tid == 0) a.lse[static_cast<int64_t>(b) * a.n_q + h] = finish_lse(m, l, heads[0].zterm);
-  }
+    l = row16_add(l);
+    auto row = [&](int at) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), at)); };
+    l = (row(0) + row(16)) + (row(32) + row(48));
+    if (lane == 0) red[4 + wave] = l;
+    *reinterpret_cast<f4*>(merge + tid * 4) = acc;              // [part % step][channel]
+    __syncthreads();
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+    if (tid < a.hd) {
+      float sum = 0.0f;
+      for (int i = 0; i < step; ++i) sum += merge[i * a.hd + tid];
+      store_out(a, f32, b * a.ld_out + h * a.hd + (vp.src & (a.hd - 1)), finish(sum, l, vp));
+      if (a.lse && tid == 0) a.lse[static_cast<int64_t>(b) * a.n_q + h] = finish_lse(m, l, buf.heads[row_of(0)].zterm);
+    }
+    if (SEVERAL) __syncthreads();                               // (the next head's is another use of the shared memory)
+  } while (SEVERAL && ++h < end);
 }
 
 template <int BITS, int NB, int RT>
@@ -711,7 +736,9 @@ int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype
   else launch_bits<8>(a, p, f32, st);
   RPTQ_HIP(hipGetLastError());
   if (!p.join) return RPTQ_OK;
-  hipLaunchKernelGGL(attend_join_kernel, dim3(a.n_q, a.B), dim3(256), 0, st, a, p, f32);
+  const int each = std::max(1, std::min(a.n_q, a.B * a.n_q / kJoinWorkgroups));
+  const auto join = each > 1 ? attend_join_kernel<true> : attend_join_kernel<false>;
+  hipLaunchKernelGGL(join, dim3((a.n_q + each - 1) / each, a.B), dim3(256), 0, st, a, p, f32, each);
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;
 }

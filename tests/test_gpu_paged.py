@@ -274,6 +274,17 @@ def test_many_sequences(rp):
     b.check(q, 2, 64 ** -0.5, out, lse)
 
 
+def test_many_sequences_some_of_them_long(rp):
+    """More sequences than a wave has lanes, a few of them cut, and heads that are joined several at a time."""
+    lens = [int(n) for n in np.random.default_rng(5).integers(0, 500, 140)]
+    lens[3], lens[77], lens[139] = 6000, 2500, 5999
+    b = Batch(rp, lens, 1, 128, 4, 64)
+    q = b.queries(33)
+    for dtype in (torch.float32, torch.bfloat16):
+        out, lse = run(rp, b, q, 33, dtype)
+        b.check(q, 33, 128 ** -0.5, out, lse)
+
+
 def test_more_tiles_than_32_bits_count(rp):
     """Sequences of 2^27 tokens whose pages are there at the start and the end only: 2^31 tiles of 64 in the batch."""
     B, page, n_q = 1040, 4096, 2
