@@ -36,6 +36,9 @@ constexpr int kLeastTiles = 2;                 // of a part of a sequence that i
 constexpr int kWholeTiles = 48;                // of a sequence that is never cut at most (one such among short ones keeps the others waiting)
 constexpr int kMostTiles = 1 << 23;            // of a sequence
 constexpr int kJoinWorkgroups = 2048;          // that join parts, about: more take several heads each (512 x 1500 of 64 on 8 x 128: 136 | 127 us)
+// Bytes of keys and values that a call can reach: beyond the last-level cache's size they are read past it.  us without | with, the same
+// cache again and again: 36 MB 14.6 | 16.2, 100 MB 23.7 | 24.9, 250 MB 47.5 | 50.4, 350 MB 71.6 | 64.2, 1.2 GB 227 | 204 (5.9 TB/s).
+constexpr int64_t kStreamBytes = 256ll << 20;
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
@@ -282,8 +285,8 @@ __host__ __device__ constexpr int part_waves(int bits, int blocks, int tiles) {
 }
 
 // ---- the parts ---------------------------------------------------------------------------------------------
-// NB: blocks of a unit; RT: row tiles (of four heads)
-template <int BITS, int NB, int RT>
+// NB: blocks of a unit; RT: row tiles (of four heads); STREAM: codes past the last-level cache
+template <int BITS, int NB, int RT, bool STREAM>
 __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_kernel(AttendArgs a, AttendPlan plan, bool f32) {
   constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
@@ -370,6 +373,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   const uint32_t v_off = (4 * g4 + (n16 & 3)) * kRow + (n16 >> 2) * (4 * BITS);
   Rows rows_at = rows_of(0, first_page);
   // (buffer loads: a descriptor of the rows in scalar registers, a lane's offset in one register)
+  constexpr int kAux = STREAM ? 2 : 0;                     // (2: non-temporal)
   uint32_t kr[4][NB][BITS], vr[4][NB][BITS];
   const int block_bytes = block_rows * kRow;
   auto load_tile = [&](int k, const uint8_t* pages, uint32_t off, uint32_t (&x)[4][NB][BITS]) {
@@ -384,13 +388,13 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if constexpr (BITS == 3) {
-          const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rows, off, nb * block_bytes, 0);
+          const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rows, off, nb * block_bytes, kAux);
 #pragma unroll
           for (int e = 0; e < 3; ++e) x[r][nb][e] = v[e];
         } else {
 #pragma unroll
           for (int h = 0; h < BITS / 4; ++h) {
-            const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rows, off + 16 * h, nb * block_bytes, 0);
+            const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rows, off + 16 * h, nb * block_bytes, kAux);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[r][nb][4 * h + e] = v[e];
           }
@@ -707,22 +711,26 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPl
 }
 
 template <int BITS, int NB, int RT>
-static void launch_parts(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
+static void launch_parts(const AttendArgs& a, const AttendPlan& p, bool f32, bool stream, hipStream_t st) {
+  // (8 bits take a cache line by two loads, where streaming costs 7 %, and more row tiles may be parts of a unit's heads, whose
+  // workgroups read the same pages: 4 %)
+  constexpr bool kMay = BITS < 8 && NB * RT <= 2;
   const dim3 grid = p.chunks == 1 ? dim3(p.units, p.slots) : dim3(8 * p.chunks, p.units, (p.slots + 7) / 8);
-  hipLaunchKernelGGL((attend_part_kernel<BITS, NB, RT>), grid, dim3(256), 0, st, a, p, f32);
+  const auto kernel = kMay && stream ? attend_part_kernel<BITS, NB, RT, kMay> : attend_part_kernel<BITS, NB, RT, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, p, f32);
 }
 
 template <int BITS>
-static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t st) {
+static void launch_bits(const AttendArgs& a, const AttendPlan& p, bool f32, bool stream, hipStream_t st) {
   const int tiles = row_tiles(p.chunk_heads);
   if (a.hd > kPageBlock) {
-    if (tiles <= 1) launch_parts<BITS, 2, 1>(a, p, f32, st);
-    else launch_parts<BITS, 2, 2>(a, p, f32, st);
+    if (tiles <= 1) launch_parts<BITS, 2, 1>(a, p, f32, stream, st);
+    else launch_parts<BITS, 2, 2>(a, p, f32, stream, st);
   } else {
-    if (tiles <= 1) launch_parts<BITS, 1, 1>(a, p, f32, st);
-    else if (tiles == 2) launch_parts<BITS, 1, 2>(a, p, f32, st);
-    else if (tiles == 3) launch_parts<BITS, 1, 3>(a, p, f32, st);
-    else launch_parts<BITS, 1, 4>(a, p, f32, st);
+    if (tiles <= 1) launch_parts<BITS, 1, 1>(a, p, f32, stream, st);
+    else if (tiles == 2) launch_parts<BITS, 1, 2>(a, p, f32, stream, st);
+    else if (tiles == 3) launch_parts<BITS, 1, 3>(a, p, f32, stream, st);
+    else launch_parts<BITS, 1, 4>(a, p, f32, stream, st);
   }
 }
 
@@ -731,9 +739,11 @@ int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype
   const bool f32 = out_dtype == RPTQ_DTYPE_F32;
   const int64_t most_tokens = static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift;
   const AttendPlan p = attend_plan(a.B, a.n_q, a.n_kv, a.hd, most_tokens);
-  if (bits == 3) launch_bits<3>(a, p, f32, st);
-  else if (bits == 4) launch_bits<4>(a, p, f32, st);
-  else launch_bits<8>(a, p, f32, st);
+  const int64_t pages = std::min<int64_t>(a.g.n_pages, static_cast<int64_t>(a.B) * a.pages_per_seq);
+  const bool stream = pages * 2 * (static_cast<int64_t>(a.g.d) * bits / 8 << a.g.page_shift) > kStreamBytes;
+  if (bits == 3) launch_bits<3>(a, p, f32, stream, st);
+  else if (bits == 4) launch_bits<4>(a, p, f32, stream, st);
+  else launch_bits<8>(a, p, f32, stream, st);
   RPTQ_HIP(hipGetLastError());
   if (!p.join) return RPTQ_OK;
   const int each = std::max(1, std::min(a.n_q, a.B * a.n_q / kJoinWorkgroups));

@@ -285,6 +285,21 @@ def test_many_sequences_some_of_them_long(rp):
         b.check(q, 33, 128 ** -0.5, out, lse)
 
 
+@pytest.mark.parametrize("bits", [3, 4])
+@pytest.mark.parametrize("H,share,hd", [(32, 1, 128), (32, 5, 128), (16, 1, 256)])
+def test_pools_beyond_the_last_level_cache(rp, H, share, hd, bits):
+    """More than 256 MiB of codes within reach of the page table, few of them taken."""
+    b = Batch(rp, [300, 0, 65, 700], H, hd, bits, 64, extra_pages=1400)
+    width = torch.full((4, 400), -1, dtype=torch.int32, device="cuda")
+    width[:, :b.page_table.shape[1]] = b.page_table
+    b.page_table = width
+    assert 1400 * 2 * rp.rptq_kv_page_bytes(H * hd, 64, bits) > 1 << 28
+    n_q = H * share
+    q = b.queries(n_q)
+    out, lse = run(rp, b, q, n_q)
+    b.check(q, n_q, hd ** -0.5, out, lse)
+
+
 def test_more_tiles_than_32_bits_count(rp):
     """Sequences of 2^27 tokens whose pages are there at the start and the end only: 2^31 tiles of 64 in the batch."""
     B, page, n_q = 1040, 4096, 2
