@@ -29,10 +29,16 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
 constexpr int kTile = 64;                      // tokens of a wave's tile
-constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;    // two and eight per compute unit of 256
-constexpr int kLongTiles = 64;                 // of a part at most where there are few,
-constexpr int kShortTiles = 16;                // and at least where there are many
-constexpr int kLeastTiles = 2;                 // of a part of a sequence that is cut (1 | 2 | 4, us: 7 x 1531 of 16 on 2 x 256 at 4 bits 12.3 | 10.9 | 11.5, at 8 12.5 | 12.3 | 14.0)
+// Into how many parts the tokens of a batch are cut, us of 4-bit codes.  Few: two workgroups per compute unit of 256 (one | two | four:
+// 16 x 8192 of 32 on 8 x 128 23.8 | 20.2 | 21.9, 16 x 4096 of 32 x 64 20.7 | 20.6 | 21.4; but 32768 of 32 on 8 14.8 | 15.7 | 17.2), if
+// a part is then of kLongTiles tiles at most (32 | 64 | 128: 2 x 20000 of 40 x 128 47.6 | 45.6 | 45.7, 64 x 8000 of 32 on 8 58.2 |
+// 57.5 | 61.9).  Else many, so that a long sequence does not end alone: 2048 with one row tile, half as many where a workgroup
+// takes longer (1024 | 2048: 64 x 16000 of 8 x 128 102 | 95, but 256 x 4000 of 64 on 8 120 | 146), and parts of kShortTiles at least
+// (4 | 16 | 64: 128 x 1000 of 64 on 8, tables for more, 47.9 | 29.5 | 29.4, 32 x 4096 of 40 x 128 65.2 | 65.4 | 70.6).
+constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;
+constexpr int kLongTiles = 64;
+constexpr int kShortTiles = 16;
+constexpr int kLeastTiles = 2;                 // of a part of a sequence that is cut (1 | 2 | 4: 7 x 1531 of 16 on 2 x 256 12.3 | 10.9 | 11.5, at 8 bits 12.5 | 12.3 | 14.0)
 constexpr int kWholeTiles = 48;                // of a sequence that is never cut at most (one such among short ones keeps the others waiting)
 constexpr int kMostTiles = 1 << 23;            // of a sequence
 constexpr int kJoinWorkgroups = 2048;          // that join parts, about: more take several heads each (512 x 1500 of 64 on 8 x 128: 136 | 127 us)
@@ -69,19 +75,20 @@ static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, 
   auto parts = [&](int workgroups) { return std::max(1, (workgroups + each - 1) / each); };
   // (rounding up adds half a part per sequence)
   p.per_few = 1.0 / parts(kFewWorkgroups - static_cast<int>(std::min<int64_t>(static_cast<int64_t>(B) * each / 2, kFewWorkgroups - 1))) * (1.0 + 0x1p-50);
-  p.per_many = 1.0 / parts(kManyWorkgroups) * (1.0 + 0x1p-50);
+  const int weight = unit / kPageBlock * row_tiles(p.chunk_heads), many = parts(weight == 1 ? kManyWorkgroups : kManyWorkgroups / 2);
+  p.per_many = 1.0 / many * (1.0 + 0x1p-50);
   // A sequence that cannot be longer than `whole` tiles is not cut, which saves the second launch (4 us, as long as a wave
   // takes for three tiles of one block and one row tile) and the search for a workgroup's part.  The more sequences there are,
   // the less cutting gives: cut | not, us, at 10, 20, 32, 48 tiles of 128 wide heads and 4 bits: 48 workgroups 8.3 9.1 9.6 10.3
   // | 6.9 9.3 12.5 17.1, 144: 9.8 10.7 13.7 15.0 | 7.0 9.3 13.9 18.4, 256: 10.5 13.8 15.8 18.4 | 7.1 11.0 14.4 19.4, 512:
   // 12.7 16.6 20.7 26.4 | 10.1 13.6 17.9 23.9; 16 heads on 2 256 wide at 8 bits, 144: 25.6 32.6 43.5 48.2 | 18.7 26.8 36.9 50.9.
-  const int alone = std::max(4, 16 / (unit / kPageBlock * row_tiles(p.chunk_heads)));
+  const int alone = std::max(4, 16 / weight);
   const int whole = std::max(alone, static_cast<int>(std::min<int64_t>(static_cast<int64_t>(B) * each / 6, kWholeTiles)));
   p.join = most_tokens > whole * kTile;
   p.least = p.join ? kLeastTiles : whole;
   // (a sequence is cut in no more parts than its pages hold)
   const int64_t per_seq = (most_tokens + p.least * kTile - 1) / (p.least * kTile);
-  p.slots = static_cast<int32_t>(std::min<int64_t>(parts(kManyWorkgroups) + static_cast<int64_t>(B), B * per_seq));   // (not cut: B)
+  p.slots = static_cast<int32_t>(std::min<int64_t>(many + static_cast<int64_t>(B), B * per_seq));   // (not cut: B)
   return p;
 }
 
