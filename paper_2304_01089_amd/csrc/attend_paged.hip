@@ -11,9 +11,18 @@
 // tile of 64 tokens once to fp32.
 //
 // A workgroup takes a part of one sequence for the heads that read one block of 128 positions (two for heads 256 wide), a
-// wave every fourth tile of 64 tokens.  How sequences are cut in parts follows their lengths, which the kernel reads: parts
-// of equal length over the whole batch, as many as fill the chip.  Parts leave (max, sum, weighted codes), a second kernel
-// joins them; sequences of one part are finished at once.
+// wave every fourth tile of 64 tokens: scores, weights and weighted codes of a tile stay in registers, its weights cross 1 KiB of
+// LDS to become an operand, keys and values of the next tile are requested before they are needed.  How sequences are cut in parts
+// follows their lengths, which the kernel reads: parts of equal length over the whole batch, as many as fill the chip.  Parts
+// leave (max, sum, weighted codes), a second kernel joins them; sequences of one part are finished at once.
+//
+// What bounds it.  One row tile: memory, 16 x 8192 tokens of 96 x 128 at 3 bits 203 us, 5.95 TB/s; 32 x 4096 of 40 x 128 at 4 bits
+// (half as many on average) 65 us, 5.3 TB/s.  More row tiles: vector instructions, 339 a tile of 4-bit codes with one and 841 with
+// four, of which 56 a row tile bring the digits' sums of 8 x 4 outputs together (16 x 8192 of 8 x 128, half as many on average, by
+// query heads 32, 64, 128: 20, 23, 35 us; memory 14).  Few tokens: a chain of latencies, 7 us for 257 tokens (lengths and page
+// numbers 1.0, keys, values and queries 1.2, a tile 0.9, the waves together and the stores 0.7, the launch the rest), and 4 more for
+// the second launch.  Tried: waves that take a row tile each and share the tokens (16 x 8192 of 64 on 8 27 -> 33 us: four
+// times the loads), a wave by itself per short sequence (512 x 60 19 -> 13 us, but 32 x 1000 9 -> 24: a wave takes 1.1 us a tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
