@@ -423,30 +423,35 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     load_tile(0, a.v_pages, v_off, vr);
   }
 
-  // ---- queries to digits: wave w takes head w of every row tile ------------------------------------------------
+  // ---- queries to digits: wave w takes head w of every row tile (all of them side by side: each is a chain of reductions) ----
   unsigned char* q_dig = smem;
+  float qx[RT][2 * NB], q_top[RT];
+  bool q_bad[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int hh = rt * kRowHeads + wave;
-    float x[2 * NB], top = 0.0f;
-    bool bad = false;
+    q_top[rt] = 0.0f;
+    q_bad[rt] = false;
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) {
-      x[i] = __uint_as_float(static_cast<uint32_t>(q_raw[rt][i]) << 16) * kp[i].s * (a.scale * kLog2e);
-      if (hh >= heads || !own(hh, i * 64 + lane)) x[i] = 0.0f;
-      top = fmaxf(top, fabsf(x[i]));
-      bad = bad || !(fabsf(x[i]) < __builtin_huge_valf());
+      const float x = __uint_as_float(static_cast<uint32_t>(q_raw[rt][i]) << 16) * kp[i].s * (a.scale * kLog2e);
+      qx[rt][i] = hh < heads && own(hh, i * 64 + lane) ? x : 0.0f;
+      q_top[rt] = fmaxf(q_top[rt], fabsf(qx[rt][i]));
+      q_bad[rt] = q_bad[rt] || !(fabsf(qx[rt][i]) < __builtin_huge_valf());
     }
-    top = wave_max(top);
-    const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;           // top < 2^e
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) q_top[rt] = wave_max(q_top[rt]);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int hh = rt * kRowHeads + wave, e = q_top[rt] > 0.0f ? __builtin_amdgcn_frexp_expf(q_top[rt]) : 0;          // q_top < 2^e
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) {
-      const uint32_t d = digits(static_cast<int>(rintf(ldexpf(x[i], 30 - e))));
+      const uint32_t d = digits(static_cast<int>(rintf(ldexpf(qx[rt][i], 30 - e))));
 #pragma unroll
-      for (int b = 0; b < 4; ++b) q_dig[(rt * 16 + wave * 4 + b) * P + i * 64 + lane] = static_cast<unsigned char>(d >> (8 * b));
+      for (int b = 0; b < 4; ++b) q_dig[(hh * 4 + b) * P + i * 64 + lane] = static_cast<unsigned char>(d >> (8 * b));
     }
-    const bool any_bad = __ballot(bad) != 0;
-    if (lane == 0) h_scale[hh] = any_bad ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);
+    h_scale[hh] = __ballot(q_bad[rt]) != 0 ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);          // (every lane the same)
   }
   __syncthreads();
   // One row tile's operands stay in registers, more are read again for every tile.
