@@ -453,8 +453,8 @@ int32_t rptq_kv_dequant(const void* codes, int64_t T, int32_t d, const void* tab
  *   workspace device, rptq_attend_paged_workspace_bytes(B, n_q_heads, n_kv_heads, head_dim) bytes; nothing
  *           in it has to be cleared or kept between calls; calls that overlap in time need one each
  * Sums and softmax statistics are fp32 or exact integers; a sequence's last bits may depend on
- * the other lengths of the call (they decide where sequences are split).  A NaN or infinity in q, or a
- * score beyond fp32, makes its head's output NaN.
+ * the other lengths of the call (they decide where sequences are split).  A NaN or infinity in q makes
+ * its head's output NaN where there are tokens; a score beyond fp32 may.
  * pages_per_seq * page_size <= 2^29; strides (ld_*) are >= the row and, but for the page table's, multiples of 8.
  *
  * All three are asynchronous on `stream`, allocate nothing and may be recorded into a graph after the first

@@ -285,6 +285,23 @@ def test_many_sequences_some_of_them_long(rp):
         b.check(q, 33, 128 ** -0.5, out, lse)
 
 
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 128, 129])
+def test_batches_around_a_wave_of_lengths(rp, B):
+    """Page tables for more than any sequence has, so that every sequence may be cut: one that is, wherever it stands, among short
+    and empty ones; and nothing at all."""
+    for long_one in sorted({0, B // 2, B - 1}):
+        lens = [(7 * i + B) % 90 * (i % 5 != 0) for i in range(B)]
+        lens[long_one] = 4000
+        b = Batch(rp, lens, 1, 128, 3, 64, seed=B)
+        b.page_table = torch.cat([b.page_table, torch.full((B, 100), -1, dtype=torch.int32, device="cuda")], 1)
+        q = b.queries(2)
+        out, lse = run(rp, b, q, 2)
+        b.check(q, 2, 128 ** -0.5, out, lse)
+    b.dev_lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    out, lse = run(rp, b, q, 2)
+    assert (out == 0).all() and (lse == -float("inf")).all()
+
+
 @pytest.mark.parametrize("bits", [3, 4])
 @pytest.mark.parametrize("H,share,hd", [(32, 1, 128), (32, 5, 128), (16, 1, 256)])
 def test_pools_beyond_the_last_level_cache(rp, H, share, hd, bits):
