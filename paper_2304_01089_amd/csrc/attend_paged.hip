@@ -72,12 +72,13 @@ struct AttendPlan {
   int32_t slots;                               // parts that there may be: one more per sequence, from rounding up
 };
 
-static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, int64_t most_tokens) {
+// row_tiles_of_one: a workgroup's at most.
+static AttendPlan attend_plan(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd, int64_t most_tokens, int row_tiles_of_one) {
   AttendPlan p;
   const int unit = hd > kPageBlock ? hd : kPageBlock;
   p.units = n_kv * hd / unit;
   p.unit_heads = n_q / p.units;
-  const int most = kRowHeads * most_row_tiles(unit / kPageBlock);
+  const int most = kRowHeads * row_tiles_of_one;
   p.chunks = (p.unit_heads + most - 1) / most;
   p.chunk_heads = (p.unit_heads + p.chunks - 1) / p.chunks;
   const int each = p.units * p.chunks;
@@ -107,8 +108,10 @@ struct PartHead {
 };
 
 size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd) {
-  const AttendPlan p = attend_plan(B, n_q, n_kv, hd, INT64_C(1) << 30);
-  const size_t rows = static_cast<size_t>(p.slots) * n_q;
+  int64_t slots = 0;
+  for (int rt = 1; rt <= most_row_tiles(hd > kPageBlock ? 2 : 1); ++rt)
+    slots = std::max<int64_t>(slots, attend_plan(B, n_q, n_kv, hd, INT64_C(1) << 30, rt).slots);
+  const size_t rows = static_cast<size_t>(slots) * n_q;
   return rows * sizeof(PartHead) + rows * hd * sizeof(float) + ((static_cast<size_t>(B) + 1) / 2) * 16;
 }
 
@@ -759,7 +762,20 @@ int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype
   if (a.B == 0) return RPTQ_OK;
   const bool f32 = out_dtype == RPTQ_DTYPE_F32;
   const int64_t most_tokens = static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift;
-  const AttendPlan p = attend_plan(a.B, a.n_q, a.n_kv, a.hd, most_tokens);
+  // As few row tiles in a workgroup, and the heads that read a unit over as many workgroups, as the chip has room for if all
+  // pages are full: four tiles for each of 1024 waves (two at 8 bits, where reading the pages again costs more), and no more than 1024
+  // workgroups (512 of heads 256 wide) if every sequence is short.  us with most row tiles | with this: 9 x 3 tokens of 28 heads on 4 x 64
+  // 8.1 | 4.7, 3 x 441 of 154 on 22 x 64 11.9 | 7.7, 2 x 13815 of 20 on 4 x 64 14.5 | 12.0, 16000 of 128 on 8 x 128 18.3 | 15.6, 7 x 1531 of
+  // 16 on 2 x 256 at 8 bits 12.7 | 11.5; but beyond the room 16 x 8192 of 128 on 8 x 128 35 | 38, at 8 bits 44 | 54, 8 x 2000 of 64 on 8 at 8
+  // bits 16.5 | 18.1, 32 x 15 of 144 on 48 x 32 8.4 | 8.7, 59 x 7 of 40 on 5 x 256 9.4 | 10.9.
+  const int blocks = a.hd > kPageBlock ? 2 : 1;
+  const int64_t tiles = (most_tokens + kTile - 1) / kTile * a.B, room = bits == 8 && blocks == 1 ? 2048 : 4096;
+  AttendPlan p;
+  for (int rt = 1; rt <= most_row_tiles(blocks); ++rt) {
+    p = attend_plan(a.B, a.n_q, a.n_kv, a.hd, most_tokens, rt);
+    const int64_t each = static_cast<int64_t>(p.units) * p.chunks;
+    if (tiles * each <= room && a.B * each <= 1024 / blocks) break;
+  }
   const int64_t pages = std::min<int64_t>(a.g.n_pages, static_cast<int64_t>(a.B) * a.pages_per_seq);
   const bool stream = pages * 2 * (static_cast<int64_t>(a.g.d) * bits / 8 << a.g.page_shift) > kStreamBytes;
   if (bits == 3) launch_bits<3>(a, p, f32, stream, st);

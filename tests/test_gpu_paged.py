@@ -257,6 +257,18 @@ def test_head_layouts(rp, H, share, hd, bits, page, lens):
         b.check(q, n_q, hd ** -0.5, out, lse)
 
 
+@pytest.mark.parametrize("bits", [3, 4, 8])
+@pytest.mark.parametrize("H,share,hd", [(1, 6, 128), (1, 12, 128), (1, 16, 128), (1, 17, 128), (2, 7, 64), (4, 4, 32), (1, 8, 256), (1, 11, 256)])
+def test_many_heads_of_a_workgroup(rp, H, share, hd, bits):
+    """Page tables for so many tokens that a workgroup takes as many heads as it can."""
+    b = Batch(rp, EDGES, H, hd, bits, 16)
+    b.page_table = torch.cat([b.page_table, torch.full((len(EDGES), 1500), -1, dtype=torch.int32, device="cuda")], 1)
+    n_q = H * share
+    q = b.queries(n_q)
+    out, lse = run(rp, b, q, n_q)
+    b.check(q, n_q, hd ** -0.5, out, lse)
+
+
 @pytest.mark.parametrize("bits,page,lens", [(4, 16, [9001]), (3, 64, [20011, 5]), (8, 256, [4096, 7000, 0, 12345]),
                                             (4, 128, [33000])])
 def test_long_sequences(rp, bits, page, lens):
