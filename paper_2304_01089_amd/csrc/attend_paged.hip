@@ -456,6 +456,17 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     }
     h_scale[hh] = __ballot(q_bad[rt]) != 0 ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);          // (every lane the same)
   }
+  // (what the zero points of the keys add to a head's scores: lse alone sees it)
+  if (a.lse && part.index == 0) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      double z = 0.0;
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) z += static_cast<double>(qx[rt][i]) * kp[i].z;
+      z = wave_sum(z);
+      if (lane == 0) h_z[rt * kRowHeads + wave] = static_cast<float>(z);
+    }
+  }
   __syncthreads();
   // One row tile's operands stay in registers, more are read again for every tile.
   auto q_operand = [&](int rt, int nb, int s) {
@@ -594,22 +605,6 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
   }
 
   // ---- the waves' sums together ------------------------------------------------------------------------------------
-  // (what the zero points of the keys add to a head's scores: lse alone sees it)
-  if (a.lse && part.index == 0) {
-#pragma unroll 1
-    for (int hh = wave; hh < heads; hh += 4) {
-      double z = 0.0;
-#pragma unroll
-      for (int i = 0; i < 2 * NB; ++i) {
-        const KvPos k = kt[i * 64 + lane];
-        const uint32_t h = a.q[part.b * a.ld_q + (q_head + hh) * a.hd + (k.src & (a.hd - 1))];
-        const float x = __uint_as_float(h << 16) * k.s * (a.scale * kLog2e);
-        z += own(hh, i * 64 + lane) ? static_cast<double>(x) * k.z : 0.0;
-      }
-      z = wave_sum(z);
-      if (lane == 0) h_z[hh] = static_cast<float>(z);
-    }
-  }
   // (first the largest scores, so that every wave scales its own sums once)
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
