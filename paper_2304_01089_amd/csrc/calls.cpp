@@ -321,7 +321,7 @@ struct Rows {
       return false;
     rows = size[0], cols = size[1];
     ld = rows > 1 ? step[0] : cols;
-    return rows >= 1 && cols > 1 && cols <= INT32_MAX && step[1] == 1;
+    return rows >= 1 && cols >= 1 && cols <= INT32_MAX && (cols == 1 || step[1] == 1);
   }
 };
 

@@ -705,3 +705,17 @@ def test_native_and_python_marshalling(rp, monkeypatch):
         assert native(*args[:-1]) is None and native(*args, None) is None, name
         torch.cuda.synchronize()
         assert all((t.view(torch.uint8) == 0x3c).all() for t in outs), name
+
+
+@pytest.mark.parametrize("lens", [[3], [16], [16, 5], [1, 0, 7]])
+def test_tables_of_one_page_are_marshalled_natively(rp, lens):
+    from paper_2304_01089_amd import binding
+    b = Batch(rp, lens, 2, 64, 4, 16)
+    assert b.page_table.shape[1] == 1
+    q = b.queries(4)
+    out, ws = torch.full((len(lens), 256), float("nan"), device="cuda"), rp.attend_paged_workspace(b.cache, len(lens), 4)
+    c = b.cache
+    assert binding._CALLS.attend_paged(dev_bf16(q), 4, 2, 64, 0.125, c.k_table, c.v_table, 4, c.k_pages, c.v_pages, 16, b.page_table,
+                                       b.dev_lens, out, None, ws, None) == 0
+    torch.cuda.synchronize()
+    b.check(q, 4, 0.125, out)
