@@ -56,7 +56,7 @@ ATTEND = dict(q=F, ld_q=1024, B=4, n_q=8, n_kv=2, hd=128, scale=0.1, k_table=F, 
 BAD_ATTEND = [(name, None, NULL) for name in ("q", "k_table", "v_table", "k_pages", "v_pages", "page_table", "lens", "out", "workspace")]
 BAD_ATTEND += [(name, ODD, ALIGN) for name in ("q", "k_table", "v_table", "k_pages", "v_pages", "out", "workspace")]
 BAD_ATTEND += [(name, ctypes.c_void_p(4098), ALIGN) for name in ("page_table", "lens", "lse")]
-BAD_ATTEND += [("bits", 2, BITS), ("B", -1, SHAPE), ("n_q", 7, SHAPE), ("n_q", 0, SHAPE), ("n_kv", 0, SHAPE), ("n_kv", -2, SHAPE), ("hd", 80, SHAPE),
+BAD_ATTEND += [("bits", 2, BITS), ("B", -1, SHAPE), ("B", 32769, SHAPE), ("n_q", 7, SHAPE), ("n_q", 0, SHAPE), ("n_kv", 0, SHAPE), ("n_kv", -2, SHAPE), ("hd", 80, SHAPE),
                ("hd", 16, SHAPE), ("hd", 0, SHAPE), ("n_q", 512, SHAPE), ("ld_q", 1016, SHAPE), ("ld_q", 1028, SHAPE), ("ld_out", 0, SHAPE),
                ("per_seq", 0, SHAPE), ("ld_pt", 2, SHAPE), ("dtype", 2, SHAPE), ("n_pages", 0, SHAPE), ("page_size", 20, SHAPE),
                ("scale", float("nan"), RANGE), ("scale", float("inf"), RANGE), ("ws_bytes", 0, WORKSPACE)]
