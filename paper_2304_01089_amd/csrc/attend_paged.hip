@@ -38,8 +38,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
 constexpr int kTile = 64;                      // tokens of a wave's tile
-// Into how many parts the tokens of a batch are cut, us of 4-bit codes.  Few: two workgroups per compute unit of 256 (one | two | four:
-// 16 x 8192 of 32 on 8 x 128 23.8 | 20.2 | 21.9, 16 x 4096 of 32 x 64 20.7 | 20.6 | 21.4; but 32768 of 32 on 8 14.8 | 15.7 | 17.2), if
+// Into how many parts the tokens of a batch are cut, us of 4-bit codes.  Few: two workgroups per compute unit of 256 (one | two: 16 x
+// 8192 of 32 on 8 x 128 22.8 | 19.4, 2 x 20000 of 40 x 128 47.9 | 45.6, 3500 of 96 x 128 at 3 bits 17.3 | 14.9; but 8000 of 32 on 8 9.2 | 10.2;
+// two | four: 16 x 8192 20.2 | 21.9, 32768 of 32 on 8 16.4 | 17.8), if
 // a part is then of kLongTiles tiles at most (32 | 64 | 128: 2 x 20000 of 40 x 128 47.6 | 45.6 | 45.7, 64 x 8000 of 32 on 8 58.2 |
 // 57.5 | 61.9).  Else many, so that a long sequence does not end alone: 2048 with one row tile, half as many where a workgroup
 // takes longer (1024 | 2048: 64 x 16000 of 8 x 128 102 | 95, but 256 x 4000 of 64 on 8 120 | 146), and parts of kShortTiles at least
