@@ -626,6 +626,15 @@ def _whole(t, dtype, what: str, least: int):
     return p
 
 
+def _position_table(t, what: str, d: int):
+    """Address of a table of exactly d records.  (Pages of half the channels divide the same pool: only the table tells whether
+    rows of this width are the cache's.)"""
+    p = _whole(t, None, what, 16 * d)
+    if t.numel() * t.element_size() != 16 * d:
+        raise ValueError("%s: %d bytes, %d for %d channels" % (what, t.numel() * t.element_size(), 16 * d, d))
+    return p
+
+
 def _matrix(t, dtype, what: str, shape):
     """(address, elements from row to row) of a two-dimensional tensor with contiguous rows."""
     p = _here(t, dtype, what)
@@ -663,7 +672,7 @@ def rptq_kv_page_bytes(d: int, page_size: int, bits: int) -> int:
 
 
 def rptq_kv_quant_paged(k, v, slots, k_table, v_table, bits: int, k_pages, v_pages, page_size: int, stream=None):
-    """k, v: bf16 [T, d], rows of any stride; slots: int64 [T]; pages: uint8, a whole number of pages."""
+    """k, v: bf16 [T, d], rows of any stride; slots: int64 [T]; tables: 16 d bytes; pages: uint8, a whole number of pages."""
     st = None if _CALLS is None else _CALLS.kv_quant_paged(k, v, slots, k_table, v_table, bits, k_pages, v_pages, page_size, stream)
     if st is None:
         import torch
@@ -671,7 +680,7 @@ def rptq_kv_quant_paged(k, v, slots, k_table, v_table, bits: int, k_pages, v_pag
         kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
         (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
         st = load_library().rptq_kv_quant_paged(
-            ka, ld_k, va, ld_v, T, d, _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), bits,
+            ka, ld_k, va, ld_v, T, d, _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), bits,
             _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
     _check(st, "rptq_kv_quant_paged")
 
@@ -686,7 +695,7 @@ def rptq_kv_dequant_paged(k_pages, v_pages, page_size: int, bits: int, slots, k_
         (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
         st = load_library().rptq_kv_dequant_paged(
             kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
-            _whole(k_table, None, "k_table", 16 * d), _whole(v_table, None, "v_table", 16 * d), ka, ld_k, va, ld_v,
+            _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), ka, ld_k, va, ld_v,
             _stream(stream)) if T else 0
     _check(st, "rptq_kv_dequant_paged")
 
@@ -719,8 +728,8 @@ def rptq_attend_paged(q, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: 
         pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
         la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
         st = load_library().rptq_attend_paged(
-            qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _whole(k_table, None, "k_table", 16 * d),
-            _whole(v_table, None, "v_table", 16 * d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
+            qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d),
+            _position_table(v_table, "v_table", d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
             _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
             workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_paged")

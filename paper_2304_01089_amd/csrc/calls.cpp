@@ -325,7 +325,8 @@ struct Rows {
   }
 };
 
-// Both tensors' pages and tables: the same whole number of pages, and a record for each of d positions.
+// Both tensors' pages and tables: the same whole number of pages, and a record for each of d positions and no more (a table of
+// another width is another cache's).
 struct Pages {
   uint8_t *k, *v;
   void *k_table, *v_table;
@@ -337,7 +338,7 @@ struct Pages {
     if (size == 0 || !get_whole(kp, t_u8, device, &k, &kb) || !get_whole(vp, t_u8, device, &v, &vb) || kb != vb || kb < size || kb % size != 0)
       return false;
     n = kb / size;
-    return get_whole(kt, nullptr, device, &k_table, &ktb) && get_whole(vt, nullptr, device, &v_table, &vtb) && ktb >= 16 * d && vtb >= 16 * d;
+    return get_whole(kt, nullptr, device, &k_table, &ktb) && get_whole(vt, nullptr, device, &v_table, &vtb) && ktb == 16 * d && vtb == 16 * d;
   }
 };
 
