@@ -191,7 +191,8 @@ def cluster_gemm_cw(cal: Calibration, lin: FoldedLinearCw, codes, rowsums, M, y=
 # ---- the key/value cache in pages ------------------------------------------------------------------
 @dataclass
 class PagedCache:
-    """Keys and values of one layer: pages of codes, and the position tables (rptq_kv_tables) they are written and read by."""
+    """Keys and values of one layer: pages of codes, and the position tables (rptq_kv_tables, of n_heads heads) they are written and
+    read by.  The pages have to have the shape that the sizes name: it is compared at the first call after any of them was set."""
     n_heads: int
     head_dim: int
     bits: int
@@ -201,25 +202,46 @@ class PagedCache:
     k_table: object
     v_table: object
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_compared", False)
+
+    def compare(self):
+        """Refuses pages of another shape than the sizes name: the codes would be taken for other tokens' or channels'."""
+        _page_bytes(self.n_heads * self.head_dim, self.page_size, self.bits)
+        want = (self.n_heads * self.head_dim // 128, self.page_size, 16 * self.bits)
+        for name, pages in (("k_pages", self.k_pages), ("v_pages", self.v_pages)):
+            if pages.dim() != 4 or tuple(pages.shape[1:]) != want:
+                raise ValueError("%s: expected shape [pages, %d, %d, %d], got %s" % ((name,) + want + (tuple(pages.shape),)))
+        object.__setattr__(self, "_compared", True)
+
+
+def _page_bytes(d: int, page_size: int, bits: int) -> int:
+    n = B.rptq_kv_page_bytes(d, page_size, bits)
+    if n == 0:
+        raise B.RptqError(-3 if bits not in (3, 4, 8) else -2, "rptq_kv_page_bytes")
+    return n
+
 
 def paged_cache(n_pages: int, page_size: int, n_heads: int, head_dim: int, bits: int, k_table, v_table) -> PagedCache:
     """A cache with room for n_pages * page_size tokens.  (What no token was written to holds no values: no call reads it but
     for a token that a page table and a length claim.)"""
     import torch
     d = n_heads * head_dim
-    if B.rptq_kv_page_bytes(d, page_size, bits) == 0:
-        raise B.RptqError(-3 if bits not in (3, 4, 8) else -2, "rptq_kv_page_bytes")
+    _page_bytes(d, page_size, bits)
     pages = [torch.zeros((n_pages, d // 128, page_size, 16 * bits), dtype=torch.uint8, device=k_table.device) for _ in range(2)]
     return PagedCache(n_heads, head_dim, bits, page_size, pages[0], pages[1], k_table, v_table)
 
 
 def kv_quant_paged(cache: PagedCache, k, v, slots):
     """Keys and values [T, d] of new tokens into the cache; a negative slot: that row is stored nowhere."""
+    cache._compared or cache.compare()
     B.rptq_kv_quant_paged(k, v, slots, cache.k_table, cache.v_table, cache.bits, cache.k_pages, cache.v_pages, cache.page_size)
 
 
 def kv_dequant_paged(cache: PagedCache, slots, k=None, v=None):
     """The rows at these slots, bf16 in the original channel order; where a slot is none, zeros, or what a given tensor held."""
+    cache._compared or cache.compare()
     if k is None or v is None:
         import torch
         shape = (slots.shape[0], cache.n_heads * cache.head_dim)
@@ -241,6 +263,7 @@ def attend_paged_workspace(cache: PagedCache, batch: int, n_q_heads: int):
 def attend_paged(cache: PagedCache, q, page_table, lens, scale=None, out=None, lse=None, want_lse=False, workspace=None):
     """Attention of one new token of every sequence over the cache.  q: [B, n_q_heads * head_dim]; scale: 1 / sqrt(head_dim)
     unless given.  Returns (out, lse); lse is None unless given or wanted."""
+    cache._compared or cache.compare()
     n_q_heads = q.shape[1] // cache.head_dim
     if out is None or (lse is None and want_lse) or workspace is None:
         import torch
