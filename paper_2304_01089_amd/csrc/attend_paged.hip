@@ -293,8 +293,9 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, bool f32, int64_t
 __device__ __forceinline__ float finish(float acc, float l, const KvPos& v) {
   return l != 0.0f ? v.s * (acc / l - static_cast<float>(v.z)) : 0.0f;
 }
+// (l is a sum of weights times 2^30, which comes off it before the logarithm: next to 30 a small score would be rounded to 2^-20)
 __device__ __forceinline__ float finish_lse(float m, float l, float zterm) {
-  return l != 0.0f ? kLn2 * ((m - 30.0f - zterm) + __log2f(l)) : -__builtin_huge_valf();
+  return l != 0.0f ? kLn2 * ((m - zterm) + __log2f(l * 0x1p-30f)) : -__builtin_huge_valf();
 }
 
 // Waves per SIMD that the registers are shared out for: what is fastest, with few spills or none.  (three with two row tiles at 8 bits,
