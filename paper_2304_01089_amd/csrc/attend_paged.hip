@@ -293,9 +293,8 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, bool f32, int64_t
 __device__ __forceinline__ float finish(float acc, float l, const KvPos& v) {
   return l != 0.0f ? v.s * (acc / l - static_cast<float>(v.z)) : 0.0f;
 }
-// (l is a sum of weights times 2^30, which comes off it before the logarithm: next to 30 a small score would be rounded to 2^-20)
 __device__ __forceinline__ float finish_lse(float m, float l, float zterm) {
-  return l != 0.0f ? kLn2 * ((m - zterm) + __log2f(l * 0x1p-30f)) : -__builtin_huge_valf();
+  return l != 0.0f ? kLn2 * ((m - zterm) + __log2f(l)) : -__builtin_huge_valf();
 }
 
 // Waves per SIMD that the registers are shared out for: what is fastest, with few spills or none.  (three with two row tiles at 8 bits,
@@ -566,9 +565,10 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
       v4i d;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f((s[r] - top) + 30.0f);
+        // (2^30 is a factor of the weight and no term of its exponent, which next to 30 would be rounded to 2^-20)
+        const float e = __builtin_amdgcn_exp2f(s[r] - top);
         sum += e;
-        d[r] = static_cast<int>(quad_transpose(digits(static_cast<int>(e)), sel));
+        d[r] = static_cast<int>(quad_transpose(digits(static_cast<int>(e * 0x1p30f)), sel));
       }
       l_run[rt] = fmaf(l_run[rt], alpha[rt], sum * beta[rt]);
       m_run[rt] = m_new;
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
     const float m = fmaxf(fmaxf(w_m[0][hh], w_m[1][hh]), fmaxf(w_m[2][hh], w_m[3][hh]));
     const float f = __builtin_amdgcn_exp2f(m_run[rt] - m), l = row16_add(l_run[rt]) * f;
     if (n16 == 0) w_l[wave][hh] = l;
-    const float fs = f * (1.0f / (1 << kShift));
+    const float fs = f * (0x1p-30f / (1 << kShift));
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll

@@ -55,6 +55,38 @@ def attend(rp, cache, q, tokens, scale, wide):
 
 
 @pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("bits", [3, 4, 8])
+@pytest.mark.parametrize("hd,share", [(128, 1), (128, 8), (128, 16), (256, 4), (256, 8)])
+def test_two_tokens_whose_weights_are_close(rp, hd, share, bits, wide):
+    """Keys 0 and -1 in one channel, queries q there: scores 0 and -q exactly but for q' = q log2(e), so w = exp(-q) is all that there
+    is: out = c w / (1 + w) for value codes 0 and c, lse = log(1 + w).
+
+    q' takes three roundings of half a step (the constant log2(e), its product with q, the score's conversion to fp32) and 2^-30 in
+    its fixed point, which move w by a relative 3 U q + 2^-30 q; 2^x has one step (2 U).  A weight above 1/2 has all its bits in
+    the fixed point.  1 + w, the conversion of c w and the quotient round once each.  lse: 1 + w moves by w / (1 + w) of w's error
+    and its own rounding, log2 has one step, ln 2 and the product with it a half each."""
+    k, v = np.zeros((2, hd), np.int64), np.zeros((2, hd), np.int64)
+    k[1, 0] = -1
+    v[1] = 1 + np.arange(hd) % 3
+    plain = records(np.ones(hd), np.zeros(hd))
+    cache = one_page(rp, hd, bits, k, v, plain, plain)
+    rng = np.random.default_rng(hd + share)
+    q = np.zeros((256, share, hd))
+    q[..., 0] = kvo.round_to_bf16(np.exp(rng.uniform(np.log(2.0 ** -7), np.log(0.6), q.shape[:2])).astype(np.float32))
+    out, lse = attend(rp, cache, q, 2, 1.0, wide)
+    x = q[..., 0]
+    w = np.exp(-x)
+    e = (3 * U + 2.0 ** -30) * x + 2 * U
+    want = w / (1 + w)
+    tol = want * (e / (1 + w) + 3 * U) * (1 + 1e-6)
+    off = np.abs(out - want[..., None] * v[1])
+    assert (off <= tol[..., None] * v[1]).all(), (off / (tol[..., None] * v[1])).max()
+    tol = (e * w / (1 + w) + U + 4 * U * np.log1p(w)) * (1 + 1e-6)
+    off = np.abs(lse - np.log1p(w))
+    assert (off <= tol).all(), (off / tol).max()
+
+
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("size", [0.002, 0.05])
 @pytest.mark.parametrize("hd,share,bits", [(128, 1, 4), (128, 12, 8), (256, 4, 3), (256, 8, 8)])
 def test_the_logarithm_of_one_token(rp, hd, share, bits, size, wide):
