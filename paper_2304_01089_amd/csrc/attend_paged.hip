@@ -3,12 +3,15 @@
 // the zero points of the keys add one number to every score of a head, which the softmax does not see (only lse does), and
 // those of the values come off the weighted mean.
 //
-// Both sums run on the int8 matrix cores, exactly.  A query's q' and a tile's weights p are written in fixed point, 31 bits
-// below the head's largest |q'| and 30 below the tile's largest weight, as four signed digits to the base 256; a digit is a
-// row of the matrix product, so four heads fill its 16 rows (one query head on a key/value head uses four of them: rows cost
-// nothing here, the product is bound by the bytes of the cache).  Codes are the other operand as they are stored, one shift
-// and one mask per four of them.  The digits' sums meet again in one lane.  What is rounded: q' once per factor, the sum of a
-// tile of 64 tokens once to fp32.
+// Both sums run on the int8 matrix cores, whose products are exact.  A query's q' and a tile's weights p are written in fixed
+// point, 31 bits below the head's largest |q'| and 30 below the tile's largest weight, as four signed digits to the base 256; a
+// digit is a row of the matrix product, so four heads fill its 16 rows (one query head on a key/value head uses four of them: rows
+// cost nothing here, the product is bound by the bytes of the cache).  Codes are the other operand as they are stored, one shift
+// and one mask per four of them.  The digits' sums meet again in one lane.  What is rounded: q', once per factor and to its fixed
+// point; a score, as its digits' sums become fp32 (the upper half of them and the whole, a half step each); the difference from
+// the largest score and its 2^x (the hardware's, one step); a weight to its fixed point, downwards (a tile loses less than 2^-24 of its
+// sum of weights); the weighted codes of a tile of 64 tokens like a score, then as they are scaled and added in fp32, as the sums of
+// weights are.
 //
 // A workgroup takes a part of one sequence for the heads that read one block of 128 positions (two for heads 256 wide), a
 // wave every fourth tile of 64 tokens: scores, weights and weighted codes of a tile stay in registers, its weights cross 1 KiB of
@@ -16,13 +19,15 @@
 // follows their lengths, which the kernel reads: parts of equal length over the whole batch, as many as fill the chip.  Parts
 // leave (max, sum, weighted codes), a second kernel joins them; sequences of one part are finished at once.
 //
-// What bounds it.  One row tile: memory, 16 x 8192 tokens of 96 x 128 at 3 bits 203 us, 5.95 TB/s; 32 x 4096 of 40 x 128 at 4 bits
-// (half as many on average) 65 us, 5.3 TB/s.  More row tiles: vector instructions, 339 a tile of 4-bit codes with one and 841 with
-// four, of which 56 a row tile bring the digits' sums of 8 x 4 outputs together (16 x 8192 of 8 x 128, half as many on average, by
-// query heads 32, 64, 128: 20, 23, 35 us; memory 14).  Few tokens: a chain of latencies, 7 us for 257 tokens (lengths and page
-// numbers 1.0, keys, values and queries 1.2, a tile 0.9, the waves together and the stores 0.7, the launch the rest), and 4 more for
-// the second launch.  Tried: waves that take a row tile each and share the tokens (16 x 8192 of 64 on 8 27 -> 33 us: four
-// times the loads), a wave by itself per short sequence (512 x 60 19 -> 13 us, but 32 x 1000 9 -> 24: a wave takes 1.1 us a tile).
+// What bounds it.  One row tile: memory, 16 x 8192 tokens of 96 x 128 at 3 bits 196 us, 6.2 TB/s; 32 x 4096 of 40 x 128 at 4
+// bits (half as many on average) 62 us, 5.6 TB/s.  More row tiles: vector instructions, 339 a tile of 4-bit codes with one and
+// 841 with four, of which 56 a row tile bring the digits' sums of 8 x 4 outputs together (16 x 8192 of 8 x 128, half as many on
+// average, by query heads 32, 64, 128: 20, 24, 35 us; memory 14).  With 128 the part kernel takes 29: compute units hold waves
+// for 24 of them, vector instructions issue two thirds of that time, two waves per SIMD that wait for memory or each other a
+// third of theirs.  Few tokens: a chain of latencies, 7 us for 257 tokens (lengths and page numbers 1.0, keys, values and
+// queries 1.2, a tile 0.9, the waves together and the stores 0.7, the launch the rest), and 4 more for the second launch.
+// Tried: waves that take a row tile each and share the tokens (16 x 8192 of 64 on 8 27 -> 33 us: four times the loads), a wave
+// by itself per short sequence (512 x 60 19 -> 13 us, but 32 x 1000 9 -> 24: a wave takes 1.1 us a tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -45,6 +50,7 @@ constexpr int kTile = 64;                      // tokens of a wave's tile
 // 57.5 | 61.9).  Else many, so that a long sequence does not end alone: 2048 with one row tile, half as many where a workgroup
 // takes longer (1024 | 2048: 64 x 16000 of 8 x 128 102 | 95, but 256 x 4000 of 64 on 8 120 | 146), and parts of kShortTiles at least
 // (4 | 16 | 64: 128 x 1000 of 64 on 8, tables for more, 47.9 | 29.5 | 29.4, 32 x 4096 of 40 x 128 65.2 | 65.4 | 70.6).
+// (Counts for the 256 compute units of a whole device; on a part of one they are right, and not measured.)
 constexpr int kFewWorkgroups = 512, kManyWorkgroups = 2048;
 constexpr int kLongTiles = 64;
 constexpr int kShortTiles = 16;
@@ -52,8 +58,10 @@ constexpr int kLeastTiles = 2;                 // of a part of a sequence that i
 constexpr int kWholeTiles = 48;                // of a sequence that is never cut at most (one such among short ones keeps the others waiting)
 constexpr int kMostTiles = 1 << 23;            // of a sequence
 constexpr int kJoinWorkgroups = 2048;          // that join parts, about: more take several heads each (512 x 1500 of 64 on 8 x 128: 136 | 127 us)
-// Bytes of keys and values that a call can reach: beyond the last-level cache's size they are read past it.  us without | with, the same
-// cache again and again: 36 MB 14.6 | 16.2, 100 MB 23.7 | 24.9, 250 MB 47.5 | 50.4, 350 MB 71.6 | 64.2, 1.2 GB 227 | 204 (5.9 TB/s).
+// Bytes of keys and values that a call can reach: beyond the last-level cache's size they are read past it.  (By the pool and the tables:
+// the lengths are not known here, so a short batch on a large pool is read past the cache too and loses what the small sizes below show.)
+// us without | with, the same cache again and again: 36 MB 14.6 | 16.2, 100 MB 23.7 | 24.9, 250 MB 47.5 | 50.4, 350 MB 71.6 | 64.2, 1.2 GB
+// 227 | 204 (5.9 TB/s).
 constexpr int64_t kStreamBytes = 256ll << 20;
 constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
@@ -218,6 +226,8 @@ struct Part {
   int b, len, index, count, first_tile, end_tile;
 };
 
+// Every workgroup adds up all lengths where sequences may be cut: B sequences of up to 300 tokens, half as many on average, 32 on 8 x 128,
+// tables for 300 | 32768 tokens, us: 512 26 | 39, 2048 95 | 222, 8192 367 | 1814.  (Tables no wider than the sequences are not cut.)
 // The part that slot number `slot` holds; false: none.  A sequence's first part is in the slot of its own number, the others,
 // sequence after sequence, in those behind.  own_len: the length of sequence number `slot`; first_len: lane i's is that of sequence
 // i (or the last's), where sequences may be cut.
@@ -676,8 +686,9 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendPl
     auto row_of = [&](int part) { return static_cast<int64_t>(part == 0 ? b : where.x + part - 1) * a.n_q + h; };
     const int per = a.hd / 4, c = tid % per, p0 = tid / per, step = 256 / per;
     const f4* src = reinterpret_cast<const f4*>(buf.acc) + c;
-    // (what a join of up to 8 * step parts reads is requested before anything is waited for: 32768 tokens of 32 on 8 x 128, 64 parts,
-    // 16.0 -> 14.8 us; the second half only where there are so many)
+    // (what a join of up to 8 * step parts reads is requested before anything is waited for, the second half only where there are so
+    // many; four | eight, us in a recorded graph: 32768 tokens of 32 on 8 x 128, 64 parts, 14.5 | 13.4, 16000 of 128 on 8 15.0 | 15.0,
+    // 16 x 8192 of 32 on 8 19.5 | 19.7)
     constexpr int kAhead = 8;
     f4 first[kAhead];
     auto request = [&](int k) { first[k] = src[row_of(min(p0 + k * step, where.y - 1)) * per]; };
