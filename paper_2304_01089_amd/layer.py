@@ -201,6 +201,7 @@ class PagedCache:
     v_pages: object
     k_table: object
     v_table: object
+    _compared = False     # (no field)
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)

@@ -62,3 +62,12 @@ def test_sizes_that_no_cache_has():
         for call in calls(cache(**change)):
             with pytest.raises(rp.RptqError, match="status %d" % status):
                 call()
+
+
+def test_a_cache_whose_fields_came_past_the_constructor_is_looked_at():
+    """(As unpickling and copying bring them.)"""
+    c = rp.PagedCache.__new__(rp.PagedCache)
+    c.__dict__.update({n: v for n, v in cache(page_size=32).__dict__.items() if not n.startswith("_")})
+    for call in calls(c):
+        with pytest.raises(ValueError, match=r"k_pages: expected shape \[pages, 2, 32, 64\]"):
+            call()
