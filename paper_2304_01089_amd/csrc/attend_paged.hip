@@ -32,17 +32,14 @@
 
 #include <algorithm>
 
+#include "attend_common.h"
 #include "device_common.h"
 #include "rptq_internal.h"
 
 namespace rptq {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
-
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.402823466e38f;      // below every score
-constexpr int kTile = 64;                      // tokens of a wave's tile
 // Into how many parts the tokens of a batch are cut, us of 4-bit codes.  Few: two workgroups per compute unit of 256 (one | two: 16 x
 // 8192 of 32 on 8 x 128 22.8 | 19.4, 2 x 20000 of 40 x 128 47.9 | 45.6, 3500 of 96 x 128 at 3 bits 17.3 | 14.9; but 8000 of 32 on 8 9.2 | 10.2;
 // two | four: 16 x 8192 20.2 | 21.9, 32768 of 32 on 8 16.4 | 17.8), if
@@ -63,7 +60,6 @@ constexpr int kJoinWorkgroups = 2048;          // that join parts, about: more t
 // us without | with, the same cache again and again: 36 MB 14.6 | 16.2, 100 MB 23.7 | 24.9, 250 MB 47.5 | 50.4, 350 MB 71.6 | 64.2, 1.2 GB
 // 227 | 204 (5.9 TB/s).
 constexpr int64_t kStreamBytes = 256ll << 20;
-constexpr int kRowHeads = 4;                   // query heads per 16 rows of the matrix product
 
 // Row tiles that a workgroup's registers hold: heads 256 wide take twice as many per row tile.
 __host__ __device__ constexpr int most_row_tiles(int blocks) { return blocks == 2 ? 2 : 4; }
@@ -137,88 +133,6 @@ __device__ __forceinline__ PartBuffers part_buffers(const AttendArgs& a, const A
   b.acc = reinterpret_cast<float*>(b.heads + rows);
   b.where = reinterpret_cast<int2*>(b.acc + rows * a.hd);
   return b;
-}
-
-// ---- lane arithmetic ------------------------------------------------------------------------------------
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_row(uint32_t v) {                // a permutation inside a row of 16 lanes
-  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true));
-}
-template <int CTRL>
-__device__ __forceinline__ float dpp_row(float v) { return __uint_as_float(dpp_row<CTRL>(__float_as_uint(v))); }
-
-__device__ __forceinline__ float row16_max(float v) {
-  v = fmaxf(v, dpp_row<0xB1>(v));
-  v = fmaxf(v, dpp_row<0x4E>(v));
-  v = fmaxf(v, dpp_row<0x141>(v));
-  return fmaxf(v, dpp_row<0x140>(v));
-}
-__device__ __forceinline__ float row16_add(float v) {
-  v += dpp_row<0xB1>(v);
-  v += dpp_row<0x4E>(v);
-  v += dpp_row<0x141>(v);
-  return v + dpp_row<0x140>(v);
-}
-__device__ __forceinline__ float wave_max(float v) {
-  v = row16_max(v);
-  auto row = [&](int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); };
-  return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
-}
-
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_plus(int v) {
-  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int wave_prefix(int v) {                      // inclusive
-  v = dpp_plus<0x111, 0xf>(v);
-  v = dpp_plus<0x112, 0xf>(v);
-  v = dpp_plus<0x114, 0xf>(v);
-  v = dpp_plus<0x118, 0xf>(v);
-  v = dpp_plus<0x142, 0xa>(v);
-  return dpp_plus<0x143, 0xc>(v);
-}
-
-// Four lanes' four bytes transposed: lane i's byte b becomes lane b's byte i.  (Two exchanges, of neighbours and of pairs.)
-struct QuadSel {
-  uint32_t s0, s1;
-};
-__device__ __forceinline__ QuadSel quad_sel(int lane) {
-  return {lane & 1 ? 0x03070105u : 0x06020400u, lane & 2 ? 0x03020706u : 0x05040100u};
-}
-__device__ __forceinline__ uint32_t quad_transpose(uint32_t x, const QuadSel& s) {
-  x = __builtin_amdgcn_perm(dpp_row<0xB1>(x), x, s.s0);
-  return __builtin_amdgcn_perm(dpp_row<0x4E>(x), x, s.s1);
-}
-
-// A number of up to 31 bits as four signed digits to the base 256, lowest in the lowest byte.
-__device__ __forceinline__ uint32_t digits(int v) { return (static_cast<uint32_t>(v) + 0x80808080u) ^ 0x80808080u; }
-
-// The digits' sums, lowest first, as one fp32 number (the products of two digits' sums with the base are exact).
-__device__ __forceinline__ float undigit(const v4i& c) {
-  return fmaf(static_cast<float>(c[3] * 256 + c[2]), 65536.0f, static_cast<float>(c[1] * 256 + c[0]));
-}
-
-// 32 packed codes (of one token; or, after quad_transpose, byte b of four tokens) -> operand bytes code << kShift, codes 4e..4e+3 in w[e]
-template <int BITS>
-__device__ __forceinline__ void expand(const uint32_t (&x)[BITS], uint32_t (&w)[8]) {
-  if constexpr (BITS == 8) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = x[e];
-  } else if constexpr (BITS == 4) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      w[2 * u] = x[u] & 0xf0f0f0f0u;
-      w[2 * u + 1] = (x[u] << 4) & 0xf0f0f0f0u;
-    }
-  } else {
-#pragma unroll
-    for (int u = 0; u < 3; ++u) {
-      w[2 * u] = x[u] & 0xe0e0e0e0u;
-      w[2 * u + 1] = (x[u] << 3) & 0xe0e0e0e0u;
-    }
-    w[6] = ((x[0] << 6) & 0xc0c0c0c0u) | ((x[2] << 5) & 0x20202020u);
-    w[7] = ((x[1] << 6) & 0xc0c0c0c0u) | ((x[2] << 4) & 0x20202020u);
-  }
 }
 
 // ---- which tokens a workgroup takes ------------------------------------------------------------------------
