@@ -477,6 +477,99 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
                           int64_t ld_page_table, int32_t pages_per_seq, const int32_t* lens, void* out, int64_t ld_out,
                           int32_t out_dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- rotary positions, alone and in front of the cache ----------------------------------------
+ * A pair (a, b) of channels of a head at position p turns by theta = p * freqs[j]:
+ *     (a, b)  ->  (c a - s b, c b + s a),   c = amplitude cos(theta), s = amplitude sin(theta)
+ * Pair j, 0 <= j < rotary_dim / 2, is channels (j, j + rotary_dim / 2) of the head, or (2 j, 2 j + 1) with `interleaved`;
+ * the channels from rotary_dim on are not touched.  theta, its cosine and sine and their products with amplitude are
+ * 64-bit numbers, c and s are rounded once to fp32, the two products and their sum to fp32 each.
+ *
+ * rptq_rope_freqs (host): frequencies in radians per position and the amplitude that goes with them.
+ *   RPTQ_ROPE_PLAIN   freqs[j] = base^(-2 j / rotary_dim), amplitude 1
+ *   RPTQ_ROPE_LINEAR  the same divided by `factor`
+ *   RPTQ_ROPE_BASE    the same with base * factor^(rotary_dim / (rotary_dim - 2))  (rotary_dim 2: base * factor^2)
+ *   RPTQ_ROPE_PARTS   f = base^(-2 j / rotary_dim) turns w = f * trained / (2 pi) times over the trained length; with
+ *                     u = (w - slow) / (fast - slow) held in [0, 1]: freqs[j] = u f + (1 - u) f / factor,
+ *                     amplitude = 0.1 log(factor) + 1
+ *   base > 0, factor >= 1; parts: trained > 0, 0 <= slow < fast.   freqs host out [rotary_dim / 2], amplitude host out.
+ *
+ * rptq_rope: rows of n_heads heads rotated, y = x turned.
+ *   x, y    device, RPTQ_DTYPE_BF16 or RPTQ_DTYPE_F32 each (y is rounded once), rows of n_heads * head_dim values, ld_x and
+ *           ld_y apart, on the type's own alignment; they may be columns of wider tensors.  y may be x (same type and stride), and
+ *           may overlap it no other way.
+ *   positions device int32 [T]: any number, also below zero;  freqs device double [rotary_dim / 2], any finite
+ *   rotary_dim even, 2 .. head_dim; head_dim <= RPTQ_MAX_ROTARY_HEAD; n_heads * head_dim <= 2 RPTQ_MAX_CHANNELS
+ *
+ * rptq_rope_quant_paged: one launch for a step's queries, keys and values.  Queries are rotated as by rptq_rope (bf16 in and
+ * out; q and q_out NULL: none).  Row t's key is rotated, and as fp32 quantized as by rptq_kv_quant_paged into slot slots[t]; its
+ * value is quantized into the same slot as it is.  (A key that rptq_rope has rounded to bf16 first may get neighbouring codes.)
+ *   rows as for rptq_rope and rptq_kv_quant_paged: strides multiples of 8, pointers on 16 bytes; head_dim 32, 64, 128 or 256,
+ *   rotary_dim a multiple of 16; n_q_heads * head_dim <= RPTQ_MAX_CHANNELS; q_out may be q.  A row whose slot is none has its
+ *   query rotated all the same.
+ *
+ * Both are asynchronous on `stream` and allocate nothing; rptq_rope needs no call before it is recorded into a graph,
+ * rptq_rope_quant_paged the first one on the device.
+ */
+#define RPTQ_MAX_ROTARY_HEAD 1024
+enum { RPTQ_ROPE_PLAIN = 0, RPTQ_ROPE_LINEAR = 1, RPTQ_ROPE_BASE = 2, RPTQ_ROPE_PARTS = 3 };
+int32_t rptq_rope_freqs(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double slow, double fast,
+                        double* freqs, double* amplitude);
+int32_t rptq_rope(const void* x, int32_t x_dtype, int64_t ld_x, void* y, int32_t y_dtype, int64_t ld_y, const int32_t* positions,
+                  int64_t T, int32_t n_heads, int32_t head_dim, int32_t rotary_dim, int32_t interleaved, const double* freqs,
+                  double amplitude, void* stream);
+int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t ld_q_out, int32_t n_q_heads, const void* k, int64_t ld_k,
+                              const void* v, int64_t ld_v, int64_t T, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions,
+                              int32_t rotary_dim, int32_t interleaved, const double* freqs, double amplitude, const void* k_table,
+                              const void* v_table, int32_t bits, const int64_t* slots, void* k_pages, void* v_pages, int64_t n_pages,
+                              int32_t page_size, void* stream);
+
+/* ---- bounding the cache by accumulated attention weight ----------------------------------------
+ * A program that drops tokens keeps a record of every token of every key/value head: weights, fp32 [B, n_kv_heads, capacity], what
+ * the token got of the attention so far, and token_positions, int32 of the same shape, where in the text it stands.  Entry
+ * [b, h, t] belongs to token t of sequence b as the page table numbers them.  Both contiguous; entries behind the
+ * sequence's length are neither read nor written.  A sequence has min(lens[b], pages_per_seq * page_size, capacity) tokens.
+ *
+ * rptq_attend_weights_paged: the last `queries` tokens of every sequence have attended to the cache (rptq_attend_paged, one row
+ * each); with a_git query head g's score of token t for query i and lse_gi what that call left,
+ *     weights[b, h, t] += sum_i sum_{g of h} exp(a_git - lse_gi)
+ * over the queries that see token t: query i of n sees t < lens[b] - (n - 1 - i), and no token whose page is not there.
+ * The newest `fresh` tokens start here: their weight is set to that sum instead, and their position to
+ * positions[b] - (lens[b] - 1 - t), positions[b] being the newest token's, or to t where positions is NULL.
+ *   q       device bf16 [B * queries, n_q_heads * head_dim], rows ld_q apart, sequence after sequence, oldest query first
+ *   lse     device fp32 [B * queries, n_q_heads];  positions device int32 [B] or NULL
+ *   1 <= queries <= RPTQ_MAX_WINDOW; fresh >= 0; the others as for rptq_attend_paged.  Sums are fp32, in an order that the call alone
+ *   decides.  A NaN or infinity in q makes the weights of the tokens that it sees NaN.  Sequences that share pages keep records of their own.
+ *
+ * rptq_evict_paged: every key/value head of every sequence of more than `budget` tokens keeps `budget` of them: those at positions
+ * below `first`, those at positions beyond the head's largest minus `recent`, then those of the largest weight, equal ones
+ * from token 0 on (a NaN counts as larger than any other weight; should those at safe positions alone be more than the
+ * budget, the ones of the lowest t stay).  Of the kept tokens those with t >= budget move, in their order, to the
+ * t < budget that are not kept: the head's codes in both tensors' pages, and the record.  lens_out[b] = budget; the heads of a
+ * sequence may keep different tokens.  A sequence of no more tokens, or one of whose tokens' pages is not there, stays as it is,
+ * lens_out[b] its number of tokens.  Attention over the result is attention over the kept tokens.
+ *   weights_out, token_positions_out  the records of lens_out[b] tokens; may be weights and token_positions, and overlap them no other way
+ *   lens_out  device int32 [B], must not be lens
+ *   workspace device, rptq_evict_paged_workspace_bytes(B, n_kv_heads, capacity, budget) bytes, nothing to clear or keep
+ *   budget >= 1; first, recent >= 0, first + recent <= budget; B * n_kv_heads <= RPTQ_MAX_TRACKED_HEADS
+ * No page may belong to two sequences of the call, nor to one that lives on elsewhere: rows move in place.
+ *
+ * Both are asynchronous on `stream`, allocate nothing and may be recorded into a graph without a call before.
+ * 1 <= capacity <= 2^29.
+ */
+#define RPTQ_MAX_WINDOW 65536
+#define RPTQ_MAX_TRACKED_HEADS 2097152
+int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t head_dim, float scale, const void* k_table, int32_t bits, const void* k_pages,
+                                  int64_t n_pages, int32_t page_size, const int32_t* page_table, int64_t ld_page_table,
+                                  int32_t pages_per_seq, const int32_t* lens, const float* lse, const int32_t* positions, int32_t fresh,
+                                  float* weights, int32_t* token_positions, int64_t capacity, void* stream);
+size_t rptq_evict_paged_workspace_bytes(int32_t B, int32_t n_kv_heads, int64_t capacity, int32_t budget);
+int32_t rptq_evict_paged(int32_t B, int32_t n_kv_heads, int32_t head_dim, int32_t bits, void* k_pages, void* v_pages, int64_t n_pages,
+                         int32_t page_size, const int32_t* page_table, int64_t ld_page_table, int32_t pages_per_seq,
+                         const int32_t* lens, const float* weights, const int32_t* token_positions, int64_t capacity, int32_t budget,
+                         int32_t first, int32_t recent, float* weights_out, int32_t* token_positions_out, int32_t* lens_out,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- helpers for verification (not on the timed path) ---------------------------- */
 
 /* The literal per-cluster integers Yq_i of App. A.4 from the same MFMA main loop:

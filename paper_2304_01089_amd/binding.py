@@ -14,6 +14,7 @@ import numpy as np
 
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
+ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 EXPORTED_SYMBOLS = (
     "rptq_padded_k", "rptq_codes_bytes", "rptq_weight_bytes", "rptq_calibrate_workspace_bytes",
@@ -25,7 +26,8 @@ EXPORTED_SYMBOLS = (
     "rptq_cluster_gemm_cw", "rptq_cluster_gemm_partials_cw",
     "rptq_cluster_channels", "rptq_cluster_heads", "rptq_kv_table_bytes", "rptq_kv_tables", "rptq_kv_quant",
     "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
-    "rptq_attend_paged_workspace_bytes", "rptq_attend_paged", "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
+    "rptq_attend_paged_workspace_bytes", "rptq_attend_paged", "rptq_rope_freqs", "rptq_rope", "rptq_rope_quant_paged",
+    "rptq_attend_weights_paged", "rptq_evict_paged_workspace_bytes", "rptq_evict_paged", "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
 )
 
 _LIB = None
@@ -63,7 +65,7 @@ def load_library():
     if not os.path.exists(path):
         raise RuntimeError("librptq.so is not built (%s): run `python -m paper_2304_01089_amd.build`" % path)
     lib = C.CDLL(path)
-    vp, i32, i64, u64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
+    vp, i32, i64, u64, f32, f64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_double, C.c_size_t
     sig = {
         "rptq_padded_k": (i32, [vp, i32, vp]),
         "rptq_codes_bytes": (sz, [i64, i32, i32]),
@@ -108,6 +110,15 @@ def load_library():
         "rptq_attend_paged_workspace_bytes": (sz, [i32, i32, i32, i32]),
         "rptq_attend_paged": (i32, [vp, i64, i32, i32, i32, i32, f32, vp, vp, i32, vp, vp, i64, i32, vp, i64, i32, vp, vp, i64,
                                     i32, vp, vp, sz, vp]),
+        "rptq_rope_freqs": (i32, [i32, f64, i32, f64, f64, f64, f64, vp, vp]),
+        "rptq_rope": (i32, [vp, i32, i64, vp, i32, i64, vp, i64, i32, i32, i32, i32, vp, f64, vp]),
+        "rptq_rope_quant_paged": (i32, [vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, i32, i32, vp, i32, i32, vp, f64, vp, vp, i32, vp,
+                                        vp, vp, i64, i32, vp]),
+        "rptq_attend_weights_paged": (i32, [vp, i64, i32, i32, i32, i32, i32, f32, vp, i32, vp, i64, i32, vp, i64, i32, vp, vp, vp, i32,
+                                            vp, vp, i64, vp]),
+        "rptq_evict_paged_workspace_bytes": (sz, [i32, i32, i64, i32]),
+        "rptq_evict_paged": (i32, [i32, i32, i32, i32, vp, vp, i64, i32, vp, i64, i32, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp,
+                                   sz, vp]),
         "rptq_device_info": (i32, [vp, vp, vp, vp]),
         "rptq_strerror": (C.c_char_p, [i32]),
         "rptq_last_hip_error": (i32, []),
@@ -132,13 +143,13 @@ def _set_up_calls(lib):
         import torch
         from . import _calls
         objects = dict(bfloat16=torch.bfloat16, float32=torch.float32, int32=torch.int32, int64=torch.int64,
-                       uint8=torch.uint8, get_device=torch._C._cuda_getDevice,
+                       uint8=torch.uint8, float64=torch.float64, get_device=torch._C._cuda_getDevice,
                        get_stream=torch._C._cuda_getCurrentRawStream)
     except (ImportError, AttributeError):
         return
     names = ("rptq_ln_quant", "rptq_cluster_gemm", "rptq_cluster_gemm_quant", "rptq_cluster_rowsums", "rptq_cluster_gemm_cw",
              "rptq_kv_quant", "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
-             "rptq_attend_paged")
+             "rptq_attend_paged", "rptq_rope", "rptq_rope_quant_paged", "rptq_attend_weights_paged", "rptq_evict_paged")
     _calls.setup({n: C.cast(getattr(lib, n), C.c_void_p).value for n in names}, objects)
     _CALLS = _calls
 
@@ -733,6 +744,155 @@ def rptq_attend_paged(q, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: 
             _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
             workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_paged")
+
+
+# ---- rotary positions, alone and in front of the cache --------------------------------------------------
+def _float_type(t, what: str):
+    import torch
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    raise ValueError("%s must be bf16 or fp32" % what)
+
+
+def _frequencies(freqs, rotary_dim: int):
+    import torch
+    if freqs.dim() != 1 or 2 * freqs.shape[0] != rotary_dim:
+        raise ValueError("freqs: expected %d, one per pair" % (rotary_dim // 2))
+    return _whole(freqs, torch.float64, "freqs", 0)
+
+
+def _row_positions(positions, T: int):
+    import torch
+    if positions.dim() != 1 or positions.shape[0] != T:
+        raise ValueError("positions: expected one per row")
+    return _whole(positions, torch.int32, "positions", 0)
+
+
+def rptq_rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, trained: float = 0.0,
+                    slow: float = 1.0, fast: float = 32.0):
+    """(float64 array of rotary_dim / 2 frequencies, amplitude).  scaling: None, "linear", "base" or "parts"."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling: expected one of %s, got %r" % (list(ROPE_SCALINGS), scaling))
+    freqs, amplitude = np.zeros(max(1, rotary_dim // 2), np.float64), C.c_double()
+    st = load_library().rptq_rope_freqs(rotary_dim, base, ROPE_SCALINGS[scaling], factor, trained, slow, fast,
+                                        freqs.ctypes.data_as(C.c_void_p), C.byref(amplitude))
+    _check(st, "rptq_rope_freqs")
+    return freqs, amplitude.value
+
+
+def rptq_rope(x, y, positions, head_dim: int, rotary_dim: int, interleaved: bool, freqs, amplitude: float, stream=None):
+    """x, y: bf16 or fp32 [T, n_heads * head_dim], rows of any stride (y may be x); positions: int32 [T]; freqs: float64."""
+    st = None if _CALLS is None else _CALLS.rope(x, y, positions, head_dim, rotary_dim, interleaved, freqs, amplitude, stream)
+    if st is None:
+        if x.dim() != 2 or head_dim < 1 or x.shape[1] % head_dim != 0:
+            raise ValueError("x: expected [T, n_heads * %d]" % head_dim)
+        (xa, ld_x), (ya, ld_y) = _matrix(x, None, "x", x.shape), _matrix(y, None, "y", x.shape)
+        st = load_library().rptq_rope(xa, _float_type(x, "x"), ld_x, ya, _float_type(y, "y"), ld_y, _row_positions(positions, x.shape[0]),
+                                      x.shape[0], x.shape[1] // head_dim, head_dim, rotary_dim, int(interleaved),
+                                      _frequencies(freqs, rotary_dim), amplitude, _stream(stream)) if x.shape[0] else 0
+    _check(st, "rptq_rope")
+
+
+def rptq_rope_quant_paged(q, q_out, k, v, positions, slots, head_dim: int, rotary_dim: int, interleaved: bool, freqs, amplitude: float,
+                          k_table, v_table, bits: int, k_pages, v_pages, page_size: int, stream=None):
+    """q, q_out: bf16 [T, n_q_heads * head_dim] or both None; the others as for rptq_rope and rptq_kv_quant_paged."""
+    st = None if _CALLS is None else _CALLS.rope_quant_paged(
+        q, q_out, k, v, positions, slots, head_dim, rotary_dim, interleaved, freqs, amplitude, k_table, v_table, bits, k_pages, v_pages,
+        page_size, stream)
+    if st is None:
+        import torch
+        T, d = _tokens(k, v, slots)
+        if head_dim < 1 or d % head_dim != 0:
+            raise ValueError("k and v: expected [T, n_kv_heads * %d]" % head_dim)
+        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+        (qa, ld_q), (oa, ld_out), n_q = (None, 0), (None, 0), 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out: expected both or none")
+        if q is not None:
+            if q.dim() != 2 or q.shape[1] % head_dim != 0:
+                raise ValueError("q: expected [T, n_q_heads * %d]" % head_dim)
+            n_q = q.shape[1] // head_dim
+            qa, ld_q = _matrix(q, torch.bfloat16, "q", (T, n_q * head_dim))
+            oa, ld_out = _matrix(q_out, torch.bfloat16, "q_out", (T, n_q * head_dim))
+        st = load_library().rptq_rope_quant_paged(
+            qa, ld_q, oa, ld_out, n_q, ka, ld_k, va, ld_v, T, d // head_dim, head_dim, _row_positions(positions, T), rotary_dim,
+            int(interleaved), _frequencies(freqs, rotary_dim), amplitude, _position_table(k_table, "k_table", d),
+            _position_table(v_table, "v_table", d), bits, _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size,
+            _stream(stream)) if T else 0
+    _check(st, "rptq_rope_quant_paged")
+
+
+# ---- bounding the cache by accumulated attention weight -------------------------------------------------
+def _records(weights, token_positions, B: int, n_kv_heads: int, what: str = ""):
+    """(addresses of both tensors of a record of every token, capacity)."""
+    import torch
+    shape = tuple(weights.shape)
+    if len(shape) != 3 or shape[:2] != (B, n_kv_heads) or tuple(token_positions.shape) != shape:
+        raise ValueError("%sweights and positions: expected two tensors [%d, %d, capacity]" % (what, B, n_kv_heads))
+    return (_whole(weights, torch.float32, what + "weights", 0), _whole(token_positions, torch.int32, what + "positions", 0), shape[2])
+
+
+def _sequences(page_table, lens):
+    """(address, stride, pages of a sequence, address of lens, sequences)."""
+    import torch
+    if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != page_table.shape[0]:
+        raise ValueError("expected page_table [B, pages] and lens [B]")
+    at, ld = _matrix(page_table, torch.int32, "page_table", page_table.shape)
+    return at, ld, page_table.shape[1], _whole(lens, torch.int32, "lens", 0), lens.shape[0]
+
+
+def rptq_attend_weights_paged(q, queries: int, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, k_table, bits: int, k_pages,
+                              page_size: int, page_table, lens, lse, positions, fresh: int, weights, token_positions, stream=None):
+    """q: bf16 [B * queries, n_q_heads * head_dim], rows of any stride; lse: fp32 [B * queries, n_q_heads]; positions: int32 [B] or
+    None; weights, token_positions: fp32 and int32 [B, n_kv_heads, capacity]."""
+    st = None if _CALLS is None else _CALLS.attend_weights_paged(
+        q, queries, n_q_heads, n_kv_heads, head_dim, scale, k_table, bits, k_pages, page_size, page_table, lens, lse, positions, fresh,
+        weights, token_positions, stream)
+    if st is None:
+        import torch
+        d = n_kv_heads * head_dim
+        pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
+        kp, _, n_pages = _pages(k_pages, k_pages, d, page_size, bits)
+        qa, ld_q = _matrix(q, torch.bfloat16, "q", (B * queries, n_q_heads * head_dim))
+        if tuple(lse.shape) != (B * queries, n_q_heads):
+            raise ValueError("lse: expected shape %s, got %s" % ((B * queries, n_q_heads), tuple(lse.shape)))
+        wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
+        st = load_library().rptq_attend_weights_paged(
+            qa, ld_q, B, queries, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d), bits, kp, n_pages,
+            page_size, pa, ld_pt, per_seq, la, _whole(lse, torch.float32, "lse", 0),
+            None if positions is None else _row_positions(positions, B), fresh, wa, ta, capacity, _stream(stream)) if B else 0
+    _check(st, "rptq_attend_weights_paged")
+
+
+def rptq_evict_paged_workspace_bytes(B: int, n_kv_heads: int, capacity: int, budget: int) -> int:
+    return int(load_library().rptq_evict_paged_workspace_bytes(B, n_kv_heads, capacity, budget))
+
+
+def rptq_evict_paged(n_kv_heads: int, head_dim: int, bits: int, k_pages, v_pages, page_size: int, page_table, lens, weights,
+                     token_positions, budget: int, first: int, recent: int, weights_out, token_positions_out, lens_out, workspace,
+                     stream=None):
+    """weights, token_positions and their outputs: fp32 and int32 [B, n_kv_heads, capacity]; lens_out: int32 [B], not lens."""
+    st = None if _CALLS is None else _CALLS.evict_paged(
+        n_kv_heads, head_dim, bits, k_pages, v_pages, page_size, page_table, lens, weights, token_positions, budget, first, recent,
+        weights_out, token_positions_out, lens_out, workspace, stream)
+    if st is None:
+        import torch
+        pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
+        kp, vp, n_pages = _pages(k_pages, v_pages, n_kv_heads * head_dim, page_size, bits)
+        wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
+        wo, to, cap_out = _records(weights_out, token_positions_out, B, n_kv_heads, "the new ")
+        if cap_out != capacity:
+            raise ValueError("the new weights and positions: expected the old ones' shape")
+        if lens_out.dim() != 1 or lens_out.shape[0] != B:
+            raise ValueError("lens_out: expected one per sequence")
+        st = load_library().rptq_evict_paged(
+            B, n_kv_heads, head_dim, bits, kp, vp, n_pages, page_size, pa, ld_pt, per_seq, la, wa, ta, capacity, budget, first, recent,
+            wo, to, _whole(lens_out, torch.int32, "lens_out", 0), _whole(workspace, None, "workspace", 0),
+            workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+    _check(st, "rptq_evict_paged")
 
 
 def rptq_unpack_codes(codes_packed, rows: int, cluster_off, bits: int, out, stream=None):

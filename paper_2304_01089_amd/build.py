@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librptq.so")
 # the binding's native argument marshalling (csrc/calls.cpp); the suffix keeps other interpreters from loading it
 CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["host.cpp", "api.cpp", "calib_minmax.hip", "fold.hip", "ln_quant.hip", "ln_rows.hip", "gemm.hip", "gemm_small.hip", "kv_cache.hip", "kv_paged.hip", "attend_paged.hip", "ln_scatter.hip", "method1.hip"]
+SOURCES = ["host.cpp", "api.cpp", "calib_minmax.hip", "fold.hip", "ln_quant.hip", "ln_rows.hip", "gemm.hip", "gemm_small.hip", "kv_cache.hip", "kv_paged.hip", "attend_paged.hip", "attend_weights.hip", "evict_paged.hip", "rope.hip", "kv_rope.hip", "ln_scatter.hip", "method1.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-ffp-contract=off",

@@ -447,6 +447,179 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
   return launch_attend_paged(a, bits, out_dtype, static_cast<hipStream_t>(stream));
 }
 
+// ---- rotary positions -------------------------------------------------------------------------------
+static bool rotary_ok(int32_t rotary_dim, int32_t head_dim) { return rotary_dim >= 2 && rotary_dim % 2 == 0 && rotary_dim <= head_dim; }
+
+static bool rows_ok(int64_t T) { return T >= 0 && T <= (INT64_C(1) << 40); }
+
+int32_t rptq_rope_freqs(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double slow, double fast,
+                        double* freqs, double* amplitude) {
+  if (!freqs || !amplitude) return RPTQ_ERR_NULL;
+  if (!rotary_ok(rotary_dim, RPTQ_MAX_ROTARY_HEAD) || scaling < RPTQ_ROPE_PLAIN || scaling > RPTQ_ROPE_PARTS) return RPTQ_ERR_SHAPE;
+  const bool scaled = scaling != RPTQ_ROPE_PLAIN, parts = scaling == RPTQ_ROPE_PARTS;
+  if (!std::isfinite(base) || !(base > 0.0) || (scaled && !(std::isfinite(factor) && factor >= 1.0))) return RPTQ_ERR_RANGE;
+  if (parts && !(std::isfinite(trained) && trained > 0.0 && slow >= 0.0 && slow < fast && std::isfinite(fast))) return RPTQ_ERR_RANGE;
+  const double used = scaling == RPTQ_ROPE_BASE ? base * std::pow(factor, rotary_dim > 2 ? rotary_dim / (rotary_dim - 2.0) : 2.0) : base;
+  if (!std::isfinite(used)) return RPTQ_ERR_RANGE;
+  for (int32_t j = 0; j < rotary_dim / 2; ++j) {
+    const double f = std::pow(used, -2.0 * j / rotary_dim);
+    const double turns = f * trained / 6.283185307179586477, keep = parts ? std::fmin(1.0, std::fmax(0.0, (turns - slow) / (fast - slow))) : 0.0;
+    freqs[j] = !scaled || scaling == RPTQ_ROPE_BASE ? f : f * keep + f / factor * (1.0 - keep);
+  }
+  *amplitude = parts ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return RPTQ_OK;
+}
+
+int32_t rptq_rope(const void* x, int32_t x_dtype, int64_t ld_x, void* y, int32_t y_dtype, int64_t ld_y, const int32_t* positions,
+                  int64_t T, int32_t n_heads, int32_t head_dim, int32_t rotary_dim, int32_t interleaved, const double* freqs,
+                  double amplitude, void* stream) {
+  if (!x || !y || !positions || !freqs) return RPTQ_ERR_NULL;
+  for (int32_t t : {x_dtype, y_dtype})
+    if (t != RPTQ_DTYPE_BF16 && t != RPTQ_DTYPE_F32) return RPTQ_ERR_SHAPE;
+  if (!rows_ok(T) || n_heads < 1 || head_dim < 2 || head_dim > RPTQ_MAX_ROTARY_HEAD || !rotary_ok(rotary_dim, head_dim)) return RPTQ_ERR_SHAPE;
+  const int64_t row = static_cast<int64_t>(n_heads) * head_dim;
+  if (row > 2 * RPTQ_MAX_CHANNELS || ld_x < row || ld_y < row) return RPTQ_ERR_SHAPE;
+  if (x == y && (x_dtype != y_dtype || ld_x != ld_y)) return RPTQ_ERR_SHAPE;
+  if (!std::isfinite(amplitude)) return RPTQ_ERR_RANGE;
+  if (!aligned_to(x, x_dtype == RPTQ_DTYPE_F32 ? 4 : 2) || !aligned_to(y, y_dtype == RPTQ_DTYPE_F32 ? 4 : 2) || !aligned_to(positions, 4) ||
+      !aligned_to(freqs, 8))
+    return RPTQ_ERR_ALIGN;
+  const RopeArgs a{x, ld_x, y, ld_y, positions, T, x_dtype, y_dtype, n_heads, head_dim, rotary_dim, interleaved, freqs, amplitude};
+  return launch_rope(a, static_cast<hipStream_t>(stream));
+}
+
+int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t ld_q_out, int32_t n_q_heads, const void* k, int64_t ld_k,
+                              const void* v, int64_t ld_v, int64_t T, int32_t n_kv_heads, int32_t head_dim, const int32_t* positions,
+                              int32_t rotary_dim, int32_t interleaved, const double* freqs, double amplitude, const void* k_table,
+                              const void* v_table, int32_t bits, const int64_t* slots, void* k_pages, void* v_pages, int64_t n_pages,
+                              int32_t page_size, void* stream) {
+  if (!positions || !freqs || !q != !q_out) return RPTQ_ERR_NULL;
+  PagedGeom g;
+  const int64_t d = static_cast<int64_t>(n_kv_heads) * head_dim;
+  if (int32_t st = check_bits(bits)) return st;
+  if ((head_dim != 32 && head_dim != 64 && head_dim != 128 && head_dim != 256) || n_kv_heads < 1 || d > RPTQ_MAX_CHANNELS) return RPTQ_ERR_SHAPE;
+  if (int32_t st = check_kv_paged(k, ld_k, v, ld_v, T, static_cast<int32_t>(d), k_table, v_table, bits, slots, k_pages, v_pages, n_pages,
+                                  page_size, &g))
+    return st;
+  if (!rotary_ok(rotary_dim, head_dim) || rotary_dim % 16 != 0) return RPTQ_ERR_SHAPE;
+  if (!std::isfinite(amplitude)) return RPTQ_ERR_RANGE;
+  if (!aligned_to(positions, 4) || !aligned_to(freqs, 8)) return RPTQ_ERR_ALIGN;
+  const RopeArgs ka{k, ld_k, nullptr, 0, positions, T, RPTQ_DTYPE_BF16, RPTQ_DTYPE_BF16, n_kv_heads, head_dim, rotary_dim, interleaved, freqs, amplitude};
+  RopeArgs qa = ka;
+  if (q) {
+    const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
+    if (n_q_heads < 1 || row > RPTQ_MAX_CHANNELS || !row_stride_ok(ld_q, row) || !row_stride_ok(ld_q_out, row)) return RPTQ_ERR_SHAPE;
+    if (q == q_out && ld_q != ld_q_out) return RPTQ_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(q_out)) return RPTQ_ERR_ALIGN;
+    qa.x = q, qa.ld_x = ld_q, qa.y = q_out, qa.ld_y = ld_q_out, qa.n_heads = n_q_heads;
+  }
+  const PagedTensor kt{static_cast<const KvPos*>(k_table), static_cast<uint8_t*>(k_pages),
+                       const_cast<uint16_t*>(static_cast<const uint16_t*>(k)), ld_k};
+  const PagedTensor vt{static_cast<const KvPos*>(v_table), static_cast<uint8_t*>(v_pages),
+                       const_cast<uint16_t*>(static_cast<const uint16_t*>(v)), ld_v};
+  return launch_rope_quant_paged(q ? &qa : nullptr, ka, kt, vt, slots, g, bits, static_cast<hipStream_t>(stream));
+}
+
+// ---- bounding the cache by accumulated attention weight -----------------------------------------------
+static bool capacity_ok(int64_t capacity) { return capacity >= 1 && capacity <= (INT64_C(1) << 29); }
+
+static bool page_table_ok(int32_t pages_per_seq, int64_t ld_page_table, int32_t page_size) {
+  return pages_per_seq >= 1 && ld_page_table >= pages_per_seq && static_cast<int64_t>(pages_per_seq) * page_size <= (INT64_C(1) << 29);
+}
+
+int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t head_dim, float scale, const void* k_table, int32_t bits, const void* k_pages,
+                                  int64_t n_pages, int32_t page_size, const int32_t* page_table, int64_t ld_page_table,
+                                  int32_t pages_per_seq, const int32_t* lens, const float* lse, const int32_t* positions, int32_t fresh,
+                                  float* weights, int32_t* token_positions, int64_t capacity, void* stream) {
+  if (!q || !k_table || !k_pages || !page_table || !lens || !lse || !weights || !token_positions) return RPTQ_ERR_NULL;
+  if (int32_t st = check_bits(bits)) return st;
+  if (!attend_heads_ok(B, n_q_heads, n_kv_heads, head_dim)) return RPTQ_ERR_SHAPE;
+  WeightArgs a;
+  if (int32_t st = check_paged(static_cast<int64_t>(n_kv_heads) * head_dim, n_pages, page_size, bits, &a.g)) return st;
+  if (!row_stride_ok(ld_q, static_cast<int64_t>(n_q_heads) * head_dim) || !page_table_ok(pages_per_seq, ld_page_table, page_size) ||
+      !capacity_ok(capacity) || queries < 1 || queries > RPTQ_MAX_WINDOW || fresh < 0)
+    return RPTQ_ERR_SHAPE;
+  if (!std::isfinite(scale)) return RPTQ_ERR_RANGE;
+  if (!aligned16(q) || !aligned16(k_table) || !aligned16(k_pages) || !aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_to(lse, 4) ||
+      !aligned_to(positions, 4) || !aligned_to(weights, 4) || !aligned_to(token_positions, 4))
+    return RPTQ_ERR_ALIGN;
+  a.q = static_cast<const uint16_t*>(q);
+  a.ld_q = ld_q;
+  a.B = B;
+  a.queries = queries;
+  a.n_q = n_q_heads;
+  a.n_kv = n_kv_heads;
+  a.hd = head_dim;
+  a.scale = scale;
+  a.k_pos = static_cast<const KvPos*>(k_table);
+  a.k_pages = static_cast<const uint8_t*>(k_pages);
+  a.page_table = page_table;
+  a.ld_pt = ld_page_table;
+  a.pages_per_seq = pages_per_seq;
+  a.lens = lens;
+  a.lse = lse;
+  a.positions = positions;
+  a.fresh = fresh;
+  a.weights = weights;
+  a.token_positions = token_positions;
+  a.capacity = capacity;
+  return launch_attend_weights(a, bits, static_cast<hipStream_t>(stream));
+}
+
+static bool tracked_ok(int32_t B, int32_t n_kv, int64_t capacity, int32_t budget) {
+  return B >= 0 && B <= RPTQ_MAX_SEQUENCES && n_kv >= 1 && static_cast<int64_t>(B) * n_kv <= RPTQ_MAX_TRACKED_HEADS &&
+         capacity_ok(capacity) && budget >= 1;
+}
+
+size_t rptq_evict_paged_workspace_bytes(int32_t B, int32_t n_kv_heads, int64_t capacity, int32_t budget) {
+  if (!tracked_ok(B, n_kv_heads, capacity, budget)) return 0;
+  return evict_workspace_bytes(B, n_kv_heads, capacity, budget);
+}
+
+int32_t rptq_evict_paged(int32_t B, int32_t n_kv_heads, int32_t head_dim, int32_t bits, void* k_pages, void* v_pages, int64_t n_pages,
+                         int32_t page_size, const int32_t* page_table, int64_t ld_page_table, int32_t pages_per_seq,
+                         const int32_t* lens, const float* weights, const int32_t* token_positions, int64_t capacity, int32_t budget,
+                         int32_t first, int32_t recent, float* weights_out, int32_t* token_positions_out, int32_t* lens_out,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (!k_pages || !v_pages || !page_table || !lens || !weights || !token_positions || !weights_out || !token_positions_out || !lens_out || !workspace)
+    return RPTQ_ERR_NULL;
+  if (int32_t st = check_bits(bits)) return st;
+  if (!attend_heads_ok(B, n_kv_heads, n_kv_heads, head_dim) || !tracked_ok(B, n_kv_heads, capacity, budget)) return RPTQ_ERR_SHAPE;
+  EvictArgs a;
+  if (int32_t st = check_paged(static_cast<int64_t>(n_kv_heads) * head_dim, n_pages, page_size, bits, &a.g)) return st;
+  if (!page_table_ok(pages_per_seq, ld_page_table, page_size) || first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > budget)
+    return RPTQ_ERR_SHAPE;
+  if (lens_out == lens || k_pages == v_pages) return RPTQ_ERR_SHAPE;
+  if (workspace_bytes < evict_workspace_bytes(B, n_kv_heads, capacity, budget)) return RPTQ_ERR_WORKSPACE;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(workspace)) return RPTQ_ERR_ALIGN;
+  for (const void* p : {static_cast<const void*>(page_table), static_cast<const void*>(lens), static_cast<const void*>(weights),
+                        static_cast<const void*>(token_positions), static_cast<const void*>(weights_out),
+                        static_cast<const void*>(token_positions_out), static_cast<const void*>(lens_out)})
+    if (!aligned_to(p, 4)) return RPTQ_ERR_ALIGN;
+  a.B = B;
+  a.n_kv = n_kv_heads;
+  a.hd = head_dim;
+  a.bits = bits;
+  a.k_pages = static_cast<uint8_t*>(k_pages);
+  a.v_pages = static_cast<uint8_t*>(v_pages);
+  a.page_table = page_table;
+  a.ld_pt = ld_page_table;
+  a.pages_per_seq = pages_per_seq;
+  a.lens = lens;
+  a.weights = weights;
+  a.positions = token_positions;
+  a.capacity = capacity;
+  a.budget = budget;
+  a.first = first;
+  a.recent = recent;
+  a.weights_out = weights_out;
+  a.positions_out = token_positions_out;
+  a.lens_out = lens_out;
+  a.workspace = workspace;
+  return launch_evict_paged(a, static_cast<hipStream_t>(stream));
+}
+
 int32_t rptq_cluster_gemm_partials(const void* codes_packed, int64_t M, int32_t bits,
                                    const void* Wq_packed, int32_t N, const int32_t* cluster_off, int32_t g,
                                    const int32_t* zX, const int32_t* zW, const int32_t* xsum,

@@ -25,9 +25,13 @@ decltype(&rptq_kv_page_bytes) f_kv_page_bytes;
 decltype(&rptq_kv_quant_paged) f_kv_quant_paged;
 decltype(&rptq_kv_dequant_paged) f_kv_dequant_paged;
 decltype(&rptq_attend_paged) f_attend_paged;
+decltype(&rptq_rope) f_rope;
+decltype(&rptq_rope_quant_paged) f_rope_quant_paged;
+decltype(&rptq_attend_weights_paged) f_attend_weights_paged;
+decltype(&rptq_evict_paged) f_evict_paged;
 
 PyObject *n_is_cuda, *n_is_contiguous, *n_dtype, *n_data_ptr, *n_nbytes, *n_get_device, *n_shape, *n_stride;     // attribute names
-PyObject *t_bf16, *t_f32, *t_i32, *t_i64, *t_u8, *get_device, *get_stream;         // torch's objects
+PyObject *t_bf16, *t_f32, *t_i32, *t_i64, *t_u8, *t_f64, *get_device, *get_stream;         // torch's objects
 
 // Each getter returns false, with no Python error set, where the ordinary case does not apply.
 bool no_error() {
@@ -406,6 +410,140 @@ PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+bool get_f64(PyObject* o, double* out) {
+  if (!PyFloat_Check(o)) return false;
+  *out = PyFloat_AS_DOUBLE(o);
+  return true;
+}
+
+// A contiguous tensor with one entry of that type per row.
+template <typename T>
+bool get_column(PyObject* t, PyObject* dtype, int64_t device, int64_t rows, T** out) {
+  int64_t bytes, size;
+  return get_whole(t, dtype, device, out, &bytes) && get_sizes(PyObject_GetAttr(t, n_shape), 1, &size) && size == rows;
+}
+
+// The arguments of a rotation: (head_dim, rotary_dim, interleaved, freqs, amplitude).
+struct Turn {
+  int32_t hd, rot, interleaved;
+  double *freqs, amplitude;
+  bool get(PyObject* const* a, int64_t device) {
+    return get_i32(a[0], &hd) && get_i32(a[1], &rot) && get_flag(a[2], &interleaved) && hd >= 1 && rot >= 2 && rot % 2 == 0 &&
+           get_column(a[3], t_f64, device, rot / 2, &freqs) && get_f64(a[4], &amplitude);
+  }
+};
+
+// (x, y, positions, head_dim, rotary_dim, interleaved, freqs, amplitude, stream)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows x, y;
+  Turn t;
+  int64_t device;
+  int32_t *positions, x_dtype, y_dtype;
+  void* stream;
+  if (n != 9 || f_rope == nullptr || !get_place(a[8], &device, &stream) || !get_y_dtype(a[0], &x_dtype) || !get_y_dtype(a[1], &y_dtype) ||
+      !x.get(a[0], nullptr, device) || !y.get(a[1], nullptr, device) || x.rows != y.rows || x.cols != y.cols ||
+      !get_column(a[2], t_i32, device, x.rows, &positions) || !t.get(a + 3, device) || x.cols % t.hd != 0)
+    Py_RETURN_NONE;
+  return run([&] {
+    return f_rope(x.at, x_dtype, x.ld, y.at, y_dtype, y.ld, positions, x.rows, static_cast<int32_t>(x.cols / t.hd), t.hd, t.rot, t.interleaved,
+                  t.freqs, t.amplitude, stream);
+  });
+}
+
+// (q, q_out, k, v, positions, slots, head_dim, rotary_dim, interleaved, freqs, amplitude, k_table, v_table, bits, k_pages, v_pages, page_size,
+//  stream)
+PyObject* rope_quant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows q{}, out{}, k, v;
+  Pages p;
+  Turn t;
+  int64_t device, *slots;
+  int32_t *positions, bits, page_size;
+  void* stream;
+  if (n != 18 || f_rope_quant_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[13], &bits) || !get_i32(a[16], &page_size) ||
+      !k.get(a[2], t_bf16, device) || !v.get(a[3], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !get_column(a[4], t_i32, device, k.rows, &positions) || !get_slots(a[5], device, k.rows, &slots) || !t.get(a + 6, device) ||
+      k.cols % t.hd != 0 || !p.get(a[14], a[15], a[11], a[12], device, k.cols, page_size, bits))
+    Py_RETURN_NONE;
+  if (a[0] != Py_None || a[1] != Py_None) {
+    if (!q.get(a[0], t_bf16, device) || !out.get(a[1], t_bf16, device) || q.rows != k.rows || out.rows != q.rows || out.cols != q.cols ||
+        q.cols % t.hd != 0)
+      Py_RETURN_NONE;
+  }
+  return run([&] {
+    return f_rope_quant_paged(q.at, q.ld, out.at, out.ld, static_cast<int32_t>(q.cols / t.hd), k.at, k.ld, v.at, v.ld, k.rows,
+                              static_cast<int32_t>(k.cols / t.hd), t.hd, positions, t.rot, t.interleaved, t.freqs, t.amplitude, p.k_table,
+                              p.v_table, bits, slots, p.k, p.v, p.n, page_size, stream);
+  });
+}
+
+// Both tensors [B, heads, capacity] of a record of every token.
+struct Records {
+  float* weights;
+  int32_t* positions;
+  int64_t capacity;
+  bool get(PyObject* w, PyObject* pos, int64_t device, int64_t B, int64_t heads) {
+    int64_t bytes, a[3], b[3];
+    if (!get_whole(w, t_f32, device, &weights, &bytes) || !get_whole(pos, t_i32, device, &positions, &bytes) ||
+        !get_sizes(PyObject_GetAttr(w, n_shape), 3, a) || !get_sizes(PyObject_GetAttr(pos, n_shape), 3, b))
+      return false;
+    capacity = a[2];
+    return a[0] == B && a[1] == heads && b[0] == B && b[1] == heads && b[2] == capacity && capacity >= 1;
+  }
+};
+
+// (q, queries, n_q_heads, n_kv_heads, head_dim, scale, k_table, bits, k_pages, page_size, page_table, lens, lse, positions, fresh, weights,
+//  token_positions, stream)
+PyObject* attend_weights_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows q, table;
+  Pages p;
+  Records w;
+  int64_t device, lse_bytes, shape[2];
+  int32_t queries, n_q, n_kv, hd, bits, page_size, fresh, *lens, *positions = nullptr;
+  float scale, *lse;
+  void* stream;
+  if (n != 18 || f_attend_weights_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[1], &queries) || !get_i32(a[2], &n_q) ||
+      !get_i32(a[3], &n_kv) || !get_i32(a[4], &hd) || !get_f32(a[5], &scale) || !get_i32(a[7], &bits) || !get_i32(a[9], &page_size) ||
+      !get_i32(a[14], &fresh) || queries < 1 || n_q < 1 || n_kv < 1 || hd < 1 || !q.get(a[0], t_bf16, device) ||
+      q.cols != static_cast<int64_t>(n_q) * hd || !table.get(a[10], t_i32, device) || table.rows > INT32_MAX || q.rows != table.rows * queries)
+    Py_RETURN_NONE;
+  if (!p.get(a[8], a[8], a[6], a[6], device, static_cast<int64_t>(n_kv) * hd, page_size, bits) || !get_column(a[11], t_i32, device, table.rows, &lens) ||
+      !get_whole(a[12], t_f32, device, &lse, &lse_bytes) || !get_sizes(PyObject_GetAttr(a[12], n_shape), 2, shape) || shape[0] != q.rows ||
+      shape[1] != n_q || !w.get(a[15], a[16], device, table.rows, n_kv))
+    Py_RETURN_NONE;
+  if (a[13] != Py_None && !get_column(a[13], t_i32, device, table.rows, &positions)) Py_RETURN_NONE;
+  return run([&] {
+    return f_attend_weights_paged(q.at, q.ld, static_cast<int32_t>(table.rows), queries, n_q, n_kv, hd, scale, p.k_table, bits, p.k, p.n, page_size,
+                                  static_cast<int32_t*>(table.at), table.ld, static_cast<int32_t>(table.cols), lens, lse, positions, fresh,
+                                  w.weights, w.positions, w.capacity, stream);
+  });
+}
+
+// (n_kv_heads, head_dim, bits, k_pages, v_pages, page_size, page_table, lens, weights, token_positions, budget, first, recent, weights_out,
+//  token_positions_out, lens_out, workspace, stream)
+PyObject* evict_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Rows table;
+  Records w, out;
+  int64_t device, kb, vb, ws_bytes;
+  int32_t n_kv, hd, bits, page_size, budget, first, recent, *lens, *lens_out;
+  uint8_t *k, *v;
+  void *workspace, *stream;
+  if (n != 18 || f_evict_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[0], &n_kv) || !get_i32(a[1], &hd) ||
+      !get_i32(a[2], &bits) || !get_i32(a[5], &page_size) || !get_i32(a[10], &budget) || !get_i32(a[11], &first) || !get_i32(a[12], &recent) ||
+      n_kv < 1 || hd < 1 || static_cast<int64_t>(n_kv) * hd > RPTQ_MAX_CHANNELS || !table.get(a[6], t_i32, device) || table.rows > INT32_MAX)
+    Py_RETURN_NONE;
+  const int64_t size = static_cast<int64_t>(f_kv_page_bytes(n_kv * hd, page_size, bits));
+  if (size == 0 || !get_whole(a[3], t_u8, device, &k, &kb) || !get_whole(a[4], t_u8, device, &v, &vb) || kb != vb || kb < size || kb % size != 0 ||
+      !get_column(a[7], t_i32, device, table.rows, &lens) || !get_column(a[15], t_i32, device, table.rows, &lens_out) ||
+      !w.get(a[8], a[9], device, table.rows, n_kv) || !out.get(a[13], a[14], device, table.rows, n_kv) || out.capacity != w.capacity ||
+      !get_whole(a[16], nullptr, device, &workspace, &ws_bytes))
+    Py_RETURN_NONE;
+  return run([&] {
+    return f_evict_paged(static_cast<int32_t>(table.rows), n_kv, hd, bits, k, v, kb / size, page_size, static_cast<int32_t*>(table.at), table.ld,
+                         static_cast<int32_t>(table.cols), lens, w.weights, w.positions, w.capacity, budget, first, recent, out.weights,
+                         out.positions, lens_out, workspace, static_cast<size_t>(ws_bytes), stream);
+  });
+}
+
 template <typename F>
 bool set_entry(PyObject* addresses, const char* name, F* f) {
   PyObject* o = PyDict_GetItemString(addresses, name);   // (borrowed)
@@ -423,7 +561,8 @@ PyObject* setup(PyObject*, PyObject* args) {
   PyObject *addresses, *objects;
   if (!PyArg_ParseTuple(args, "O!O!", &PyDict_Type, &addresses, &PyDict_Type, &objects)) return nullptr;
   const struct { const char* name; PyObject** at; } wanted[] = {
-      {"bfloat16", &t_bf16}, {"float32", &t_f32}, {"int32", &t_i32}, {"int64", &t_i64}, {"uint8", &t_u8}, {"get_device", &get_device}, {"get_stream", &get_stream}};
+      {"bfloat16", &t_bf16}, {"float32", &t_f32}, {"int32", &t_i32}, {"int64", &t_i64}, {"uint8", &t_u8}, {"float64", &t_f64},
+      {"get_device", &get_device}, {"get_stream", &get_stream}};
   for (const auto& w : wanted) {
     PyObject* o = PyDict_GetItemString(objects, w.name);
     if (o == nullptr) return PyErr_Format(PyExc_KeyError, "%s", w.name);
@@ -436,7 +575,10 @@ PyObject* setup(PyObject*, PyObject* args) {
       !set_entry(addresses, "rptq_cluster_gemm_cw", &f_cluster_gemm_cw) || !set_entry(addresses, "rptq_kv_quant", &f_kv_quant) ||
       !set_entry(addresses, "rptq_kv_dequant", &f_kv_dequant) || !set_entry(addresses, "rptq_kv_page_bytes", &f_kv_page_bytes) ||
       !set_entry(addresses, "rptq_kv_quant_paged", &f_kv_quant_paged) ||
-      !set_entry(addresses, "rptq_kv_dequant_paged", &f_kv_dequant_paged) || !set_entry(addresses, "rptq_attend_paged", &f_attend_paged))
+      !set_entry(addresses, "rptq_kv_dequant_paged", &f_kv_dequant_paged) || !set_entry(addresses, "rptq_attend_paged", &f_attend_paged) ||
+      !set_entry(addresses, "rptq_rope", &f_rope) || !set_entry(addresses, "rptq_rope_quant_paged", &f_rope_quant_paged) ||
+      !set_entry(addresses, "rptq_attend_weights_paged", &f_attend_weights_paged) ||
+      !set_entry(addresses, "rptq_evict_paged", &f_evict_paged))
     return nullptr;
   Py_RETURN_NONE;
 }
@@ -445,7 +587,8 @@ PyObject* setup(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {RPTQ_METHOD(ln_quant), RPTQ_METHOD(cluster_gemm), RPTQ_METHOD(cluster_gemm_quant),
                          RPTQ_METHOD(cluster_rowsums), RPTQ_METHOD(cluster_gemm_cw), RPTQ_METHOD(kv_quant),
                          RPTQ_METHOD(kv_dequant), RPTQ_METHOD(kv_quant_paged), RPTQ_METHOD(kv_dequant_paged),
-                         RPTQ_METHOD(attend_paged), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         RPTQ_METHOD(attend_paged), RPTQ_METHOD(rope), RPTQ_METHOD(rope_quant_paged), RPTQ_METHOD(attend_weights_paged),
+                         RPTQ_METHOD(evict_paged), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,73 @@
+// Rotary positions: the pairs (a, b) of the first rotary_dim channels of every head turned by theta = position * frequency,
+//   (a cos - b sin, b cos + a sin),   pairs (j, j + rotary_dim / 2) or (2 j, 2 j + 1),
+// cosine and sine in 64 bits and rounded once to fp32, two products and a sum rounded to fp32 each, then once to the output's type.
+//
+// A workgroup takes a few rows: first their cosines and sines, one per thread, into LDS, then all heads of the rows, every thread
+// a piece of up to 16 bytes (half style: two, W channels and their W partners).  The angles are thus computed once per row
+// and group of heads and read from memory never.  What bounds it: memory; little rows: the launch.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "device_common.h"
+#include "rope_common.h"
+#include "rptq_internal.h"
+
+namespace rptq {
+
+template <int W, bool HALF, typename TX, typename TY>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeLaunch l) {
+  __shared__ __align__(16) float turns[2 * kRopePairs];
+  rope_rows<W, HALF, TX, TY>(l, blockIdx.x, turns);
+}
+
+template <int W, bool HALF>
+static void launch_types(const RopeLaunch& l, hipStream_t st) {
+  const bool xf = l.a.x_dtype == RPTQ_DTYPE_F32, yf = l.a.y_dtype == RPTQ_DTYPE_F32;
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(l.groups), dim3(kRopeThreads), 0, st, l); };
+  if (xf) yf ? go(rope_kernel<W, HALF, float, float>) : go(rope_kernel<W, HALF, float, __bf16>);
+  else yf ? go(rope_kernel<W, HALF, __bf16, float>) : go(rope_kernel<W, HALF, __bf16, __bf16>);
+}
+
+// Rows of a workgroup: as few as make its cosines worth their time, as many as leave enough workgroups; heads are shared out
+// where there are few rows.  W: channels of a piece.
+int32_t plan_rope(const RopeArgs& a, int W, bool same, RopeLaunch* l) {
+  const int half = a.rot / 2;
+  l->a = a;
+  l->turned = a.interleaved && W > 1 ? a.rot / W : half / W;
+  l->units = l->turned + (same ? 0 : (a.hd - a.rot) / W);
+  const int64_t row = static_cast<int64_t>(a.n_heads) * l->units;                       // pieces
+  const int64_t most_rows = std::max<int64_t>(1, std::min<int64_t>({kRopePairs / half, kRopeRows, kRopeMost / row}));
+  l->rows = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most_rows, a.T / kRopeWorkgroups)));
+  const int64_t row_groups = (a.T + l->rows - 1) / l->rows;
+  const int64_t want = std::max<int64_t>(1, kRopeWorkgroups / row_groups), fill = (row + kRopeThreads - 1) / kRopeThreads;
+  const int64_t groups = std::max<int64_t>(std::min(want, fill), (row + kRopeMost - 1) / kRopeMost);
+  l->heads = static_cast<int32_t>((a.n_heads + groups - 1) / groups);
+  l->head_groups = (a.n_heads + l->heads - 1) / l->heads;
+  if (row_groups * l->head_groups > INT32_MAX) return RPTQ_ERR_SHAPE;
+  l->groups = static_cast<int32_t>(row_groups * l->head_groups);
+  return RPTQ_OK;
+}
+
+int32_t launch_rope(const RopeArgs& a, hipStream_t st) {
+  const int32_t x_size = a.x_dtype == RPTQ_DTYPE_F32 ? 4 : 2, y_size = a.y_dtype == RPTQ_DTYPE_F32 ? 4 : 2;
+  const bool same = a.x == a.y && a.ld_x == a.ld_y && a.x_dtype == a.y_dtype, halves = a.interleaved == 0;
+  if (a.T == 0) return RPTQ_OK;
+  // The widest piece (16 bytes of bf16) that strides, addresses and the ends of the rotated part allow.
+  auto fits = [&](int w) {
+    auto at = [&](const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % std::min(w * size, 16) == 0; };
+    return a.ld_x % w == 0 && a.ld_y % w == 0 && a.hd % w == 0 && (halves ? a.rot / 2 : a.rot) % w == 0 && at(a.x, x_size) && at(a.y, y_size);
+  };
+  int W = 8;
+  while (W > 1 && !fits(W)) W /= 2;
+  RopeLaunch l;
+  if (int32_t s = plan_rope(a, W, same, &l)) return s;
+  if (W == 8) halves ? launch_types<8, true>(l, st) : launch_types<8, false>(l, st);
+  else if (W == 4) halves ? launch_types<4, true>(l, st) : launch_types<4, false>(l, st);
+  else if (W == 2) halves ? launch_types<2, true>(l, st) : launch_types<2, false>(l, st);
+  else halves ? launch_types<1, true>(l, st) : launch_types<1, false>(l, st);
+  RPTQ_HIP(hipGetLastError());
+  return RPTQ_OK;
+}
+
+}  // namespace rptq

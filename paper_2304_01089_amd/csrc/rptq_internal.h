@@ -179,6 +179,62 @@ struct AttendArgs {
   float* lse;
   void* workspace;
 };
+// rope.hip, kv_rope.hip: rotary positions, alone and in front of the cache
+struct RopeArgs {
+  const void* x;
+  int64_t ld_x;
+  void* y;
+  int64_t ld_y;
+  const int32_t* positions;
+  int64_t T;
+  int32_t x_dtype, y_dtype;
+  int32_t n_heads, hd, rot, interleaved;
+  const double* freqs;
+  double amplitude;
+};
+int32_t launch_rope(const RopeArgs& a, hipStream_t st);
+int32_t launch_rope_quant_paged(const RopeArgs* q, const RopeArgs& k, const PagedTensor& kt, const PagedTensor& vt, const int64_t* slots,
+                                const PagedGeom& g, int32_t bits, hipStream_t st);
+// attend_weights.hip, evict_paged.hip: what the tokens of the cache got of the attention, and dropping the lightest
+struct WeightArgs {
+  const uint16_t* q;
+  int64_t ld_q;
+  int32_t B, queries, n_q, n_kv, hd;
+  float scale;
+  const KvPos* k_pos;
+  const uint8_t* k_pages;
+  PagedGeom g;
+  const int32_t* page_table;
+  int64_t ld_pt;
+  int32_t pages_per_seq;
+  const int32_t* lens;
+  const float* lse;
+  const int32_t* positions;
+  int32_t fresh;
+  float* weights;
+  int32_t* token_positions;
+  int64_t capacity;
+};
+int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st);
+struct EvictArgs {
+  int32_t B, n_kv, hd, bits;
+  uint8_t *k_pages, *v_pages;
+  PagedGeom g;
+  const int32_t* page_table;
+  int64_t ld_pt;
+  int32_t pages_per_seq;
+  const int32_t* lens;
+  const float* weights;
+  const int32_t* positions;
+  int64_t capacity;
+  int32_t budget, first, recent;
+  float* weights_out;
+  int32_t* positions_out;
+  int32_t* lens_out;
+  void* workspace;
+};
+size_t evict_workspace_bytes(int32_t B, int32_t n_kv, int64_t capacity, int32_t budget);
+int32_t launch_evict_paged(const EvictArgs& a, hipStream_t st);
 size_t attend_workspace_bytes(int32_t B, int32_t n_q, int32_t n_kv, int32_t hd);
 int32_t launch_attend_paged(const AttendArgs& a, int32_t bits, int32_t out_dtype, hipStream_t st);
 // Per-head clustering (host.cpp), exposed through rptq_cluster_heads.

@@ -278,3 +278,94 @@ def attend_paged(cache: PagedCache, q, page_table, lens, scale=None, out=None, l
                         cache.k_table, cache.v_table, cache.bits, cache.k_pages, cache.v_pages, cache.page_size, page_table,
                         lens, out, lse, workspace)
     return out, lse
+
+
+# ---- rotary positions in front of the cache ------------------------------------------------------------
+@dataclass
+class Rotary:
+    """How a model turns its queries and keys: frequencies (float64, radians per position, one per pair, on the device), what the
+    turned channels are multiplied by, and whether a pair is channels (2 j, 2 j + 1) or (j, j + rotary_dim / 2) of a head."""
+    rotary_dim: int
+    freqs: object
+    amplitude: float = 1.0
+    interleaved: bool = False
+
+
+def rotary(rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None, factor: float = 1.0, trained: float = 0.0,
+           slow: float = 1.0, fast: float = 32.0, device="cuda") -> Rotary:
+    """Frequencies base^(-2 j / rotary_dim), for contexts longer than the trained one scaled as rptq_rope_freqs says ("linear", "base",
+    "parts")."""
+    import torch
+    freqs, amplitude = B.rptq_rope_freqs(rotary_dim, base, scaling, factor, trained, slow, fast)
+    return Rotary(rotary_dim, torch.from_numpy(freqs).to(device), amplitude, interleaved)
+
+
+def rope(rot: Rotary, x, positions, head_dim: int, out=None):
+    """Rows x [T, n_heads * head_dim] turned by their positions (int32 [T]); out may be x, or of another type."""
+    if out is None:
+        import torch
+        out = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
+    B.rptq_rope(x, out, positions, head_dim, rot.rotary_dim, rot.interleaved, rot.freqs, rot.amplitude)
+    return out
+
+
+def rope_quant_paged(cache: PagedCache, rot: Rotary, q, k, v, positions, slots, q_out=None):
+    """kv_quant_paged of turned keys, and the same tokens' queries turned (q None: no queries), in one launch.  Returns the
+    queries; q_out may be q."""
+    cache._compared or cache.compare()
+    if q is not None and q_out is None:
+        import torch
+        q_out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=q.device)
+    B.rptq_rope_quant_paged(q, q_out, k, v, positions, slots, cache.head_dim, rot.rotary_dim, rot.interleaved, rot.freqs, rot.amplitude,
+                            cache.k_table, cache.v_table, cache.bits, cache.k_pages, cache.v_pages, cache.page_size)
+    return q_out
+
+
+# ---- bounding the cache by accumulated attention weight --------------------------------------------------
+@dataclass
+class CacheTrack:
+    """A record of every token of a batch: what each key/value head's queries gave it, and where in the text it stands."""
+    weights: object       # fp32 [B, n_heads, capacity]
+    positions: object     # int32 [B, n_heads, capacity]
+
+
+def cache_track(cache: PagedCache, batch: int, capacity: int) -> CacheTrack:
+    """Records of up to `capacity` tokens of each of `batch` sequences; attend_weights_paged fills in a token's when it is fresh."""
+    import torch
+    shape, dev = (batch, cache.n_heads, capacity), cache.k_pages.device
+    return CacheTrack(torch.zeros(shape, dtype=torch.float32, device=dev), torch.zeros(shape, dtype=torch.int32, device=dev))
+
+
+def attend_weights_paged(cache: PagedCache, q, page_table, lens, lse, track: CacheTrack, positions=None, queries: int = 1, fresh: int = 1,
+                         scale=None):
+    """Adds what the last `queries` tokens of every sequence gave each of its tokens to the records.  q: [B * queries, n_q_heads *
+    head_dim]; lse: what attend_paged left for these rows; the newest `fresh` tokens' records start here, the newest one's
+    position being positions[b] (its index where None).  scale: attend_paged's."""
+    cache._compared or cache.compare()
+    B.rptq_attend_weights_paged(q, queries, q.shape[1] // cache.head_dim, cache.n_heads, cache.head_dim,
+                                cache.head_dim ** -0.5 if scale is None else scale, cache.k_table, cache.bits, cache.k_pages, cache.page_size,
+                                page_table, lens, lse, positions, fresh, track.weights, track.positions)
+
+
+def evict_paged_workspace(cache: PagedCache, batch: int, capacity: int, budget: int):
+    """Device memory for evict_paged calls of such sizes, one call at a time."""
+    import torch
+    return torch.empty(max(16, B.rptq_evict_paged_workspace_bytes(batch, cache.n_heads, capacity, budget)), dtype=torch.uint8,
+                       device=cache.k_pages.device)
+
+
+def evict_paged(cache: PagedCache, page_table, lens, track: CacheTrack, budget: int, first: int = 0, recent: int = 0, out=None,
+                lens_out=None, workspace=None):
+    """Every head of every sequence of more than `budget` tokens keeps that many: the ones at positions below `first`, the newest
+    `recent`, then the heaviest.  Rows move in place, records too unless `out` is another track.  Returns the new lengths."""
+    cache._compared or cache.compare()
+    if lens_out is None or workspace is None:
+        import torch
+        if lens_out is None:
+            lens_out = torch.empty(tuple(lens.shape), dtype=torch.int32, device=lens.device)
+        if workspace is None:
+            workspace = evict_paged_workspace(cache, lens.shape[0], track.weights.shape[2], budget)
+    out = track if out is None else out
+    B.rptq_evict_paged(cache.n_heads, cache.head_dim, cache.bits, cache.k_pages, cache.v_pages, cache.page_size, page_table, lens,
+                       track.weights, track.positions, budget, first, recent, out.weights, out.positions, lens_out, workspace)
+    return lens_out

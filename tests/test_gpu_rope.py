@@ -1,0 +1,290 @@
+"""Rotary positions on the GPU, alone and in front of the paged cache: fp32 results bit for bit as the documented roundings give them,
+codes bit for bit, and everything that a call must leave alone."""
+import numpy as np
+import pytest
+
+from oracle import kv_cache as kvo
+
+import bounding
+import paged
+from test_gpu_paged import dev, dev_bf16, site, slots_for
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def rp():
+    import paper_2304_01089_amd as rp_
+    rp_.load_library()
+    assert torch.cuda.is_available()
+    return rp_
+
+
+def handle(rp, rot, interleaved, amplitude=1.0, base=10000.0):
+    r = rp.rotary(rot, base, interleaved=interleaved)
+    r.amplitude = amplitude
+    return r
+
+
+def rows(rng, T, n):
+    return kvo.round_to_bf16(rng.standard_normal((T, n)).astype(np.float32))
+
+
+def bf16_bits_of(x32):
+    return kvo.round_to_bf16(np.asarray(x32, np.float32))
+
+
+# (T, heads, head width, rotated, columns in front of the rows in a wider tensor, columns of that tensor more than the rows)
+SHAPES = [
+    (1, 1, 64, 64, 0, 0), (1, 24, 64, 64, 0, 64), (3, 5, 128, 128, 128, 256), (7, 25, 80, 32, 0, 0), (5, 3, 80, 20, 0, 4), (9, 2, 100, 100, 4, 12),
+    (4, 7, 6, 2, 2, 2), (6, 3, 10, 6, 1, 2), (2, 2, 1024, 1024, 0, 0), (130, 1, 256, 64, 8, 16), (1030, 6, 128, 128, 0, 0), (5000, 2, 32, 16, 0, 0),
+    (2, 256, 256, 256, 0, 0), (33, 1, 2, 2, 0, 1), (3, 65, 1000, 998, 0, 0), (3000, 4, 64, 62, 3, 5),
+]
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "interleaved"])
+@pytest.mark.parametrize("T,heads,hd,rot,front,more", SHAPES)
+def test_rows_turned(rp, T, heads, hd, rot, front, more, interleaved):
+    rng = np.random.default_rng(T * 7 + heads * hd + rot)
+    n = heads * hd
+    r = handle(rp, rot, interleaved, amplitude=1.25)
+    freqs = r.freqs.cpu().numpy()
+    positions = rng.integers(0, 70000, T)
+    positions[:min(T, 3)] = [0, 131071, -77][:min(T, 3)]
+    x = rows(rng, T, n)
+    want = bounding.rope32(x, positions, hd, rot, interleaved, freqs, 1.25)
+    y64, tol = bounding.rope64(x, positions, hd, rot, interleaved, freqs, 1.25)
+    pos = dev(positions, np.int32)
+    for xt, yt in ((BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)):
+        wide = torch.full((T, n + front + more), 7.0, dtype=xt, device="cuda")
+        wide[:, front:front + n] = dev(x).to(xt)
+        out = torch.full((T, n + front + more), 9.0, dtype=yt, device="cuda")
+        rp.rope(r, wide[:, front:front + n], pos, hd, out=out[:, front:front + n])
+        torch.cuda.synchronize()
+        got = out[:, front:front + n].float().cpu().numpy()
+        assert np.array_equal(got, want if yt is F32 else bf16_bits_of(want)), (xt, yt)
+        near = tol if yt is F32 else tol + 2.0 ** -8 * (np.abs(y64) + tol)
+        assert (np.abs(got - y64) <= near).all()
+        assert (out[:, :front] == 9.0).all() and (out[:, front + n:] == 9.0).all() and torch.equal(wide[:, front:front + n], dev(x).to(xt))
+        if xt is yt:                                                   # in place, and the allocating form
+            fresh = rp.rope(r, wide[:, front:front + n], pos, hd)
+            assert fresh.dtype == xt and torch.equal(fresh, out[:, front:front + n])
+            assert rp.rope(r, wide[:, front:front + n], pos, hd, out=wide[:, front:front + n]) is not None
+            assert torch.equal(wide[:, front:front + n], fresh) and (wide[:, :front] == 7.0).all() and (wide[:, front + n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_positions(rp, interleaved):
+    """Angles with 31 bits in front of the point."""
+    positions = np.array([2 ** 31 - 1, -2 ** 31, 2 ** 30 + 1, 10 ** 9, 16777217, 1, 0, -1])
+    rng = np.random.default_rng(3)
+    x = rows(rng, 8, 256)
+    r = handle(rp, 128, interleaved)
+    got = rp.rope(r, dev(x), dev(positions, np.int32), 128).cpu().numpy()
+    assert np.array_equal(got, bounding.rope32(x, positions, 128, 128, interleaved, r.freqs.cpu().numpy()))
+    assert np.array_equal(got[6], x[6])
+
+
+def test_every_quarter_of_the_circle(rp):
+    """One pair, frequencies of pi / 2 and thereabouts: the quadrants' borders."""
+    positions = np.arange(-400, 400)
+    x = np.tile(np.array([[1.0, 0.5]], np.float32), (800, 1))
+    for f in (np.pi / 2, np.pi / 4, 1.0, 3 * np.pi / 7, 0.0, 1e-300, 25.0):
+        r = rp.Rotary(2, dev(np.array([f])))
+        got = rp.rope(r, dev(x), dev(positions, np.int32), 2).cpu().numpy()
+        y64, tol = bounding.rope64(x, positions, 2, 2, False, np.array([f]))
+        assert (np.abs(got - y64) <= tol + 1e-15).all(), f               # (pi / 2 in 64 bits is off by 6e-17 a quarter)
+
+
+def test_values_that_are_not_finite_stay_in_their_pair(rp):
+    rng = np.random.default_rng(9)
+    x = rows(rng, 2, 3 * 64)
+    bad = x.copy()
+    bad[0, 64 + 3], bad[1, 5], bad[0, 130], bad[1, 63] = np.nan, np.inf, -np.inf, np.nan
+    r = handle(rp, 32, False)
+    pos = dev([5, 6], np.int32)
+    a, b = (rp.rope(r, dev_bf16(t), pos, 64).float().cpu().numpy() for t in (x, bad))
+    same = np.ones((2, 192), bool)
+    for row, head, ch in ((0, 1, 3), (1, 0, 5), (0, 2, 2), (1, 0, 63)):
+        same[row, head * 64 + ch] = False
+        if ch < 32:
+            same[row, head * 64 + (ch + 16) % 32] = False
+    assert np.array_equal(a[same], b[same]) and not np.isfinite(b[~same]).any()
+
+
+def test_more_values_than_32_bits_count(rp):
+    """Row offsets past 2^32 bytes: the last rows of a tall tensor."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough free memory")
+    T, n = (1 << 31) // 4096 + 5, 4096
+    x = torch.ones(T, n, dtype=BF16, device="cuda")
+    r = handle(rp, 128, False)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    y = rp.rope(r, x, pos, 128)
+    tail = rp.rope(r, x[-9:].clone(), pos[-9:].clone(), 128)
+    assert torch.equal(y[-9:], tail) and torch.equal(y[:3], rp.rope(r, x[:3].clone(), pos[:3].clone(), 128))
+    middle = T // 2
+    assert torch.equal(y[middle:middle + 5], rp.rope(r, x[:5].clone(), pos[middle:middle + 5].clone(), 128))
+
+
+# ---- in front of the cache ----------------------------------------------------------------------------------
+WRITES = [(1, 1, 1, 128, 16, 128), (1, 12, 12, 64, 16, 64), (3, 2, 6, 64, 16, 32), (17, 9, 9, 128, 32, 64), (33, 6, 12, 256, 64, 256), (5, 4, 8, 32, 4096, 16),
+          (300, 12, 12, 64, 128, 48), (700, 3, 24, 128, 256, 128), (9, 5, 5, 256, 16, 16), (64, 36, 36, 32, 16, 32)]
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "interleaved"])
+@pytest.mark.parametrize("bits", [3, 4, 8])
+@pytest.mark.parametrize("T,H,n_q,hd,page,rot", WRITES)
+def test_rotated_rows_written_bit_for_bit(rp, T, H, n_q, hd, page, rot, bits, interleaved):
+    (hk, klo, khi), (hv, vlo, vhi), kt, vt = site(H, hd, bits)
+    d, nq = H * hd, n_q * hd
+    rng = np.random.default_rng(T + d + page + bits + rot)
+    n_pages = (T + page - 1) // page + 2
+    slots = slots_for(rng, T, n_pages, page)
+    k, v, q = paged.values(rng, klo, khi, T), paged.values(rng, vlo, vhi, T), rows(rng, T, nq)
+    positions = rng.integers(0, 40000, T)
+    r = handle(rp, rot, interleaved, amplitude=1.125)
+    freqs = r.freqs.cpu().numpy()
+    turned = bounding.rope32(k, positions, hd, rot, interleaved, freqs, 1.125)
+    want = [np.full((n_pages, d // 128, page, 16 * bits), 0xA5, np.uint8) for _ in range(2)]
+    for p, c in zip(want, (kvo.kv_quant(turned, hk, 0, bits), kvo.kv_quant(v, hv, 0, bits))):
+        paged.put(p, slots, paged.page_rows(c, bits), page)
+    want_q = bf16_bits_of(bounding.rope32(q, positions, hd, rot, interleaved, freqs, 1.125))
+    wide = torch.full((T, nq + 2 * d + 8), float("nan"), dtype=BF16, device="cuda")
+    wide[:, :nq], wide[:, nq:nq + d], wide[:, nq + d:nq + 2 * d] = dev_bf16(q), dev_bf16(k), dev_bf16(v)
+    qc, kc, vc = wide[:, :nq], wide[:, nq:nq + d], wide[:, nq + d:nq + 2 * d]
+    pos, sl = dev(positions, np.int32), dev(slots)
+    for form in ("packed, in place", "apart", "no queries"):
+        pool = torch.full((2, n_pages + 1, d // 128, page, 16 * bits), 0xA5, dtype=torch.uint8, device="cuda")
+        cache = rp.PagedCache(H, hd, bits, page, pool[0, :n_pages], pool[1, :n_pages], kt, vt)
+        if form == "apart":
+            got = rp.rope_quant_paged(cache, r, dev_bf16(q), dev_bf16(k), dev_bf16(v), pos, sl)
+        elif form == "no queries":
+            assert rp.rope_quant_paged(cache, r, None, kc, vc, pos, sl) is None
+        else:
+            got = rp.rope_quant_paged(cache, r, qc, kc, vc, pos, sl, q_out=qc)
+            assert torch.equal(kc, dev_bf16(k)) and torch.equal(vc, dev_bf16(v)) and torch.isnan(wide[:, nq + 2 * d:]).all()
+        torch.cuda.synchronize()
+        if form != "no queries":
+            assert np.array_equal(got.float().cpu().numpy(), want_q), form
+        for p, t in zip(want, pool.cpu().numpy()):
+            assert np.array_equal(t[:n_pages], p) and (t[n_pages] == 0xA5).all(), form
+
+
+def test_position_zero_writes_what_the_plain_write_does(rp):
+    H, hd, bits, page, T = 4, 64, 4, 16, 50
+    (hk, klo, khi), (hv, vlo, vhi), kt, vt = site(H, hd, bits)
+    rng = np.random.default_rng(2)
+    k, v = dev_bf16(paged.values(rng, klo, khi, T)), dev_bf16(paged.values(rng, vlo, vhi, T))
+    a, b = (rp.paged_cache(5, page, H, hd, bits, kt, vt) for _ in range(2))
+    slots = dev(rng.permutation(80)[:T].astype(np.int64))
+    rp.kv_quant_paged(a, k, v, slots)
+    rp.rope_quant_paged(b, handle(rp, 64, True), None, k, v, torch.zeros(T, dtype=torch.int32, device="cuda"), slots)
+    assert torch.equal(a.k_pages, b.k_pages) and torch.equal(a.v_pages, b.v_pages)
+
+
+def test_long_prompts_written(rp):
+    """More rows than a wave's window of 64 slots and positions, several windows long."""
+    H, hd, bits, page, T = 2, 64, 4, 64, 70000
+    (hk, klo, khi), (hv, vlo, vhi), kt, vt = site(H, hd, bits)
+    rng = np.random.default_rng(8)
+    k = paged.values(rng, klo, khi, T)
+    kd, n_pages = dev_bf16(k), T // page + 2
+    cache = rp.paged_cache(n_pages, page, H, hd, bits, kt, vt)
+    slots = rng.permutation(n_pages * page)[:T]
+    positions = rng.integers(0, 100000, T)
+    r = handle(rp, 64, False)
+    rp.rope_quant_paged(cache, r, None, kd, kd, dev(positions, np.int32), dev(slots.astype(np.int64)))
+    pages = cache.k_pages.cpu().numpy()
+    some = np.concatenate([np.arange(300), np.arange(T - 300, T), rng.integers(0, T, 5000)])
+    turned = bounding.rope32(k[some], positions[some], hd, 64, False, r.freqs.cpu().numpy())
+    want = paged.page_rows(kvo.kv_quant(turned, hk, 0, bits), bits)
+    assert np.array_equal(pages[slots[some] // page, :, slots[some] % page], want)
+
+
+def test_streams_and_recorded_steps(rp):
+    """Two streams at once, then a step recorded twice and replayed with other positions and slots between eager ones."""
+    H, hd, bits, page, T, n_q = 2, 64, 4, 16, 6, 4
+    (hk, klo, khi), (hv, vlo, vhi), kt, vt = site(H, hd, bits)
+    d = H * hd
+    rng = np.random.default_rng(4)
+    cache, eager = (rp.paged_cache(8, page, H, hd, bits, kt, vt) for _ in range(2))
+    r = handle(rp, 32, True)
+    qkv = torch.zeros(T, (n_q + 2 * H) * hd, dtype=BF16, device="cuda")
+    q, k, v = qkv[:, :n_q * hd], qkv[:, n_q * hd:n_q * hd + d], qkv[:, n_q * hd + d:]
+    pos, slots = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.arange(T, device="cuda")
+    step = lambda c: (rp.rope_quant_paged(c, r, q, k, v, pos, slots), rp.rope(r, qkv, pos, hd))       # noqa: E731
+    step(eager)
+    torch.cuda.synchronize()
+    graphs, results = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            results.append(step(cache))
+        graphs.append(g)
+    eager.k_pages.copy_(cache.k_pages), eager.v_pages.copy_(cache.v_pages)
+    for i in range(8):
+        qkv.copy_(dev_bf16(rows(rng, T, qkv.shape[1])))
+        pos.copy_(dev(rng.integers(0, 9999, T), np.int32))
+        slots.copy_(dev(rng.permutation(128)[:T].astype(np.int64)))
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        for a, b in zip([t.clone() for t in results[i % 2]], step(eager)):
+            assert torch.equal(a, b)
+        assert torch.equal(cache.k_pages, eager.k_pages) and torch.equal(cache.v_pages, eager.v_pages)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    want = rp.rope(r, qkv, pos, hd)
+    outs = [torch.zeros_like(want) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, o in zip(streams, outs):
+            with torch.cuda.stream(s):
+                o.zero_()
+                rp.rope(r, qkv, pos, hd, out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_recording_a_first_rotation(rp):
+    x, pos, r = torch.randn(5, 3 * 48, device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda"), handle(rp, 48, False)
+    out = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rp.rope(r, x, pos, 48, out=out)
+    for _ in range(3):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, rp.rope(r, x, pos, 48))
+
+
+def test_refusals(rp):
+    H, hd, bits, page = 2, 64, 4, 16
+    _, _, kt, vt = site(H, hd, bits)
+    cache = rp.paged_cache(3, page, H, hd, bits, kt, vt)
+    r = handle(rp, 64, False)
+    x, pos, slots = torch.zeros(3, 128, dtype=BF16, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    for match, call in (
+            ("one per row", lambda: rp.rope(r, x, pos[:2], 64)), ("dtype", lambda: rp.rope(r, x, pos.long(), 64)), ("n_heads", lambda: rp.rope(r, x, pos, 48)),
+            ("bf16 or fp32", lambda: rp.rope(r, x.half(), pos, 64)), ("bf16 or fp32", lambda: rp.rope(r, x, pos, 64, out=x.half())),
+            ("shape", lambda: rp.rope(r, x, pos, 64, out=x[:2])), ("contiguous rows", lambda: rp.rope(r, x.t().contiguous().t(), pos, 64, out=x)),
+            ("per pair", lambda: rp.rope(rp.Rotary(64, r.freqs[:16]), x, pos, 64)), ("dtype", lambda: rp.rope(rp.Rotary(64, r.freqs.float()), x, pos, 64)),
+            ("device", lambda: rp.rope(r, x, pos.cpu(), 64)), ("device", lambda: rp.rope(rp.Rotary(64, r.freqs.cpu()), x, pos, 64)),
+            ("dtype", lambda: rp.rope_quant_paged(cache, r, x, x.float(), x, pos, slots)), ("dtype", lambda: rp.rope_quant_paged(cache, r, x, x, x, pos, slots.int())),
+            ("dtype", lambda: rp.rope_quant_paged(cache, r, x.float(), x, x, pos, slots, q_out=x)), ("one per row", lambda: rp.rope_quant_paged(cache, r, x, x, x, pos[:2], slots)),
+            ("shape", lambda: rp.rope_quant_paged(cache, r, x[:2], x, x, pos, slots)), ("n_q_heads", lambda: rp.rope_quant_paged(cache, r, x[:, :100], x, x, pos, slots)),
+            ("both or none", lambda: rp.rope_quant_paged(cache, r, None, x, x, pos, slots, q_out=x))):
+        with pytest.raises(ValueError, match=match):
+            call()
+    for status, call in (
+            (-2, lambda: rp.rope(rp.Rotary(66, torch.zeros(33, dtype=torch.float64, device="cuda")), x, pos, 64)), (-6, lambda: rp.rope(rp.Rotary(64, r.freqs, float("nan")), x, pos, 64)),
+            (-2, lambda: rp.rope(r, x[:1].expand(3, 128), pos, 64)), (-2, lambda: rp.rope_quant_paged(cache, handle(rp, 24, False), x, x, x, pos, slots)),
+            (-4, lambda: rp.rope_quant_paged(cache, r, torch.zeros(3, 136, dtype=BF16, device="cuda")[:, 4:132], x, x, pos, slots, q_out=x))):
+        with pytest.raises(rp.RptqError, match="status %d" % status):
+            call()
+    none = x[:0]
+    assert rp.rope(r, none, pos[:0], 64).shape == (0, 128)
+    assert rp.rope_quant_paged(cache, r, none, none, none, pos[:0], slots[:0]).shape == (0, 128) and not cache.k_pages.any()
