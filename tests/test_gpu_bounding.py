@@ -220,7 +220,7 @@ def test_long_sequences_cut(rp, n, budget):
         evicted(rp, b, budget, 0, 0, w, p, n, True)
 
 
-@pytest.mark.parametrize("what", ["all equal", "all zero", "zeros of both signs", "infinities and nan", "negative", "ends of the range", "steps of the last bit", "safe ones first"])
+@pytest.mark.parametrize("what", ["all equal", "all zero", "zeros of both signs", "infinities and nan", "negative", "ends of the range", "steps of the last bit", "steps of the last bits", "safe ones first"])
 def test_orders_of_weights(rp, what):
     rng = np.random.default_rng(6)
     n, budget = 500, 123
@@ -242,6 +242,8 @@ def test_orders_of_weights(rp, what):
         w = rng.choice(np.array([np.finfo(np.float32).max, np.finfo(np.float32).tiny, 1e-45, 0.0, 3e38], np.float32), w.shape)
     elif what == "steps of the last bit":
         w = (np.float32(1.0).view(np.int32) + rng.integers(0, 300, w.shape).astype(np.int32)).view(np.float32)
+    elif what == "steps of the last bits":
+        w = (np.float32(1.0).view(np.int32) + rng.integers(0, 1 << 14, w.shape).astype(np.int32)).view(np.float32)
     else:
         w = -np.arange(n, dtype=np.float32) * np.ones((2, 2, 1), np.float32)
         p[:] = np.arange(n)
