@@ -29,53 +29,60 @@ struct WeightPlan {
   int32_t group;                               // rows of a tile that belong to one key/value head: 1, 2 or 4
   int32_t set_tiles, tiles;                    // row tiles of a set of heads (4 / group of them), and all
   int32_t parts;                               // workgroups that share a sequence's tokens
+  int32_t share;                               // query heads on a key/value head
+  double per_share, per_set;                   // 1 / share and 1 / set_tiles, a little more
 };
 
 struct QueryRow {
-  float scale, off;                            // score = digits' sum * scale - off, in units of log2
-  int32_t end, unused;                         // tokens that it sees
+  float low, high, off;                        // a score in units of log2: low * (digits 0, 1) + high * (digits 2, 3) - off
+  int32_t end;                                 // tokens that the query sees
 };
 
-template <int BITS, int NB>
-__global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
+// NB: blocks of a unit; HEADS: key/value heads of a unit
+template <int BITS, int NB, int HEADS>
+__global__ void __launch_bounds__(256, NB == 2 ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
+  constexpr int kHd = P / HEADS;
   constexpr int kDigitRow = P + 16;                        // (16 more: other banks)
   constexpr int kHeld = held_tiles(NB);
   __shared__ __align__(16) unsigned char q_dig[kHeld * 16 * kDigitRow];
   __shared__ __align__(16) QueryRow rows[kHeld * kRowHeads];
+  __shared__ __align__(16) unsigned char table[P / 8 * 144];           // eight positions' records, and 16 bytes (banks)
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = blockIdx.x, unit = blockIdx.y, b = blockIdx.z;
   const int64_t room = min(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
-  const int len = static_cast<int>(min(static_cast<int64_t>(max(a.lens[b], 0)), room));
+  // (requested first, all at once: the length, the first two tiles' pages, the positions' records)
+  const int length = a.lens[b];
+  const int32_t* pt = a.page_table + b * a.ld_pt;
+  auto token_of = [&](int k) { return (part + k * plan.parts) * kTileTokens + wave * kTile; };
+  auto page_at = [&](int k) { return pt[min((token_of(k) + (lane & 3) * 16) >> a.g.page_shift, a.pages_per_seq - 1)]; };
+  const int page0 = page_at(0), page1 = page_at(1);
+  typedef int i4v __attribute__((ext_vector_type(4)));
+  const i4v record = reinterpret_cast<const i4v*>(a.k_pos + unit * P)[threadIdx.x & (P - 1)];
+  const int len = static_cast<int>(min(static_cast<int64_t>(max(length, 0)), room));
   if (part * kTileTokens >= len) return;
 
-  const int share = a.n_q / a.n_kv, pairs = share * a.queries;
-  const int unit_heads = P / a.hd;                         // key/value heads
-  const int hd_shift = __builtin_ctz(a.hd), set_heads = kRowHeads / plan.group;
-  const int group_shift = plan.group >> 1;                 // (log2 of 1, 2, 4)
-  const KvPos* kt = a.k_pos + unit * P;
-  KvPos kp[2 * NB];
-#pragma unroll
-  for (int i = 0; i < 2 * NB; ++i) kp[i] = kt[i * 64 + lane];
+  const int share = plan.share, pairs = share * a.queries;
+  // (pairs and tiles are below 2^31, a quotient's fraction is a multiple of its divisor's inverse or 0: 2^-50 of it does not reach the next number)
+  const double by_share = plan.per_share, by_set = plan.per_set;
+  auto quotient = [](int n, double per) { return static_cast<int>(n * per); };
+  const int group = HEADS == 1 ? 4 : plan.group, group_shift = group >> 1;                 // (log2 of 1, 2, 4)
+  const int set_heads = kRowHeads / group;
+  const bool full_rows = pairs % group == 0;               // (no row without a query)
 
   // ---- a wave's tiles: every parts-th run of 256 tokens, 64 of them each -----------------------------------------
-  const int32_t* pt = a.page_table + b * a.ld_pt;
-  const int last_page = (len - 1) >> a.g.page_shift, block_rows = 1 << a.g.page_shift;
-  auto token_of = [&](int k) { return (part + k * plan.parts) * kTileTokens + wave * kTile; };
+  const int block_rows = 1 << a.g.page_shift;
   const int first_token = token_of(0), step = plan.parts * kTileTokens;
   const int my_tiles = first_token < len ? (len - first_token + step - 1) / step : 0;
   // lane 4 i + r's 16 tokens (r: lane & 3) of tile k: their page's number, or -1
-  auto page_of = [&](int k) {
-    const int t = token_of(k) + (lane & 3) * 16;
-    const int id = pt[min(t >> a.g.page_shift, last_page)];
-    return t < len && id >= 0 && id < a.g.n_pages ? id : -1;
-  };
+  auto page_of = [&](int k, int id) { return token_of(k) + (lane & 3) * 16 < len && id >= 0 && id < a.g.n_pages ? id : -1; };
   const uint32_t k_off = n16 * kRow + g4 * (4 * BITS);
   const int block_bytes = block_rows * kRow;
-  auto load_tile = [&](int k, int id, uint32_t (&x)[4][NB][BITS]) {
+  uint32_t kr[4][NB][BITS];
+  auto load_keys = [&](int k, int id) __attribute__((always_inline)) {
     typedef unsigned u3v __attribute__((ext_vector_type(3)));
     typedef unsigned u4v __attribute__((ext_vector_type(4)));
     const int t = (token_of(k) + (lane & 3) * 16) & (block_rows - 1);
@@ -91,66 +98,116 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightArgs a, We
         if constexpr (BITS == 3) {
           const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rsrc, k_off, nb * block_bytes, 0);
 #pragma unroll
-          for (int e = 0; e < 3; ++e) x[r][nb][e] = v[e];
+          for (int e = 0; e < 3; ++e) kr[r][nb][e] = v[e];
         } else {
 #pragma unroll
           for (int h = 0; h < BITS / 4; ++h) {
             const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_off + 16 * h, nb * block_bytes, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[r][nb][4 * h + e] = v[e];
+            for (int e = 0; e < 4; ++e) kr[r][nb][4 * h + e] = v[e];
           }
         }
       }
     }
   };
+  // What this lane adds up of a tile, slot e: head e / set_heads * set_heads + g4 / group of the unit, token e % set_heads plus (g4 % group)
+  // * set_heads times 16, plus n16, of the tile (every weight of the tile's 64 tokens and HEADS heads is one lane's).
+  const int64_t first_at = (static_cast<int64_t>(b) * a.n_kv + unit * HEADS) * a.capacity;
+  auto slot_head = [&](int e) { return e / set_heads * set_heads + (g4 >> group_shift); };
+  auto slot_group = [&](int e) { return (g4 & (group - 1)) * set_heads + (e & (set_heads - 1)); };       // of 16 tokens
+  auto slot_token = [&](int k, int e) { return token_of(k) + slot_group(e) * 16 + n16; };
+  float old[HEADS], old_next[HEADS];
+  auto load_old = [&](int k) __attribute__((always_inline)) {      // (behind the end: the last token's, not used)
+#pragma unroll
+    for (int e = 0; e < HEADS; ++e) old_next[e] = a.weights[first_at + slot_head(e) * a.capacity + min(slot_token(k, e), len - 1)];
+  };
 
   for (int tile0 = 0; tile0 < plan.tiles; tile0 += kHeld) {
     const int tile1 = min(tile0 + kHeld, plan.tiles);
-    uint32_t kr[4][NB][BITS];
-    int id = my_tiles > 0 ? page_of(0) : -1;
-    int next_id = my_tiles > 1 ? page_of(1) : -1;
-    if (my_tiles > 0) load_tile(0, id, kr);
-    if (tile0 > 0) __syncthreads();                        // (the digits before have been read)
+    int id = page_of(0, page0), next_page = page1;
+    if (tile0 == 0) *reinterpret_cast<i4v*>(table + (threadIdx.x & (P - 1)) * 16 + (threadIdx.x & (P - 1)) / 8 * 16) = record;
+    __syncthreads();                                       // (later: the digits before have been read)
 
-    // ---- queries to digits: a wave takes every fourth row ----------------------------------------------------------
-    for (int i = wave; i < (tile1 - tile0) * kRowHeads; i += 4) {
-      const int tile = tile0 + i / kRowHeads, g = i & (kRowHeads - 1);
-      const int set = tile / plan.set_tiles, in_set = tile - set * plan.set_tiles;
-      const int head = set * set_heads + (g >> group_shift);                   // of the unit
-      const int pair = in_set * plan.group + (g & (plan.group - 1));
-      const bool there = head < unit_heads && pair < pairs;
-      const int query = there ? pair / share : 0, q_head = (unit * unit_heads + (there ? head : 0)) * share + (there ? pair - query * share : 0);
-      const int64_t q_row = static_cast<int64_t>(b) * a.queries + query;
-      const uint16_t* q = a.q + q_row * a.ld_q + q_head * a.hd;
-      float x[2 * NB], top = 0.0f;
-      bool bad = false;
-      double z = 0.0;
+    // ---- queries to digits: a wave takes every fourth row tile, 16 lanes a row, a lane eight positions of a block -----------
+    {
+      i4v kp[NB][8];
 #pragma unroll
-      for (int j = 0; j < 2 * NB; ++j) {
-        const int pos = j * 64 + lane;
-        const bool own = there && (NB == 2 || pos >> hd_shift == head);
-        const float v = __uint_as_float(static_cast<uint32_t>(q[kp[j].src & (a.hd - 1)]) << 16) * kp[j].s * (a.scale * kLog2e);
-        x[j] = own ? v : 0.0f;
-        top = fmaxf(top, fabsf(x[j]));
-        bad = bad || !(fabsf(x[j]) < __builtin_huge_valf());
-        z += static_cast<double>(x[j]) * kp[j].z;
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) kp[nb][e] = *reinterpret_cast<const i4v*>(table + (nb * 16 + n16) * 144 + e * 16);
+      const float to_log2 = a.scale * kLog2e;
+      struct Query {
+        int end;                                           // 0: no query
+        bool own;                                          // whether the lane's positions are its head's
+        float lse;
+        uint16_t raw[NB][8];
+      };
+      auto request = [&](int tile) __attribute__((always_inline)) {
+        Query r;
+        const int set = HEADS == 1 ? 0 : quotient(tile, by_set), in_set = tile - set * plan.set_tiles;
+        const int head = set * set_heads + (g4 >> group_shift);                // of the unit
+        const int pair = in_set * group + (g4 & (group - 1));
+        const bool there = head < HEADS && pair < pairs;
+        const int query = there ? quotient(pair, by_share) : 0, q_head = (unit * HEADS + (there ? head : 0)) * share + (there ? pair - query * share : 0);
+        const int64_t q_row = static_cast<int64_t>(b) * a.queries + query;
+        const uint16_t* q = a.q + q_row * a.ld_q + q_head * kHd;
+        r.lse = a.lse[q_row * a.n_q + q_head];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r.raw[nb][e] = q[kp[nb][e][0] & (kHd - 1)];
+        r.end = there ? len - (a.queries - 1 - query) : 0;
+        r.own = there && (NB == 2 || n16 * 8 / kHd == head);
+        return r;
+      };
+      if (my_tiles > 0) {
+        load_old(0);
+        load_keys(0, id);
       }
-      top = wave_max(top);
-      z = wave_sum(z);
-      const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;         // top < 2^e
+      Query next = request(min(tile0 + wave, tile1 - 1));
+      for (int tile = tile0 + wave; tile < tile1; tile += 4) {
+        const Query now = next;
+        next = request(min(tile + 4, tile1 - 1));
+        float x[NB][8], top = 0.0f;
+        bool bad = false;
+        double zterm = 0.0;
 #pragma unroll
-      for (int j = 0; j < 2 * NB; ++j) {
-        const uint32_t d = digits(static_cast<int>(rintf(ldexpf(x[j], 30 - e))));
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int by = 0; by < 4; ++by) q_dig[(i * 4 + by) * kDigitRow + j * 64 + lane] = static_cast<unsigned char>(d >> (8 * by));
+          for (int e = 0; e < 8; ++e) {
+            const float v = __uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16) * __int_as_float(kp[nb][e][2]) * to_log2;
+            x[nb][e] = now.own ? v : 0.0f;
+            top = fmaxf(top, fabsf(x[nb][e]));
+            bad = bad || !(fabsf(x[nb][e]) < __builtin_huge_valf());
+            zterm = fma(static_cast<double>(x[nb][e]), static_cast<double>(kp[nb][e][3]), zterm);
+          }
+        top = row16_max(top);
+        zterm = row16_sum(zterm);
+        const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;      // top < 2^ex
+        const int local = tile - tile0;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          uint32_t d[8], plane[4][2];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[e] = digits(static_cast<int>(rintf(ldexpf(x[nb][e], 30 - ex))));
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {                    // (four numbers' bytes to four planes)
+            const uint32_t l01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x05010400u), h01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x07030602u);
+            const uint32_t l23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x05010400u), h23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x07030602u);
+            plane[0][f] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
+            plane[1][f] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
+            plane[2][f] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
+            plane[3][f] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+          }
+#pragma unroll
+          for (int by = 0; by < 4; ++by)
+            *reinterpret_cast<uint2*>(q_dig + (local * 16 + g4 * 4 + by) * kDigitRow + nb * kPageBlock + n16 * 8) = make_uint2(plane[by][0], plane[by][1]);
+        }
+        const float scale = (__ballot(bad) >> (g4 * 16) & 0xffffu) != 0 ? __builtin_nanf("") : ldexpf(1.0f, ex - 30 - kShift);
+        if (n16 == 0)
+          rows[local * kRowHeads + g4] = QueryRow{scale, scale * 65536.0f, static_cast<float>(zterm + static_cast<double>(now.lse) * 1.4426950408889634074),
+                                                  now.end};
       }
-      QueryRow row;
-      row.scale = __ballot(bad) != 0 ? __builtin_nanf("") : ldexpf(1.0f, e - 30 - kShift);
-      const float lse = a.lse[q_row * a.n_q + q_head];
-      row.off = static_cast<float>(z + static_cast<double>(lse) * 1.4426950408889634074);
-      row.end = there ? len - (a.queries - 1 - query) : 0;
-      row.unused = 0;
-      if (lane == 0) rows[i] = row;
     }
     __syncthreads();
 
@@ -162,71 +219,101 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightArgs a, We
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) expand<BITS>(kr[r][nb], kw[r][nb]);
-      id = next_id;
-      if (k + 1 < my_tiles) load_tile(k + 1, id, kr);
-      next_id = k + 2 < my_tiles ? page_of(k + 2) : -1;
-      // lane (row g4, token n16 of every 16): tokens of the r-th 16 that there are, before the row's own end
-      int first_of[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) first_of[r] = here >> r & 1 ? token + r * 16 + n16 : 0x7fffffff;
+      for (int e = 0; e < HEADS; ++e) old[e] = old_next[e];
+      // (the next tile's: weights first, loads come back in order)
+      if (k + 1 < my_tiles) {
+        id = page_of(k + 1, next_page);
+        if (k + 2 < my_tiles) next_page = page_at(k + 2);
+        load_old(k + 1);
+        load_keys(k + 1, id);
+      }
+      // lane (row g4, token n16 of every 16): tokens of the r-th 16 that there are
+      int token_r[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) token_r[r] = here >> r & 1 ? token + r * 16 + n16 : 0x7fffffff;
 
-      for (int tile = tile0; tile < tile1;) {
-        const int set = tile / plan.set_tiles, set_end = min((set + 1) * plan.set_tiles, tile1);
-        const bool first = tile == set * plan.set_tiles;
-        // what this lane will write of the set: 4 / group of its tokens, of head `head`
-        const int head = set * set_heads + (g4 >> group_shift);
-        const int64_t at = (static_cast<int64_t>(b) * a.n_kv + unit * unit_heads + head) * a.capacity;
-        const int r0 = (g4 & (plan.group - 1)) * set_heads;
-        float old[4];
+      const bool whole = (here & 15) == 15 && token + kTile <= len - (a.queries - 1) && full_rows;
+      // Adds the weights of row tiles from .. to - 1 to `sum`; the next one's rows are read while one is worked on.
+      auto add_up = [&](int from, int to, float (&sum)[4], auto&& seen) __attribute__((always_inline)) {
+        struct Operands {
+          QueryRow row;
+          v4i q[NB][2];
+        };
+        auto fetch = [&](int i) __attribute__((always_inline)) {
+          Operands o;
+          o.row = rows[i * kRowHeads + g4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int t = token + (r0 + j) * 16 + n16;
-          old[j] = 0.0f;
-          if (j < set_heads && head < unit_heads && t < len && !(first && t >= len - a.fresh)) old[j] = a.weights[at + t];
-        }
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (; tile < set_end; ++tile) {
-          const int i = tile - tile0;
-          const QueryRow row = rows[i * kRowHeads + g4];
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              o.q[nb][s] = *reinterpret_cast<const v4i*>(q_dig + (i * 16 + n16) * kDigitRow + nb * kPageBlock + g4 * 32 + s * 16);
+          return o;
+        };
+        Operands next = fetch(min(from, kHeld - 1));
+        for (int i = from; i < to; ++i) {
+          const Operands o = next;
+          if (NB == 1) next = fetch(min(i + 1, kHeld - 1));
           v4i c[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) c[r] = v4i{0, 0, 0, 0};
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const v4i q = *reinterpret_cast<const v4i*>(q_dig + (i * 16 + n16) * kDigitRow + nb * kPageBlock + g4 * 32 + s * 16);
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const v4i w = {static_cast<int>(kw[r][nb][4 * s]), static_cast<int>(kw[r][nb][4 * s + 1]), static_cast<int>(kw[r][nb][4 * s + 2]),
                                static_cast<int>(kw[r][nb][4 * s + 3])};
-                c[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q, w, c[r], 0, 0, 0);
+                c[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.q[nb][s], w, c[r], 0, 0, 0);
               }
-            }
+          if (NB > 1) next = fetch(min(i + 1, kHeld - 1));
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(undigit(c[r]), row.scale, -row.off));
-            sum[r] += first_of[r] < row.end ? p : 0.0f;
+            // (the small half and lse first: one rounding each)
+            const float low = fmaf(static_cast<float>(c[r][1] * 256 + c[r][0]), o.row.low, -o.row.off);
+            sum[r] += seen(__builtin_amdgcn_exp2f(fmaf(static_cast<float>(c[r][3] * 256 + c[r][2]), o.row.high, low)), r, o.row.end);
           }
         }
-        if (plan.group >= 2) {
+      };
+
+      float got[HEADS];
+#pragma unroll
+      for (int e = 0; e < HEADS; ++e) got[e] = 0.0f;
+#pragma unroll
+      for (int e0 = 0; e0 < HEADS; ++e0) {                 // (slots of a set begin at a multiple of set_heads)
+        if (HEADS > 1 && (e0 & (set_heads - 1)) != 0) continue;
+        const int set = HEADS == 1 ? 0 : e0 / set_heads;
+        const int from = max(set * plan.set_tiles, tile0) - tile0, to = min((set + 1) * plan.set_tiles, tile1) - tile0;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (whole) add_up(from, to, sum, [&](float p, int, int) { return p; });
+        else add_up(from, to, sum, [&](float p, int r, int end) { return token_r[r] < end ? p : 0.0f; });
+        // the rows of a head together
+        if (HEADS == 1 || group >= 2) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) sum[r] += __shfl_xor(sum[r], 16, kWave);
         }
-        if (plan.group == 4) {
+        if (HEADS == 1 || group == 4) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) sum[r] += __shfl_xor(sum[r], 32, kWave);
         }
-        if (head < unit_heads) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = r0 + j, t = token + r * 16 + n16;
-            if (j >= set_heads || t >= len) continue;
-            const float mine = r == 0 ? sum[0] : (r == 1 ? sum[1] : (r == 2 ? sum[2] : sum[3]));
-            a.weights[at + t] = old[j] + mine;
-            if (first && t >= len - a.fresh) a.token_positions[at + t] = a.positions ? a.positions[b] - (len - 1 - t) : t;
-          }
+        for (int j = 0; j < HEADS; ++j) {
+          if (j < e0 || (HEADS > 1 && j >= e0 + set_heads)) continue;
+          const int r = slot_group(j);
+          got[j] = r == 0 ? sum[0] : (r == 1 ? sum[1] : (r == 2 ? sum[2] : sum[3]));
         }
+      }
+      // (a head's first row tiles set what starts here, later ones add to it)
+#pragma unroll
+      for (int e = 0; e < HEADS; ++e) {
+        const int t = slot_token(k, e), set = HEADS == 1 ? 0 : e / set_heads;
+        const int64_t at = first_at + slot_head(e) * a.capacity + t;
+        const bool first = set * plan.set_tiles >= tile0, any = first ? set * plan.set_tiles < tile1 : (set + 1) * plan.set_tiles > tile0;
+        const bool starts = first && t >= len - a.fresh;
+        if (!any || t >= len) continue;
+        a.weights[at] = (starts ? 0.0f : old[e]) + got[e];
+        if (starts) a.token_positions[at] = a.positions ? a.positions[b] - (len - 1 - t) : t;
       }
     }
   }
@@ -234,25 +321,24 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightArgs a, We
 
 int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st) {
   if (a.B == 0) return RPTQ_OK;
-  const int P = a.hd > kPageBlock ? a.hd : kPageBlock, units = a.n_kv * a.hd / P, unit_heads = P / a.hd;
+  const int P = a.hd > kPageBlock ? a.hd : kPageBlock, units = a.n_kv * a.hd / P, heads = P / a.hd;
   const int pairs = a.n_q / a.n_kv * a.queries;
   WeightPlan p;
-  p.group = pairs >= 3 ? 4 : pairs;
+  p.share = a.n_q / a.n_kv;
+  p.group = std::max(pairs >= 3 ? 4 : pairs, kRowHeads / heads);         // (not less than gives every lane a weight to write)
   p.set_tiles = (pairs + p.group - 1) / p.group;
-  p.tiles = p.set_tiles * ((unit_heads + kRowHeads / p.group - 1) / (kRowHeads / p.group));
+  p.per_share = 1.0 / p.share * (1.0 + 0x1p-50);
+  p.per_set = 1.0 / p.set_tiles * (1.0 + 0x1p-50);
+  p.tiles = p.set_tiles * (heads / (kRowHeads / p.group));
   const int64_t most = std::min<int64_t>(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
   const int64_t runs = (most + kTileTokens - 1) / kTileTokens, each = static_cast<int64_t>(a.B) * units;
   p.parts = static_cast<int32_t>(std::min<int64_t>(runs, std::max<int64_t>(1, (kSeenWorkgroups + each - 1) / each)));
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(p.parts, units, a.B), dim3(256), 0, st, a, p); };
-  if (a.hd > kPageBlock) {
-    if (bits == 3) go(attend_weights_kernel<3, 2>);
-    else if (bits == 4) go(attend_weights_kernel<4, 2>);
-    else go(attend_weights_kernel<8, 2>);
-  } else {
-    if (bits == 3) go(attend_weights_kernel<3, 1>);
-    else if (bits == 4) go(attend_weights_kernel<4, 1>);
-    else go(attend_weights_kernel<8, 1>);
-  }
+  auto by_bits = [&](auto k3, auto k4, auto k8) { bits == 3 ? go(k3) : (bits == 4 ? go(k4) : go(k8)); };
+  if (a.hd > kPageBlock) by_bits(attend_weights_kernel<3, 2, 1>, attend_weights_kernel<4, 2, 1>, attend_weights_kernel<8, 2, 1>);
+  else if (heads == 1) by_bits(attend_weights_kernel<3, 1, 1>, attend_weights_kernel<4, 1, 1>, attend_weights_kernel<8, 1, 1>);
+  else if (heads == 2) by_bits(attend_weights_kernel<3, 1, 2>, attend_weights_kernel<4, 1, 2>, attend_weights_kernel<8, 1, 2>);
+  else by_bits(attend_weights_kernel<3, 1, 4>, attend_weights_kernel<4, 1, 4>, attend_weights_kernel<8, 1, 4>);
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;
 }
