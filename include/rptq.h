@@ -537,6 +537,8 @@ int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t 
  * positions[b] - (lens[b] - 1 - t), positions[b] being the newest token's, or to t where positions is NULL.
  *   q       device bf16 [B * queries, n_q_heads * head_dim], rows ld_q apart, sequence after sequence, oldest query first
  *   lse     device fp32 [B * queries, n_q_heads];  positions device int32 [B] or NULL
+ *   workspace device, rptq_attend_weights_paged_workspace_bytes(B, queries, n_q_heads, n_kv_heads, head_dim) bytes, nothing to clear or keep;
+ *           that may be none (a few queries), then it may be NULL
  *   1 <= queries <= RPTQ_MAX_WINDOW; fresh >= 0; the others as for rptq_attend_paged.  Sums are fp32, in an order that the call alone
  *   decides.  A NaN or infinity in q makes the weights of the tokens that it sees NaN.  Sequences that share pages keep records of their own.
  *
@@ -558,11 +560,13 @@ int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t 
  */
 #define RPTQ_MAX_WINDOW 65536
 #define RPTQ_MAX_TRACKED_HEADS 2097152
+size_t rptq_attend_weights_paged_workspace_bytes(int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
                                   int32_t head_dim, float scale, const void* k_table, int32_t bits, const void* k_pages,
                                   int64_t n_pages, int32_t page_size, const int32_t* page_table, int64_t ld_page_table,
                                   int32_t pages_per_seq, const int32_t* lens, const float* lse, const int32_t* positions, int32_t fresh,
-                                  float* weights, int32_t* token_positions, int64_t capacity, void* stream);
+                                  float* weights, int32_t* token_positions, int64_t capacity, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 size_t rptq_evict_paged_workspace_bytes(int32_t B, int32_t n_kv_heads, int64_t capacity, int32_t budget);
 int32_t rptq_evict_paged(int32_t B, int32_t n_kv_heads, int32_t head_dim, int32_t bits, void* k_pages, void* v_pages, int64_t n_pages,
                          int32_t page_size, const int32_t* page_table, int64_t ld_page_table, int32_t pages_per_seq,

@@ -27,7 +27,8 @@ EXPORTED_SYMBOLS = (
     "rptq_cluster_channels", "rptq_cluster_heads", "rptq_kv_table_bytes", "rptq_kv_tables", "rptq_kv_quant",
     "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
     "rptq_attend_paged_workspace_bytes", "rptq_attend_paged", "rptq_rope_freqs", "rptq_rope", "rptq_rope_quant_paged",
-    "rptq_attend_weights_paged", "rptq_evict_paged_workspace_bytes", "rptq_evict_paged", "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
+    "rptq_attend_weights_paged_workspace_bytes", "rptq_attend_weights_paged", "rptq_evict_paged_workspace_bytes", "rptq_evict_paged",
+    "rptq_dequant_codes", "rptq_dequant_weights", "rptq_gemm_bf16", "rptq_device_info", "rptq_strerror", "rptq_last_hip_error", "rptq_version",
 )
 
 _LIB = None
@@ -115,7 +116,8 @@ def load_library():
         "rptq_rope_quant_paged": (i32, [vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, i32, i32, vp, i32, i32, vp, f64, vp, vp, i32, vp,
                                         vp, vp, i64, i32, vp]),
         "rptq_attend_weights_paged": (i32, [vp, i64, i32, i32, i32, i32, i32, f32, vp, i32, vp, i64, i32, vp, i64, i32, vp, vp, vp, i32,
-                                            vp, vp, i64, vp]),
+                                            vp, vp, i64, vp, sz, vp]),
+        "rptq_attend_weights_paged_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
         "rptq_evict_paged_workspace_bytes": (sz, [i32, i32, i64, i32]),
         "rptq_evict_paged": (i32, [i32, i32, i32, i32, vp, vp, i64, i32, vp, i64, i32, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp,
                                    sz, vp]),
@@ -844,13 +846,18 @@ def _sequences(page_table, lens):
     return at, ld, page_table.shape[1], _whole(lens, torch.int32, "lens", 0), lens.shape[0]
 
 
+def rptq_attend_weights_paged_workspace_bytes(B: int, queries: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(load_library().rptq_attend_weights_paged_workspace_bytes(B, queries, n_q_heads, n_kv_heads, head_dim))
+
+
 def rptq_attend_weights_paged(q, queries: int, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, k_table, bits: int, k_pages,
-                              page_size: int, page_table, lens, lse, positions, fresh: int, weights, token_positions, stream=None):
+                              page_size: int, page_table, lens, lse, positions, fresh: int, weights, token_positions, workspace=None,
+                              stream=None):
     """q: bf16 [B * queries, n_q_heads * head_dim], rows of any stride; lse: fp32 [B * queries, n_q_heads]; positions: int32 [B] or
-    None; weights, token_positions: fp32 and int32 [B, n_kv_heads, capacity]."""
+    None; weights, token_positions: fp32 and int32 [B, n_kv_heads, capacity]; workspace: where that many queries need one."""
     st = None if _CALLS is None else _CALLS.attend_weights_paged(
         q, queries, n_q_heads, n_kv_heads, head_dim, scale, k_table, bits, k_pages, page_size, page_table, lens, lse, positions, fresh,
-        weights, token_positions, stream)
+        weights, token_positions, workspace, stream)
     if st is None:
         import torch
         d = n_kv_heads * head_dim
@@ -863,7 +870,9 @@ def rptq_attend_weights_paged(q, queries: int, n_q_heads: int, n_kv_heads: int, 
         st = load_library().rptq_attend_weights_paged(
             qa, ld_q, B, queries, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d), bits, kp, n_pages,
             page_size, pa, ld_pt, per_seq, la, _whole(lse, torch.float32, "lse", 0),
-            None if positions is None else _row_positions(positions, B), fresh, wa, ta, capacity, _stream(stream)) if B else 0
+            None if positions is None else _row_positions(positions, B), fresh, wa, ta, capacity,
+            None if workspace is None else _whole(workspace, None, "workspace", 0),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_weights_paged")
 
 

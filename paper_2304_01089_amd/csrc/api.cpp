@@ -527,11 +527,17 @@ static bool page_table_ok(int32_t pages_per_seq, int64_t ld_page_table, int32_t 
   return pages_per_seq >= 1 && ld_page_table >= pages_per_seq && static_cast<int64_t>(pages_per_seq) * page_size <= (INT64_C(1) << 29);
 }
 
+size_t rptq_attend_weights_paged_workspace_bytes(int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (!attend_heads_ok(B, n_q_heads, n_kv_heads, head_dim) || queries < 1 || queries > RPTQ_MAX_WINDOW) return 0;
+  return attend_weights_workspace_bytes(B, queries, n_q_heads, n_kv_heads, head_dim);
+}
+
 int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
                                   int32_t head_dim, float scale, const void* k_table, int32_t bits, const void* k_pages,
                                   int64_t n_pages, int32_t page_size, const int32_t* page_table, int64_t ld_page_table,
                                   int32_t pages_per_seq, const int32_t* lens, const float* lse, const int32_t* positions, int32_t fresh,
-                                  float* weights, int32_t* token_positions, int64_t capacity, void* stream) {
+                                  float* weights, int32_t* token_positions, int64_t capacity, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
   if (!q || !k_table || !k_pages || !page_table || !lens || !lse || !weights || !token_positions) return RPTQ_ERR_NULL;
   if (int32_t st = check_bits(bits)) return st;
   if (!attend_heads_ok(B, n_q_heads, n_kv_heads, head_dim)) return RPTQ_ERR_SHAPE;
@@ -542,8 +548,10 @@ int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_
     return RPTQ_ERR_SHAPE;
   if (!std::isfinite(scale)) return RPTQ_ERR_RANGE;
   if (!aligned16(q) || !aligned16(k_table) || !aligned16(k_pages) || !aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_to(lse, 4) ||
-      !aligned_to(positions, 4) || !aligned_to(weights, 4) || !aligned_to(token_positions, 4))
+      !aligned_to(positions, 4) || !aligned_to(weights, 4) || !aligned_to(token_positions, 4) || !aligned16(workspace))
     return RPTQ_ERR_ALIGN;
+  const size_t bytes = attend_weights_workspace_bytes(B, queries, n_q_heads, n_kv_heads, head_dim);
+  if (bytes > 0 && (!workspace || workspace_bytes < bytes)) return RPTQ_ERR_WORKSPACE;
   a.q = static_cast<const uint16_t*>(q);
   a.ld_q = ld_q;
   a.B = B;
@@ -564,6 +572,7 @@ int32_t rptq_attend_weights_paged(const void* q, int64_t ld_q, int32_t B, int32_
   a.weights = weights;
   a.token_positions = token_positions;
   a.capacity = capacity;
+  a.workspace = workspace;
   return launch_attend_weights(a, bits, static_cast<hipStream_t>(stream));
 }
 

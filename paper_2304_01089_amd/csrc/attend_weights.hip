@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_common.h"
 #include "device_common.h"
@@ -21,6 +22,10 @@ namespace rptq {
 
 constexpr int kTileTokens = 4 * kTile;         // of a workgroup's four waves
 constexpr int kSeenWorkgroups = 2048;          // as many parts as make this many workgroups, where there are tokens for them
+
+constexpr int kFewTiles = 4;                   // row tiles of which each wave of a workgroup makes one
+
+constexpr int kSide = 2;                       // row tiles that a wave works on side by side
 
 // Row tiles whose digits lie in LDS at one time; more go through the tokens several times.
 __host__ __device__ constexpr int held_tiles(int blocks) { return blocks == 2 ? 8 : 16; }
@@ -38,37 +43,139 @@ struct QueryRow {
   int32_t end;                                 // tokens that the query sees
 };
 
-// NB: blocks of a unit; HEADS: key/value heads of a unit
+typedef int i4v __attribute__((ext_vector_type(4)));
+
+// Queries to digits: a wave makes row tile number `tile` of a unit's, 16 lanes a row, a lane eight positions of every block.
 template <int BITS, int NB, int HEADS>
-__global__ void __launch_bounds__(256, NB == 2 ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
-  constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
+struct QueryDigits {
+  static constexpr int kShift = BITS == 8 ? 0 : (BITS == 4 ? 4 : 5);
+  static constexpr int P = NB * kPageBlock, kHd = P / HEADS;
+  const WeightArgs& a;
+  const WeightPlan& plan;
+  int b, unit, len, group, g4, n16;
+  i4v kp[NB][8];                                           // the lane's positions' records
+  struct Query {
+    int end;                                               // 0: no query
+    bool own;                                              // whether the lane's positions are its head's
+    float lse;
+    uint16_t raw[NB][8];
+  };
+  __device__ __forceinline__ Query request(int tile) const {
+    // (pairs and tiles are below 2^31, a quotient's fraction is a multiple of its divisor's inverse or 0: 2^-50 of it does not reach the next number)
+    auto quotient = [](int n, double per) { return static_cast<int>(n * per); };
+    Query r;
+    const int set = HEADS == 1 ? 0 : quotient(tile, plan.per_set), in_set = tile - set * plan.set_tiles;
+    const int head = set * (kRowHeads / group) + (g4 >> (group >> 1));         // of the unit
+    const int pair = in_set * group + (g4 & (group - 1));
+    const bool there = head < HEADS && pair < plan.share * a.queries;
+    const int query = there ? quotient(pair, plan.per_share) : 0;
+    const int q_head = (unit * HEADS + (there ? head : 0)) * plan.share + (there ? pair - query * plan.share : 0);
+    const int64_t q_row = static_cast<int64_t>(b) * a.queries + query;
+    const uint16_t* q = a.q + q_row * a.ld_q + q_head * kHd;
+    r.lse = a.lse[q_row * a.n_q + q_head];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.raw[nb][e] = q[kp[nb][e][0] & (kHd - 1)];
+    r.end = there ? len - (a.queries - 1 - query) : 0;
+    r.own = there && (NB == 2 || n16 * 8 / kHd == head);
+    return r;
+  }
+  // to: the tile's 16 rows, `stride` bytes apart
+  __device__ __forceinline__ QueryRow make(const Query& now, unsigned char* to, int stride) const {
+    const float to_log2 = a.scale * kLog2e;
+    float x[NB][8], top = 0.0f;
+    bool bad = false;
+    double zterm = 0.0;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = __uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16) * __int_as_float(kp[nb][e][2]) * to_log2;
+        x[nb][e] = now.own ? v : 0.0f;
+        top = fmaxf(top, fabsf(x[nb][e]));
+        bad = bad || !(fabsf(x[nb][e]) < __builtin_huge_valf());
+        zterm = fma(static_cast<double>(x[nb][e]), static_cast<double>(kp[nb][e][3]), zterm);
+      }
+    top = row16_max(top);
+    zterm = row16_sum(zterm);
+    const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;          // top < 2^ex
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      uint32_t d[8], plane[4][2];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = digits(static_cast<int>(rintf(ldexpf(x[nb][e], 30 - ex))));
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {                        // (four numbers' bytes to four planes)
+        const uint32_t l01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x05010400u), h01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x07030602u);
+        const uint32_t l23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x05010400u), h23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x07030602u);
+        plane[0][f] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
+        plane[1][f] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
+        plane[2][f] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
+        plane[3][f] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+      }
+#pragma unroll
+      for (int by = 0; by < 4; ++by)
+        *reinterpret_cast<uint2*>(to + (g4 * 4 + by) * stride + nb * kPageBlock + n16 * 8) = make_uint2(plane[by][0], plane[by][1]);
+    }
+    const float scale = (__ballot(bad) >> (g4 * 16) & 0xffffu) != 0 ? __builtin_nanf("") : ldexpf(1.0f, ex - 30 - kShift);
+    return QueryRow{scale, scale * 65536.0f, static_cast<float>(zterm + static_cast<double>(now.lse) * 1.4426950408889634074), now.end};
+  }
+};
+
+// Workspace, where there are more than kFewTiles row tiles: per (sequence, unit, tile) 16 rows of P digits and four QueryRows.
+template <int NB>
+__host__ __device__ constexpr int made_bytes() { return NB * 16 * kPageBlock + static_cast<int>(kRowHeads * sizeof(QueryRow)); }
+
+__device__ __forceinline__ int tokens_of(const WeightArgs& a, int length) {
+  const int64_t room = min(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
+  return static_cast<int>(min(static_cast<int64_t>(max(length, 0)), room));
+}
+
+// A wave makes one tile's digits.
+template <int BITS, int NB, int HEADS>
+__global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightPlan plan) {
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
+  const int tile = static_cast<int>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = blockIdx.y, b = blockIdx.z;
+  if (tile >= plan.tiles) return;
+  const int len = tokens_of(a, a.lens[b]);
+  if (len == 0) return;
+  QueryDigits<BITS, NB, HEADS> maker{a, plan, b, unit, len, HEADS == 1 ? 4 : plan.group, g4, n16, {}};
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      maker.kp[nb][e] = *reinterpret_cast<const i4v*>(a.k_pos + unit * maker.P + nb * kPageBlock + n16 * 8 + e);
+  unsigned char* to = static_cast<unsigned char*>(a.workspace) + ((static_cast<int64_t>(b) * gridDim.y + unit) * plan.tiles + tile) * made_bytes<NB>();
+  const QueryRow row = maker.make(maker.request(tile), to, maker.P);
+  if (n16 == 0) reinterpret_cast<QueryRow*>(to + 16 * maker.P)[g4] = row;
+}
+
+// NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace
+template <int BITS, int NB, int HEADS, bool MADE>
+__global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
-  constexpr int kHd = P / HEADS;
   constexpr int kDigitRow = P + 16;                        // (16 more: other banks)
-  constexpr int kHeld = held_tiles(NB);
+  constexpr int kHeld = MADE ? held_tiles(NB) : kFewTiles;
   __shared__ __align__(16) unsigned char q_dig[kHeld * 16 * kDigitRow];
   __shared__ __align__(16) QueryRow rows[kHeld * kRowHeads];
-  __shared__ __align__(16) unsigned char table[P / 8 * 144];           // eight positions' records, and 16 bytes (banks)
+  __shared__ __align__(16) unsigned char table[MADE ? 16 : P / 8 * 144];         // eight positions' records, and 16 bytes (banks)
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = blockIdx.x, unit = blockIdx.y, b = blockIdx.z;
-  const int64_t room = min(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
   // (requested first, all at once: the length, the first two tiles' pages, the positions' records)
   const int length = a.lens[b];
   const int32_t* pt = a.page_table + b * a.ld_pt;
   auto token_of = [&](int k) { return (part + k * plan.parts) * kTileTokens + wave * kTile; };
   auto page_at = [&](int k) { return pt[min((token_of(k) + (lane & 3) * 16) >> a.g.page_shift, a.pages_per_seq - 1)]; };
   const int page0 = page_at(0), page1 = page_at(1);
-  typedef int i4v __attribute__((ext_vector_type(4)));
-  const i4v record = reinterpret_cast<const i4v*>(a.k_pos + unit * P)[threadIdx.x & (P - 1)];
-  const int len = static_cast<int>(min(static_cast<int64_t>(max(length, 0)), room));
+  i4v record;
+  if (!MADE) record = reinterpret_cast<const i4v*>(a.k_pos + unit * P)[threadIdx.x & (P - 1)];
+  const int len = tokens_of(a, length);
   if (part * kTileTokens >= len) return;
 
   const int share = plan.share, pairs = share * a.queries;
-  // (pairs and tiles are below 2^31, a quotient's fraction is a multiple of its divisor's inverse or 0: 2^-50 of it does not reach the next number)
-  const double by_share = plan.per_share, by_set = plan.per_set;
-  auto quotient = [](int n, double per) { return static_cast<int>(n * per); };
   const int group = HEADS == 1 ? 4 : plan.group, group_shift = group >> 1;                 // (log2 of 1, 2, 4)
   const int set_heads = kRowHeads / group;
   const bool full_rows = pairs % group == 0;               // (no row without a query)
@@ -125,88 +232,39 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 3) attend_weights_kernel(We
   for (int tile0 = 0; tile0 < plan.tiles; tile0 += kHeld) {
     const int tile1 = min(tile0 + kHeld, plan.tiles);
     int id = page_of(0, page0), next_page = page1;
-    if (tile0 == 0) *reinterpret_cast<i4v*>(table + (threadIdx.x & (P - 1)) * 16 + (threadIdx.x & (P - 1)) / 8 * 16) = record;
-    __syncthreads();                                       // (later: the digits before have been read)
-
-    // ---- queries to digits: a wave takes every fourth row tile, 16 lanes a row, a lane eight positions of a block -----------
-    {
-      i4v kp[NB][8];
+    if (my_tiles > 0) {
+      load_old(0);
+      load_keys(0, id);
+    }
+    if constexpr (MADE) {
+      // 16 bytes of a row at a time, rows P apart there and kDigitRow apart here
+      constexpr int kPieces = made_bytes<NB>() / 16;
+      const i4v* from = reinterpret_cast<const i4v*>(static_cast<const unsigned char*>(a.workspace) +
+                                                         ((static_cast<int64_t>(b) * gridDim.y + unit) * plan.tiles + tile0) * made_bytes<NB>());
+      constexpr int kEach = (kHeld * kPieces + 255) / 256;
+      const int pieces = (tile1 - tile0) * kPieces;
+      i4v v[kEach];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int k = 0; k < kEach; ++k) v[k] = from[min(k * 256 + static_cast<int>(threadIdx.x), pieces - 1)];
+      if (tile0 > 0) __syncthreads();                      // (the digits before have been read)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kp[nb][e] = *reinterpret_cast<const i4v*>(table + (nb * 16 + n16) * 144 + e * 16);
-      const float to_log2 = a.scale * kLog2e;
-      struct Query {
-        int end;                                           // 0: no query
-        bool own;                                          // whether the lane's positions are its head's
-        float lse;
-        uint16_t raw[NB][8];
-      };
-      auto request = [&](int tile) __attribute__((always_inline)) {
-        Query r;
-        const int set = HEADS == 1 ? 0 : quotient(tile, by_set), in_set = tile - set * plan.set_tiles;
-        const int head = set * set_heads + (g4 >> group_shift);                // of the unit
-        const int pair = in_set * group + (g4 & (group - 1));
-        const bool there = head < HEADS && pair < pairs;
-        const int query = there ? quotient(pair, by_share) : 0, q_head = (unit * HEADS + (there ? head : 0)) * share + (there ? pair - query * share : 0);
-        const int64_t q_row = static_cast<int64_t>(b) * a.queries + query;
-        const uint16_t* q = a.q + q_row * a.ld_q + q_head * kHd;
-        r.lse = a.lse[q_row * a.n_q + q_head];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r.raw[nb][e] = q[kp[nb][e][0] & (kHd - 1)];
-        r.end = there ? len - (a.queries - 1 - query) : 0;
-        r.own = there && (NB == 2 || n16 * 8 / kHd == head);
-        return r;
-      };
-      if (my_tiles > 0) {
-        load_old(0);
-        load_keys(0, id);
+      for (int k = 0; k < kEach; ++k) {
+        const int i = k * 256 + static_cast<int>(threadIdx.x);
+        const int tile = i / kPieces, at = i - tile * kPieces, row = at / (P / 16);
+        unsigned char* to = row < 16 ? q_dig + (tile * 16 + row) * kDigitRow : reinterpret_cast<unsigned char*>(rows + tile * kRowHeads);
+        if (i < pieces) *reinterpret_cast<i4v*>(to + (at & (P / 16 - 1)) * 16) = v[k];
       }
-      Query next = request(min(tile0 + wave, tile1 - 1));
-      for (int tile = tile0 + wave; tile < tile1; tile += 4) {
-        const Query now = next;
-        next = request(min(tile + 4, tile1 - 1));
-        float x[NB][8], top = 0.0f;
-        bool bad = false;
-        double zterm = 0.0;
+    } else {
+      *reinterpret_cast<i4v*>(table + (threadIdx.x & (P - 1)) * 16 + (threadIdx.x & (P - 1)) / 8 * 16) = record;
+      __syncthreads();
+      if (wave < tile1) {
+        QueryDigits<BITS, NB, HEADS> maker{a, plan, b, unit, len, group, g4, n16, {}};
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float v = __uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16) * __int_as_float(kp[nb][e][2]) * to_log2;
-            x[nb][e] = now.own ? v : 0.0f;
-            top = fmaxf(top, fabsf(x[nb][e]));
-            bad = bad || !(fabsf(x[nb][e]) < __builtin_huge_valf());
-            zterm = fma(static_cast<double>(x[nb][e]), static_cast<double>(kp[nb][e][3]), zterm);
-          }
-        top = row16_max(top);
-        zterm = row16_sum(zterm);
-        const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;      // top < 2^ex
-        const int local = tile - tile0;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          uint32_t d[8], plane[4][2];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[e] = digits(static_cast<int>(rintf(ldexpf(x[nb][e], 30 - ex))));
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {                    // (four numbers' bytes to four planes)
-            const uint32_t l01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x05010400u), h01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x07030602u);
-            const uint32_t l23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x05010400u), h23 = __builtin_amdgcn_perm(d[4 * f + 3], d[4 * f + 2], 0x07030602u);
-            plane[0][f] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
-            plane[1][f] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
-            plane[2][f] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
-            plane[3][f] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
-          }
-#pragma unroll
-          for (int by = 0; by < 4; ++by)
-            *reinterpret_cast<uint2*>(q_dig + (local * 16 + g4 * 4 + by) * kDigitRow + nb * kPageBlock + n16 * 8) = make_uint2(plane[by][0], plane[by][1]);
-        }
-        const float scale = (__ballot(bad) >> (g4 * 16) & 0xffffu) != 0 ? __builtin_nanf("") : ldexpf(1.0f, ex - 30 - kShift);
-        if (n16 == 0)
-          rows[local * kRowHeads + g4] = QueryRow{scale, scale * 65536.0f, static_cast<float>(zterm + static_cast<double>(now.lse) * 1.4426950408889634074),
-                                                  now.end};
+          for (int e = 0; e < 8; ++e) maker.kp[nb][e] = *reinterpret_cast<const i4v*>(table + (nb * 16 + n16) * 144 + e * 16);
+        const QueryRow row = maker.make(maker.request(wave), q_dig + wave * 16 * kDigitRow, kDigitRow);
+        if (n16 == 0) rows[wave * kRowHeads + g4] = row;
       }
     }
     __syncthreads();
@@ -250,31 +308,42 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 3) attend_weights_kernel(We
               o.q[nb][s] = *reinterpret_cast<const v4i*>(q_dig + (i * 16 + n16) * kDigitRow + nb * kPageBlock + g4 * 32 + s * 16);
           return o;
         };
-        Operands next = fetch(min(from, kHeld - 1));
-        for (int i = from; i < to; ++i) {
-          const Operands o = next;
-          if (NB == 1) next = fetch(min(i + 1, kHeld - 1));
-          v4i c[4];
+        // (the products of two row tiles side by side: with two waves per SIMD each is a chain of latencies)
+        auto some = [&](auto count, int i) __attribute__((always_inline)) {
+          constexpr int N = decltype(count)::value;
+          Operands o[N];
+          v4i c[N][4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) c[r] = v4i{0, 0, 0, 0};
+          for (int n = 0; n < N; ++n) {
+            o[n] = fetch(i + n);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) c[n][r] = v4i{0, 0, 0, 0};
+          }
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const v4i w = {static_cast<int>(kw[r][nb][4 * s]), static_cast<int>(kw[r][nb][4 * s + 1]), static_cast<int>(kw[r][nb][4 * s + 2]),
-                               static_cast<int>(kw[r][nb][4 * s + 3])};
-                c[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.q[nb][s], w, c[r], 0, 0, 0);
-              }
-          if (NB > 1) next = fetch(min(i + 1, kHeld - 1));
+              for (int n = 0; n < N; ++n)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            // (the small half and lse first: one rounding each)
-            const float low = fmaf(static_cast<float>(c[r][1] * 256 + c[r][0]), o.row.low, -o.row.off);
-            sum[r] += seen(__builtin_amdgcn_exp2f(fmaf(static_cast<float>(c[r][3] * 256 + c[r][2]), o.row.high, low)), r, o.row.end);
-          }
-        }
+                for (int r = 0; r < 4; ++r) {
+                  const v4i w = {static_cast<int>(kw[r][nb][4 * s]), static_cast<int>(kw[r][nb][4 * s + 1]), static_cast<int>(kw[r][nb][4 * s + 2]),
+                                 static_cast<int>(kw[r][nb][4 * s + 3])};
+                  c[n][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o[n].q[nb][s], w, c[n][r], 0, 0, 0);
+                }
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              // (the small half and lse first: one rounding each)
+              const float low = fmaf(static_cast<float>(c[n][r][1] * 256 + c[n][r][0]), o[n].row.low, -o[n].row.off);
+              sum[r] += seen(__builtin_amdgcn_exp2f(fmaf(static_cast<float>(c[n][r][3] * 256 + c[n][r][2]), o[n].row.high, low)), r, o[n].row.end);
+            }
+        };
+        int i = from;
+        if constexpr (MADE)
+          for (; i + kSide <= to; i += kSide) some(std::integral_constant<int, kSide>{}, i);
+        for (; i < to; ++i) some(std::integral_constant<int, 1>{}, i);
       };
 
       float got[HEADS];
@@ -319,26 +388,57 @@ __global__ void __launch_bounds__(256, NB == 2 ? 2 : 3) attend_weights_kernel(We
   }
 }
 
-int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st) {
-  if (a.B == 0) return RPTQ_OK;
-  const int P = a.hd > kPageBlock ? a.hd : kPageBlock, units = a.n_kv * a.hd / P, heads = P / a.hd;
-  const int pairs = a.n_q / a.n_kv * a.queries;
+static WeightPlan weight_plan(int32_t queries, int32_t n_q, int32_t n_kv, int32_t hd) {
+  const int heads = hd > kPageBlock ? 1 : kPageBlock / hd;
   WeightPlan p;
-  p.share = a.n_q / a.n_kv;
+  p.share = n_q / n_kv;
+  const int pairs = p.share * queries;
   p.group = std::max(pairs >= 3 ? 4 : pairs, kRowHeads / heads);         // (not less than gives every lane a weight to write)
   p.set_tiles = (pairs + p.group - 1) / p.group;
   p.per_share = 1.0 / p.share * (1.0 + 0x1p-50);
   p.per_set = 1.0 / p.set_tiles * (1.0 + 0x1p-50);
   p.tiles = p.set_tiles * (heads / (kRowHeads / p.group));
+  p.parts = 0;
+  return p;
+}
+
+size_t attend_weights_workspace_bytes(int32_t B, int32_t queries, int32_t n_q, int32_t n_kv, int32_t hd) {
+  const WeightPlan p = weight_plan(queries, n_q, n_kv, hd);
+  if (p.tiles <= kFewTiles) return 0;
+  const int64_t units = n_kv * hd / std::max(hd, kPageBlock);
+  return static_cast<size_t>(B * units * p.tiles) * (hd > kPageBlock ? made_bytes<2>() : made_bytes<1>());
+}
+
+int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st) {
+  if (a.B == 0) return RPTQ_OK;
+  const int P = a.hd > kPageBlock ? a.hd : kPageBlock, units = a.n_kv * a.hd / P, heads = P / a.hd;
+  WeightPlan p = weight_plan(a.queries, a.n_q, a.n_kv, a.hd);
   const int64_t most = std::min<int64_t>(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
   const int64_t runs = (most + kTileTokens - 1) / kTileTokens, each = static_cast<int64_t>(a.B) * units;
   p.parts = static_cast<int32_t>(std::min<int64_t>(runs, std::max<int64_t>(1, (kSeenWorkgroups + each - 1) / each)));
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(p.parts, units, a.B), dim3(256), 0, st, a, p); };
-  auto by_bits = [&](auto k3, auto k4, auto k8) { bits == 3 ? go(k3) : (bits == 4 ? go(k4) : go(k8)); };
-  if (a.hd > kPageBlock) by_bits(attend_weights_kernel<3, 2, 1>, attend_weights_kernel<4, 2, 1>, attend_weights_kernel<8, 2, 1>);
-  else if (heads == 1) by_bits(attend_weights_kernel<3, 1, 1>, attend_weights_kernel<4, 1, 1>, attend_weights_kernel<8, 1, 1>);
-  else if (heads == 2) by_bits(attend_weights_kernel<3, 1, 2>, attend_weights_kernel<4, 1, 2>, attend_weights_kernel<8, 1, 2>);
-  else by_bits(attend_weights_kernel<3, 1, 4>, attend_weights_kernel<4, 1, 4>, attend_weights_kernel<8, 1, 4>);
+  const dim3 grid(p.parts, units, a.B), makers((p.tiles + 3) / 4, units, a.B);
+  auto go = [&](auto digits, auto made, auto alone) {
+    if (p.tiles > kFewTiles) {
+      hipLaunchKernelGGL(digits, makers, dim3(256), 0, st, a, p);
+      hipLaunchKernelGGL(made, grid, dim3(256), 0, st, a, p);
+    } else {
+      hipLaunchKernelGGL(alone, grid, dim3(256), 0, st, a, p);
+    }
+  };
+#define RPTQ_GO(BITS, NB, HEADS) \
+  go(query_digits_kernel<BITS, NB, HEADS>, attend_weights_kernel<BITS, NB, HEADS, true>, attend_weights_kernel<BITS, NB, HEADS, false>)
+#define RPTQ_BY_BITS(NB, HEADS)                 \
+  do {                                          \
+    if (bits == 3) RPTQ_GO(3, NB, HEADS);       \
+    else if (bits == 4) RPTQ_GO(4, NB, HEADS);  \
+    else RPTQ_GO(8, NB, HEADS);                 \
+  } while (0)
+  if (a.hd > kPageBlock) RPTQ_BY_BITS(2, 1);
+  else if (heads == 1) RPTQ_BY_BITS(1, 1);
+  else if (heads == 2) RPTQ_BY_BITS(1, 2);
+  else RPTQ_BY_BITS(1, 4);
+#undef RPTQ_BY_BITS
+#undef RPTQ_GO
   RPTQ_HIP(hipGetLastError());
   return RPTQ_OK;
 }

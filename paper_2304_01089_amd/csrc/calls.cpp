@@ -492,16 +492,16 @@ struct Records {
 };
 
 // (q, queries, n_q_heads, n_kv_heads, head_dim, scale, k_table, bits, k_pages, page_size, page_table, lens, lse, positions, fresh, weights,
-//  token_positions, stream)
+//  token_positions, workspace, stream)
 PyObject* attend_weights_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Rows q, table;
   Pages p;
   Records w;
-  int64_t device, lse_bytes, shape[2];
+  int64_t device, lse_bytes, shape[2], ws_bytes = 0;
   int32_t queries, n_q, n_kv, hd, bits, page_size, fresh, *lens, *positions = nullptr;
   float scale, *lse;
-  void* stream;
-  if (n != 18 || f_attend_weights_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[1], &queries) || !get_i32(a[2], &n_q) ||
+  void *stream, *workspace = nullptr;
+  if (n != 19 || f_attend_weights_paged == nullptr || !get_place(a[18], &device, &stream) || !get_i32(a[1], &queries) || !get_i32(a[2], &n_q) ||
       !get_i32(a[3], &n_kv) || !get_i32(a[4], &hd) || !get_f32(a[5], &scale) || !get_i32(a[7], &bits) || !get_i32(a[9], &page_size) ||
       !get_i32(a[14], &fresh) || queries < 1 || n_q < 1 || n_kv < 1 || hd < 1 || !q.get(a[0], t_bf16, device) ||
       q.cols != static_cast<int64_t>(n_q) * hd || !table.get(a[10], t_i32, device) || table.rows > INT32_MAX || q.rows != table.rows * queries)
@@ -511,10 +511,11 @@ PyObject* attend_weights_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
       shape[1] != n_q || !w.get(a[15], a[16], device, table.rows, n_kv))
     Py_RETURN_NONE;
   if (a[13] != Py_None && !get_column(a[13], t_i32, device, table.rows, &positions)) Py_RETURN_NONE;
+  if (a[17] != Py_None && !get_whole(a[17], nullptr, device, &workspace, &ws_bytes)) Py_RETURN_NONE;
   return run([&] {
     return f_attend_weights_paged(q.at, q.ld, static_cast<int32_t>(table.rows), queries, n_q, n_kv, hd, scale, p.k_table, bits, p.k, p.n, page_size,
                                   static_cast<int32_t*>(table.at), table.ld, static_cast<int32_t>(table.cols), lens, lse, positions, fresh,
-                                  w.weights, w.positions, w.capacity, stream);
+                                  w.weights, w.positions, w.capacity, workspace, static_cast<size_t>(ws_bytes), stream);
   });
 }
 

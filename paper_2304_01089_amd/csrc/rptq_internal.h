@@ -214,7 +214,9 @@ struct WeightArgs {
   float* weights;
   int32_t* token_positions;
   int64_t capacity;
+  void* workspace;
 };
+size_t attend_weights_workspace_bytes(int32_t B, int32_t queries, int32_t n_q, int32_t n_kv, int32_t hd);
 int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st);
 struct EvictArgs {
   int32_t B, n_kv, hd, bits;

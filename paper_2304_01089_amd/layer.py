@@ -336,15 +336,27 @@ def cache_track(cache: PagedCache, batch: int, capacity: int) -> CacheTrack:
     return CacheTrack(torch.zeros(shape, dtype=torch.float32, device=dev), torch.zeros(shape, dtype=torch.int32, device=dev))
 
 
+def attend_weights_paged_workspace(cache: PagedCache, batch: int, n_q_heads: int, queries: int):
+    """Device memory for attend_weights_paged calls of such sizes, one call at a time; None where they need none."""
+    size = B.rptq_attend_weights_paged_workspace_bytes(batch, queries, n_q_heads, cache.n_heads, cache.head_dim)
+    if size == 0:
+        return None
+    import torch
+    return torch.empty(size, dtype=torch.uint8, device=cache.k_pages.device)
+
+
 def attend_weights_paged(cache: PagedCache, q, page_table, lens, lse, track: CacheTrack, positions=None, queries: int = 1, fresh: int = 1,
-                         scale=None):
+                         scale=None, workspace=None):
     """Adds what the last `queries` tokens of every sequence gave each of its tokens to the records.  q: [B * queries, n_q_heads *
     head_dim]; lse: what attend_paged left for these rows; the newest `fresh` tokens' records start here, the newest one's
     position being positions[b] (its index where None).  scale: attend_paged's."""
     cache._compared or cache.compare()
-    B.rptq_attend_weights_paged(q, queries, q.shape[1] // cache.head_dim, cache.n_heads, cache.head_dim,
+    n_q_heads = q.shape[1] // cache.head_dim
+    if workspace is None:
+        workspace = attend_weights_paged_workspace(cache, lens.shape[0], n_q_heads, queries)
+    B.rptq_attend_weights_paged(q, queries, n_q_heads, cache.n_heads, cache.head_dim,
                                 cache.head_dim ** -0.5 if scale is None else scale, cache.k_table, cache.bits, cache.k_pages, cache.page_size,
-                                page_table, lens, lse, positions, fresh, track.weights, track.positions)
+                                page_table, lens, lse, positions, fresh, track.weights, track.positions, workspace)
 
 
 def evict_paged_workspace(cache: PagedCache, batch: int, capacity: int, budget: int):

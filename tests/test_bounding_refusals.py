@@ -67,7 +67,7 @@ def test_rotated_writes_refused(lib):
 
 def test_accumulations_refused(lib):
     good = dict(q=F, ld_q=1024, B=4, queries=3, n_q=8, n_kv=2, hd=128, scale=0.1, k_table=F, bits=4, k_pages=F, n_pages=9, page=16, table=F, ld_pt=3,
-                per_seq=3, lens=F, lse=F, pos=F, fresh=1, weights=F, tpos=F, cap=48)
+                per_seq=3, lens=F, lse=F, pos=F, fresh=1, weights=F, tpos=F, cap=48, ws=None, ws_bytes=0)
     bad = [(n, None, NULL) for n in ("q", "k_table", "k_pages", "table", "lens", "lse", "weights", "tpos")]
     bad += [(n, OFF8, ALIGN) for n in ("q", "k_table", "k_pages")] + [(n, OFF2, ALIGN) for n in ("table", "lens", "lse", "pos", "weights", "tpos")]
     bad += [("bits", 5, BITS), ("B", -1, SHAPE), ("B", 32769, SHAPE), ("queries", 0, SHAPE), ("queries", 65537, SHAPE), ("n_q", 7, SHAPE), ("n_kv", 0, SHAPE),
@@ -77,10 +77,11 @@ def test_accumulations_refused(lib):
     def call(a):
         return lib.rptq_attend_weights_paged(a["q"], a["ld_q"], a["B"], a["queries"], a["n_q"], a["n_kv"], a["hd"], a["scale"], a["k_table"], a["bits"], a["k_pages"],
                                              a["n_pages"], a["page"], a["table"], a["ld_pt"], a["per_seq"], a["lens"], a["lse"], a["pos"], a["fresh"], a["weights"],
-                                             a["tpos"], a["cap"], None)
+                                             a["tpos"], a["cap"], a["ws"], a["ws_bytes"], None)
 
     refused(call, good, bad)
     refused(call, dict(good, page=4096, ld_pt=1 << 20), [("per_seq", (1 << 17) + 1, SHAPE)])
+    refused(call, dict(good, queries=100, ws=F, ws_bytes=1 << 30), [("ws", None, WORKSPACE), ("ws_bytes", 1000, WORKSPACE), ("ws", OFF8, ALIGN)])
 
 
 def test_evictions_refused(lib):
@@ -102,6 +103,11 @@ def test_evictions_refused(lib):
 
 
 def test_workspaces(lib):
+    assert rp.rptq_attend_weights_paged_workspace_bytes(4, 1, 8, 2, 128) == 0
+    assert rp.rptq_attend_weights_paged_workspace_bytes(4, 32, 8, 2, 128) >= 4 * 32 * 8 * 4 * 128       # (four digits of every query's value)
+    assert rp.rptq_attend_weights_paged_workspace_bytes(32768, 65536, 128, 1, 256) > 1 << 47
+    for a in ((-1, 1, 8, 2, 128), (4, 0, 8, 2, 128), (4, 65537, 8, 2, 128), (4, 1, 7, 2, 128), (4, 1, 8, 2, 100)):
+        assert rp.rptq_attend_weights_paged_workspace_bytes(*a) == 0
     assert rp.rptq_evict_paged_workspace_bytes(4, 2, 48, 10) >= 4 * 8
     few, many = (rp.rptq_evict_paged_workspace_bytes(4, 2, 100000, n) for n in (16, 50000))
     assert few < 1 << 10 and many >= 4 * 8 * 2 * 50000

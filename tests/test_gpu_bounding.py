@@ -498,7 +498,7 @@ def test_native_and_python_marshalling(rp, monkeypatch, entry):
     args, outs = {
         "rope": ((q, y, pos, 64, 32, True, freqs, 1.5, None), (y,)),
         "rope_quant_paged": ((q, q_out, k, v, pos, slots, 64, 32, False, freqs, 1.5, c.k_table, c.v_table, 4) + pages + (16, None), (q_out,) + pages),
-        "attend_weights_paged": ((q[:2], 1, 4, 2, 64, 0.125, c.k_table, 4, c.k_pages, 16, b.page_table, b.dev_lens, lse, b.dev_lens.clone(), 1, tw, tp, None), (tw, tp)),
+        "attend_weights_paged": ((q[:2], 1, 4, 2, 64, 0.125, c.k_table, 4, c.k_pages, 16, b.page_table, b.dev_lens, lse, b.dev_lens.clone(), 1, tw, tp, None, None), (tw, tp)),
         "evict_paged": ((2, 64, 4) + pages + (16, b.page_table, b.dev_lens, dev(w), dev(p), 20, 2, 5, ow, op, lens_out, ws, None), pages + (ow, op, lens_out)),
     }[entry]
     native, plain = getattr(binding._CALLS, entry), getattr(rp, "rptq_" + entry)
@@ -525,7 +525,7 @@ def test_native_and_python_marshalling(rp, monkeypatch, entry):
             if not (entry == "attend_weights_paged" and i == 13):
                 odd.append(None)
         elif a is None:
-            odd = [torch.cuda.current_stream()] if i == len(args) - 1 else [1]
+            odd = [torch.cuda.current_stream()] if i == len(args) - 1 else [1, c.k_pages.cpu()]
         elif isinstance(a, bool):
             odd = [1, 0, None]
         elif isinstance(a, float):
