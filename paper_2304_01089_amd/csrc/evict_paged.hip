@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_common.h"
 #include "device_common.h"
@@ -20,11 +21,16 @@
 
 namespace rptq {
 
-constexpr int kBins = 2048;                    // of eleven bits of a key
+constexpr int kFirstBins = 4096, kLaterBins = 1024;              // of twelve and of ten bits of a key
+constexpr int kFewItems = 8;                   // of a lane whose keys stay in registers
+constexpr int kLdsItems = 32;                  // of a lane whose keys lie in LDS
 constexpr int kHeldPages = 1024;               // page numbers of a sequence that are kept at hand
 constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them
 constexpr int kMoveChunks = 1024;              // workgroups of a head there at most
 constexpr uint32_t kSafe = 0xffffffffu, kNanKey = 0xfffffffeu;
+
+typedef unsigned Bytes16 __attribute__((ext_vector_type(4)));
+typedef unsigned Bytes8 __attribute__((ext_vector_type(2)));
 
 struct EvictPlan {
   int32_t most;                                // moves of a head at most
@@ -84,15 +90,23 @@ __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h
     const int64_t row = ((static_cast<int64_t>(page_of(t >> shift)) * blocks + block) << shift) + (t & ((1 << shift) - 1));
     return reinterpret_cast<V*>(pages + row * row_bytes);
   };
-  for (int i = first; i < end; i += 4 * step) {
-    const int i1 = min(i + step, end - 1), i2 = min(i + 2 * step, end - 1), i3 = min(i + 3 * step, end - 1);
-    const V x0 = *at(from[i]), x1 = *at(from[i1]), x2 = *at(from[i2]), x3 = *at(from[i3]);
-    V *y0 = at(to[i]), *y1 = at(to[i1]), *y2 = at(to[i2]), *y3 = at(to[i3]);
-    *y0 = x0;                                                  // (the last row several times, if need be: the same bytes)
-    *y1 = x1;
-    *y2 = x2;
-    *y3 = x3;
-  }
+  // (N at a time; the last row several times, if need be: the same bytes)
+  auto some = [&](auto count, int i) __attribute__((always_inline)) {
+    constexpr int N = decltype(count)::value;
+    V x[N];
+    V* y[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int j = min(i + k * step, end - 1);
+      x[k] = *at(from[j]);
+      y[k] = at(to[j]);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) *y[k] = x[k];
+  };
+  int i = first;
+  for (; i + 4 * step < end; i += 8 * step) some(std::integral_constant<int, 8>{}, i);
+  for (; i < end; i += 4 * step) some(std::integral_constant<int, 4>{}, i);
 }
 
 template <int THREADS, typename P>
@@ -100,8 +114,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictPlan& p
                                           int begin) {
   const int each = 2 * p.units, rows = THREADS / each, row = static_cast<int>(threadIdx.x) / each, which = static_cast<int>(threadIdx.x) - row * each;
   if (row >= rows) return;
-  if (p.vec == 16) move_pieces<uint4>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
-  else if (p.vec == 8) move_pieces<uint2>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
+  if (p.vec == 16) move_pieces<Bytes16>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
+  else if (p.vec == 8) move_pieces<Bytes8>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
   else move_pieces<uint32_t>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
 }
 
@@ -119,16 +133,23 @@ __device__ __forceinline__ int row16_add_int(int v) {
   return v + static_cast<int>(dpp_row<0x140>(static_cast<uint32_t>(v)));
 }
 
-// WAVES: of the workgroup; ITEMS: keys of a lane that stay in registers; LONG: a wave's tokens are more than 64 of those, whose keys are
-// made again whenever they are looked at
-template <int WAVES, int ITEMS, bool LONG>
+enum class Keys { registers, lds, made };      // where a token's key is when it is looked at again; made: from its record
+
+// WAVES: of the workgroup
+template <int WAVES, Keys KEYS>
 __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, EvictPlan plan) {
-  constexpr int kThreads = WAVES * 64;
-  __shared__ __align__(16) int32_t bins[3 * kBins];            // (later the lists of a few moves)
+  constexpr int kRun = KEYS == Keys::registers ? kFewItems : 16;             // of its items a lane works on so many together
+  constexpr int kThreads = WAVES * 64, kKeys = KEYS == Keys::lds ? kThreads * kLdsItems : 1;
+  constexpr int kAllBins = kFirstBins + 2 * kLaterBins;
+  __shared__ __align__(16) int32_t bins[kAllBins];             // (later the lists of a few moves)
+  __shared__ uint32_t key_lds[kKeys];
   __shared__ int32_t ids[kHeldPages];
-  __shared__ int32_t groups[3][64];                            // of 32 bins each
-  __shared__ int32_t sums[3][4][16];
-  static_assert(2 * kFewMoves <= 3 * kBins, "the lists take the bins' place");
+  __shared__ int32_t groups[3][64];                            // of a sixty-fourth of the bins each
+  __shared__ int32_t sums[3][2][16];
+  __shared__ uint32_t some[64];                                // keys of a bin that holds few
+  __shared__ uint32_t some_over[64];                           // those above, those not below
+  __shared__ int32_t some_count;
+  static_assert(2 * kFewMoves <= kAllBins, "the lists take the bins' place");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = blockIdx.x / a.n_kv, h = blockIdx.x - b * a.n_kv;
@@ -138,29 +159,33 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
   const int32_t* positions = a.positions + base;
   float* weights_out = a.weights_out + base;
   int32_t* positions_out = a.positions_out + base;
+  const bool w_apart = weights_out != weights, p_apart = positions_out != positions;
   int32_t* workspace = static_cast<int32_t*>(a.workspace);
   auto leave = [&] {                                           // the sequence as it is
     if (h == 0 && tid == 0) a.lens_out[b] = n;
     if (!plan.few && tid == 0) workspace[blockIdx.x] = 0;
-    if (weights_out != weights) copy<kThreads>(weights_out, weights, n);
-    if (positions_out != positions) copy<kThreads>(positions_out, positions, n);
+    if (w_apart) copy<kThreads>(weights_out, weights, n);
+    if (p_apart) copy<kThreads>(positions_out, positions, n);
   };
   if (n <= a.budget) {
     leave();
     return;
   }
 
-  // a wave's tokens: `items` times 64 consecutive ones
+  // a wave's tokens: `items` times 64 consecutive ones, several items at a time (a run)
   const int items = ((n + WAVES - 1) / WAVES + 63) >> 6, start = wave * items * 64;
-  float w[ITEMS];
-  int32_t pos[ITEMS];
-  auto read = [&](int first) __attribute__((always_inline)) {  // (beyond the end: the last token)
+  const int end = min(start + items * 64, n);
+  float w[kRun];
+  int32_t pos[kRun];
+  // (buffer loads: an item is 256 bytes from the last, which is part of the instruction, and what lies beyond the sequence reads as 0)
+  const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(weights), 0, 4 * n, 0x00020000);
+  const __amdgpu_buffer_rsrc_t p_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(positions), 0, 4 * n, 0x00020000);
+  auto read = [&](int first) __attribute__((always_inline)) {
+    const int at = (start + first * 64 + lane) * 4;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      if (first + i >= items) continue;
-      const int t = min(start + (first + i) * 64 + lane, n - 1);
-      w[i] = weights[t];
-      pos[i] = positions[t];
+    for (int i = 0; i < kRun; ++i) {
+      pos[i] = static_cast<int32_t>(__builtin_amdgcn_raw_buffer_load_b32(p_rsrc, at + i * 256, 0, 0));
+      w[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(w_rsrc, at + i * 256, 0, 0));
     }
   };
   read(0);
@@ -173,16 +198,22 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     gone = gone || id < 0 || id >= a.g.n_pages;
     if (p < kHeldPages) ids[p] = id;
   }
-  for (int i = tid; i < 3 * kBins / 4; i += kThreads) reinterpret_cast<int4*>(bins)[i] = make_int4(0, 0, 0, 0);
+  for (int i = tid; i < kAllBins / 4; i += kThreads) reinterpret_cast<int4*>(bins)[i] = make_int4(0, 0, 0, 0);
+  if (tid < 64) some_over[tid] = 0;
+  if (tid == 0) some_count = 0;
   int newest = INT32_MIN;
   if (a.recent > 0) {
-    for (int first = 0; first < items; first += ITEMS) {
-      if (LONG && first > 0) read(first);
+    for (int first = 0; first < items; first += kRun) {
+      if (first > 0) read(first);
+      if (start + (first + kRun) * 64 <= end) {                // (uniform: all of the run's tokens are there)
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
-        if (first + i < items) newest = max(newest, pos[i]);
+        for (int i = 0; i < kRun; ++i) newest = max(newest, pos[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+          if (start + (first + i) * 64 + lane < end) newest = max(newest, pos[i]);
+      }
     }
-    if (LONG) read(0);
     newest = wave_max_int(newest);
   }
   const bool wave_gone = __ballot(gone) != 0;
@@ -192,79 +223,140 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     leave();
     return;
   }
-  if (h == 0 && tid == 0) a.lens_out[b] = a.budget;
   if (a.recent > 0) newest = wave_max_int(sums[0][0][lane & (WAVES - 1)]);
-  const int64_t young = static_cast<int64_t>(newest) - a.recent;       // positions beyond are safe
-  uint32_t keys[ITEMS];                                        // (of a token that there is not: 0.  A weight's is at least 0x007fffff, minus infinity's)
+
+  // The run's keys from its records: 0 where no token of the wave's is.  (A weight's is at least 0x007fffff, minus infinity's.)
+  uint32_t keys[kRun];
   auto make_keys = [&](int first) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
+    for (int i = 0; i < kRun; ++i) {
       keys[i] = 0;
       if (first + i >= items) continue;
-      uint32_t k = w[i] == w[i] ? float_key(w[i] + 0.0f) : kNanKey;    // (minus zero is zero)
-      if (pos[i] < a.first || (a.recent > 0 && pos[i] > young)) k = kSafe;
-      keys[i] = start + (first + i) * 64 + lane < n ? k : 0;
+      const uint32_t k = w[i] == w[i] ? float_key(w[i] + 0.0f) : kNanKey;      // (minus zero is zero)
+      // (newest - position is no negative number and may have 32 bits)
+      const bool safe = pos[i] < a.first || static_cast<uint32_t>(newest) - static_cast<uint32_t>(pos[i]) < static_cast<uint32_t>(a.recent);
+      keys[i] = safe ? kSafe : k;
+    }
+    if (start + (first + kRun) * 64 > end) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i)
+        if (start + (first + i) * 64 + lane >= end) keys[i] = 0;
     }
   };
-  if (!LONG) make_keys(0);
-  // calls f(first) with the records and keys of items first .. first + ITEMS - 1 at hand
+  // Calls f(first) for every run, its keys at hand.
   auto each_run = [&](auto&& f) __attribute__((always_inline)) {
-    if constexpr (LONG) {
-      for (int first = 0; first < items; first += ITEMS) {
-        read(first);
-        make_keys(first);
+    if constexpr (KEYS == Keys::registers) {
+      f(0);
+    } else {
+#pragma unroll 1
+      for (int first = 0; first < items; first += kRun) {
+        if constexpr (KEYS == Keys::lds) {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) keys[i] = first + i < items ? key_lds[(wave * kLdsItems + first + i) * 64 + lane] : 0u;
+        } else {
+          read(first);
+          make_keys(first);
+        }
         f(first);
       }
-    } else {
-      f(0);
     }
   };
+  auto count = [&](int32_t* mine, uint32_t k, int shift, uint32_t size) __attribute__((always_inline)) { atomicAdd(&mine[k >> shift & (size - 1)], 1); };
+  // Every key once: to where it will be looked at again, and counted by its first eleven bits.  Records go to their place (where a
+  // token leaves, the one that comes is written later).
+#pragma unroll 1
+  for (int first = 0; first < items; first += kRun) {
+    if (KEYS == Keys::made ? items > kRun : KEYS == Keys::lds) read(first);
+    make_keys(first);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      if (first + i >= items) continue;
+      if (KEYS == Keys::lds) key_lds[(wave * kLdsItems + first + i) * 64 + lane] = keys[i];
+      if (keys[i] != 0) count(bins, keys[i], 20, kFirstBins);
+    }
+    if ((w_apart || p_apart) && start + first * 64 < a.budget) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const int t = start + (first + i) * 64 + lane;
+        if (t >= min(end, a.budget)) continue;
+        if (w_apart) weights_out[t] = w[i];
+        if (p_apart) positions_out[t] = pos[i];
+      }
+    }
+    if (KEYS == Keys::registers) break;
+  }
 
-  // ---- the budget-th largest key, eleven bits at a time (the last time ten) from the top ----------------------------
-  // All waves count into the same bins and sum them in groups of 32; then every wave finds by itself the group, and in it the bin,
-  // where the sum from the top reaches what is needed.
+  // ---- the budget-th largest key, from the top: twelve bits, ten and ten ----------------------------------------------
+  // All waves count into the same bins and sum them in 64 groups; then every wave finds by itself the group, and in it the bin, where
+  // the sum from the top reaches what is needed.
   uint32_t key = 0;                                            // the bits that are known
   int need = a.budget;                                         // that many keys of those that begin with them
-  bool exact = false;                                          // ... which are all of them
-  auto look = [&](int which, int shift, int size) __attribute__((always_inline)) {
-    int32_t* mine = bins + which * kBins;
-    each_run([&](int first) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t k = keys[i];
-        if (first + i < items && k != 0 && (which == 0 || (k ^ key) >> shift < static_cast<uint32_t>(size)))
-          atomicAdd(&mine[k >> shift & (size - 1)], 1);
-      }
-    });
+  int like = 0;                                                // ... of so many
+#pragma unroll 1
+  for (int which = 0;; ++which) {
+    const int shift = which == 0 ? 20 : (which == 1 ? 10 : 0), size = which == 0 ? kFirstBins : kLaterBins, of_group = size / 64;
+    int32_t* mine = bins + (which == 0 ? 0 : (which == 1 ? kFirstBins : kFirstBins + kLaterBins));
     __syncthreads();
-    // (a lane sums its few bins, neighbours the 32 of a group)
-    constexpr int kEach = kBins / kThreads;
+    // (WAVES neighbours sum the bins of a group)
     int part = 0;
+    if (which == 0) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) part += mine[tid * kEach + i];
+      for (int i = 0; i < kFirstBins / kThreads; ++i) part += mine[tid * (kFirstBins / kThreads) + i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLaterBins / kThreads; ++i) part += mine[tid * (kLaterBins / kThreads) + i];
+    }
     part += static_cast<int>(dpp_row<0xB1>(static_cast<uint32_t>(part)));
     part += static_cast<int>(dpp_row<0x4E>(static_cast<uint32_t>(part)));
-    if (kEach < 8) part += static_cast<int>(dpp_row<0x141>(static_cast<uint32_t>(part)));
-    if (kEach < 4) part += static_cast<int>(dpp_row<0x140>(static_cast<uint32_t>(part)));
-    if ((lane & (32 / kEach - 1)) == 0) groups[which][tid / (32 / kEach)] = part;
+    if (WAVES > 4) part += static_cast<int>(dpp_row<0x141>(static_cast<uint32_t>(part)));
+    if (WAVES > 8) part += static_cast<int>(dpp_row<0x140>(static_cast<uint32_t>(part)));
+    if ((lane & (WAVES - 1)) == 0) groups[which][tid / WAVES] = part;
     __syncthreads();
     const int sum = groups[which][63 - lane];
     const int upto = wave_prefix(sum);
     const int l = __builtin_ctzll(__ballot(upto >= need));     // (there is one: as many keys as are needed are in the bins)
     const int over = __builtin_amdgcn_readlane(upto - sum, l);
-    const int bin = kBins - 1 - 32 * l - (lane & 31), c = lane < 32 ? mine[bin] : 0;
+    const int top = size - 1 - of_group * l, c = lane < of_group ? mine[top - lane] : 0;
     const int upto2 = over + wave_prefix(c);
     const int m = __builtin_ctzll(__ballot(upto2 >= need));
-    const int count = __builtin_amdgcn_readlane(c, m);
-    key |= static_cast<uint32_t>(kBins - 1 - 32 * l - m) << shift;
-    need -= __builtin_amdgcn_readlane(upto2, m) - count;
-    exact = count == need;
-  };
-  look(0, 21, kBins);
-  if (!exact) look(1, 10, kBins);
-  if (!exact) look(2, 0, kBins / 2);
+    like = __builtin_amdgcn_readlane(c, m);
+    key |= static_cast<uint32_t>(top - m) << shift;
+    need -= __builtin_amdgcn_readlane(upto2, m) - like;
+    if (like == need || which == 2) break;
+    if (like <= 64) {
+      // Few: they are written side by side, and each is compared with all, the waves sharing them.
+      each_run([&](int first) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+          if (first + i < items && keys[i] != 0 && (keys[i] ^ key) >> shift == 0) some[atomicAdd(&some_count, 1) & 63] = keys[i];
+      });
+      __syncthreads();
+      const uint32_t v = some[min(lane, like - 1)];
+      uint32_t above = 0;                                      // those above in the lower half, those not below in the upper
+      for (int j = wave; j < like; j += WAVES) {
+        const uint32_t other = some[j];
+        above += (other > v ? 1u : 0u) + (other >= v ? 0x10000u : 0u);
+      }
+      if (above != 0) atomicAdd(&some_over[lane], above);
+      __syncthreads();
+      above = some_over[lane];
+      const int gt = above & 0xffff, ge = above >> 16;
+      const int at = __builtin_ctzll(__ballot(gt < need && ge >= need));       // (there is one)
+      key = __builtin_amdgcn_readlane(v, at);
+      need -= __builtin_amdgcn_readlane(gt, at);
+      like = __builtin_amdgcn_readlane(ge - gt, at);
+      break;
+    }
+    int32_t* later = bins + (which == 0 ? kFirstBins : kFirstBins + kLaterBins);
+    each_run([&](int first) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i)
+        if (first + i < items && keys[i] != 0 && (keys[i] ^ key) >> shift == 0) count(later, keys[i], which == 0 ? 10 : 0, kLaterBins);
+    });
+  }
+  const bool exact = like == need;                             // all keys that begin with `key`, else the first `need` that equal it
 
-  // ---- who stays: bit i of a lane's word for its item number first + i ----------------------------------------------
+  // ---- who stays -----------------------------------------------------------------------------------------------------
   // lanes 16 j .. 16 j + 15: the j-th number of every wave; row j of `all` and `before` has its sums over all waves and over those
   // before this one
   struct Sums {
@@ -276,97 +368,108 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     const int of = lane & 15, v = of < WAVES && lane < 32 ? sums[which][lane >> 4][of] : 0;
     return Sums{row16_add_int(v), row16_add_int(of < wave ? v : 0)};
   };
-  const uint64_t below = (1ull << lane) - 1;
-  int rank = 0;                                                // of equal keys before the run
-  if (!exact) {                                                // (key is the whole key, of which the first `need` are kept)
+  auto rank_in = [](uint64_t votes) { return static_cast<int>(__builtin_amdgcn_mbcnt_hi(votes >> 32, __builtin_amdgcn_mbcnt_lo(votes, 0))); };
+  int ties = 0;                                                // equal keys of the waves before
+  if (!exact) {
     int same = 0;
+    each_run([&](int) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) same += __builtin_popcountll(__ballot(keys[i] == key));
+    });
+    ties = __builtin_amdgcn_readlane(over_waves(1, same, 0).before, 0);
+  }
+  // Calls f(token of lane 0, votes: who of the item's tokens lies before the budget, who is kept) for the wave's items.
+  auto each_item = [&](auto&& f) __attribute__((always_inline)) {
+    int r = ties;
     each_run([&](int first) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i) same += __builtin_popcountll(__ballot(keys[i] == key));
-    });
-    rank = __builtin_amdgcn_readlane(over_waves(1, same, 0).before, 0);
-  }
-  auto kept = [&](int first) __attribute__((always_inline)) {
-    uint32_t mask = 0;
-    if (exact) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) mask |= static_cast<uint32_t>(keys[i] >= key) << i;
-    } else {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        bool keep = keys[i] > key;
-        const uint64_t same = __ballot(keys[i] == key);
-        if (same != 0) {
-          keep = keep || (keys[i] == key && rank + __builtin_popcountll(same & below) < need);
-          rank += __builtin_popcountll(same);
+      for (int i = 0; i < kRun; ++i) {
+        const int t0 = start + (first + i) * 64, in_front = a.budget - t0;
+        if (t0 >= end) continue;
+        const uint64_t front = in_front >= 64 ? ~0ull : (in_front > 0 ? (1ull << in_front) - 1 : 0ull);
+        uint64_t kept = __ballot(keys[i] >= key);
+        if (!exact) {
+          const uint64_t same = __ballot(keys[i] == key);
+          if (same != 0) {
+            kept = __ballot(keys[i] > key || (keys[i] == key && r + rank_in(same) < need));
+            r += __builtin_popcountll(same);
+          }
         }
-        mask |= static_cast<uint32_t>(keep) << i;
+        f(t0, front, kept);
       }
-    }
-    return mask;
+    });
   };
-  // the items of the run whose tokens lie before the budget
-  auto before = [&](int first) {
-    const int c = min((a.budget - (start + first * 64 + lane) + 63) >> 6, min(items - first, ITEMS));
-    return c >= 32 ? 0xffffffffu : (1u << max(c, 0)) - 1;
-  };
-  const int rank0 = rank;
   int holes = 0, movers = 0;
-  uint32_t stay = 0;                                           // (not LONG: the lane's one word)
-  each_run([&](int first) __attribute__((always_inline)) {
-    stay = kept(first);
-    holes += __builtin_popcount(before(first) & ~stay);
-    movers += __builtin_popcount(stay & ~before(first));
+  uint32_t votes_lo = 0, votes_hi = 0;                         // (lane i: who of item i's tokens is kept)
+  each_item([&](int t0, uint64_t front, uint64_t kept) __attribute__((always_inline)) {
+    holes += __builtin_popcountll(front & ~kept);
+    movers += __builtin_popcountll(kept & ~front);
+    if (KEYS == Keys::lds) {
+      const bool mine = lane == (t0 - start) >> 6;
+      votes_lo = mine ? static_cast<uint32_t>(kept) : votes_lo;
+      votes_hi = mine ? static_cast<uint32_t>(kept >> 32) : votes_hi;
+    }
   });
-  const int holes_here = __builtin_amdgcn_readlane(wave_prefix(holes), 63), movers_here = __builtin_amdgcn_readlane(wave_prefix(movers), 63);
-  const Sums s = over_waves(2, holes_here, movers_here);
+  const int any = holes + movers;
+  const Sums s = over_waves(2, holes, movers);
   holes = __builtin_amdgcn_readlane(s.before, 0);
   movers = __builtin_amdgcn_readlane(s.before, 16);
   // (as many holes as movers)
   const int moves = min(min(__builtin_amdgcn_readlane(s.all, 0), __builtin_amdgcn_readlane(s.all, 16)), plan.most);
-  int32_t* list = workspace + list_start(static_cast<int64_t>(a.B) * a.n_kv) + static_cast<int64_t>(blockIdx.x) * 2 * plan.most;
-  int32_t* to = plan.few ? bins : list;
-  int32_t* from = plan.few ? bins + kFewMoves : list + plan.most;
-  rank = rank0;
-  const bool apart = weights_out != weights, pos_apart = positions_out != positions;
-  if (holes_here + movers_here > 0 || apart || pos_apart)
-    each_run([&](int first) __attribute__((always_inline)) {
-      if (LONG) stay = kept(first);
-      const uint32_t front = before(first);
-      const uint32_t go = front & ~stay, come = stay & ~front;
-      if (holes_here > 0)
-        for (int i = 0; i < ITEMS && first + i < items; ++i) {
-          const uint64_t votes = __ballot(go >> i & 1);
-          const int r = holes + __builtin_popcountll(votes & below);
-          if ((go >> i & 1) && r < moves) to[r] = start + (first + i) * 64 + lane;
-          holes += __builtin_popcountll(votes);
+  auto write_lists = [&](int32_t* to, int32_t* from) __attribute__((always_inline)) {
+    if constexpr (KEYS == Keys::lds) {
+      // Lane i has item i's votes and writes its movers down one after the other (there are few of an item as a rule).
+      static_assert(kLdsItems <= 64, "a lane has one item");
+      const int t0 = start + lane * 64, in_front = a.budget - t0;
+      const uint64_t front = in_front >= 64 ? ~0ull : (in_front > 0 ? (1ull << in_front) - 1 : 0ull);
+      uint64_t come = (static_cast<uint64_t>(votes_hi) << 32 | votes_lo) & ~front;
+      const int n_come = __builtin_popcountll(come);
+      int r = movers + wave_prefix(n_come) - n_come;
+      while (__ballot(come != 0) != 0) {
+        if (come != 0) {
+          if (r < moves) from[r] = t0 + __builtin_ctzll(come);
+          ++r;
+          come &= come - 1;
         }
-      if (movers_here > 0)
-        for (int i = 0; i < ITEMS && first + i < items; ++i) {
-          const uint64_t votes = __ballot(come >> i & 1);
-          const int r = movers + __builtin_popcountll(votes & below);
-          if ((come >> i & 1) && r < moves) from[r] = start + (first + i) * 64 + lane;
-          movers += __builtin_popcountll(votes);
-        }
-      // the records of those that stay where they are
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int t = start + (first + i) * 64 + lane;
-        if (!(front & stay & 1u << i)) continue;
-        if (apart) weights_out[t] = w[i];
-        if (pos_apart) positions_out[t] = pos[i];
+      }
+      if (start < a.budget)
+        each_item([&](int first, uint64_t before, uint64_t kept) __attribute__((always_inline)) {
+          const uint64_t go = before & ~kept;
+          const int at = holes + rank_in(go);
+          if (__builtin_amdgcn_inverse_ballot_w64(go) && at < moves) to[at] = first + lane;
+          holes += __builtin_popcountll(go);
+        });
+      return;
+    }
+    each_item([&](int t0, uint64_t front, uint64_t kept) __attribute__((always_inline)) {
+      const uint64_t go = front & ~kept, come = kept & ~front;
+      if (go != 0) {
+        const int r = holes + rank_in(go);
+        if (__builtin_amdgcn_inverse_ballot_w64(go) && r < moves) to[r] = t0 + lane;
+        holes += __builtin_popcountll(go);
+      }
+      if (come != 0) {
+        const int r = movers + rank_in(come);
+        if (__builtin_amdgcn_inverse_ballot_w64(come) && r < moves) from[r] = t0 + lane;
+        movers += __builtin_popcountll(come);
       }
     });
-  __syncthreads();
-  // (records by the last threads, rows by the first: few of both go side by side)
-  move_records<kThreads>(a, base, to, from, moves);
-  if (!plan.few) {
-    if (tid == 0) workspace[blockIdx.x] = moves;
-  } else if (pages <= kHeldPages) {
-    move_rows<kThreads>(a, plan, h, [&](int page) { return ids[page]; }, to, from, moves, 0);
+  };
+  if (plan.few) {
+    if (any > 0) write_lists(bins, bins + kFewMoves);
+    __syncthreads();
+    // (records by the last threads, rows by the first: few of both go side by side)
+    if (pages <= kHeldPages) move_rows<kThreads>(a, plan, h, [&](int page) { return ids[page]; }, bins, bins + kFewMoves, moves, 0);
+    else move_rows<kThreads>(a, plan, h, [&](int page) { return pt[page]; }, bins, bins + kFewMoves, moves, 0);
+    move_records<kThreads>(a, base, bins, bins + kFewMoves, moves);
   } else {
-    move_rows<kThreads>(a, plan, h, [&](int page) { return pt[page]; }, to, from, moves, 0);
+    int32_t* to = workspace + list_start(static_cast<int64_t>(a.B) * a.n_kv) + static_cast<int64_t>(blockIdx.x) * 2 * plan.most;
+    if (any > 0) write_lists(to, to + plan.most);
+    __syncthreads();
+    if (tid == 0) workspace[blockIdx.x] = moves;
+    move_records<kThreads>(a, base, to, to + plan.most, moves);
   }
+  if (h == 0 && tid == 0) a.lens_out[b] = a.budget;
 }
 
 // A workgroup: the rows that its 256 threads move four each of at a time, about (the grid has room for `most` moves of a head).
@@ -398,10 +501,10 @@ int32_t launch_evict_paged(const EvictArgs& a, hipStream_t st) {
   p.few = p.most <= kFewMoves;
   const int64_t heads = static_cast<int64_t>(a.B) * a.n_kv;
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(heads)), dim3(waves * 64), 0, st, a, p); };
-  if (room <= 4 * 64 * 8) go(evict_select_kernel<4, 8, false>, 4);
-  else if (room <= 16 * 64 * 8) go(evict_select_kernel<16, 8, false>, 16);
-  else if (room <= 16 * 64 * 32) go(evict_select_kernel<16, 32, false>, 16);
-  else go(evict_select_kernel<16, 32, true>, 16);
+  if (room <= 8 * 64 * kFewItems) go(evict_select_kernel<8, Keys::registers>, 8);
+  else if (room <= 16 * 64 * kFewItems) go(evict_select_kernel<16, Keys::registers>, 16);
+  else if (room <= 16 * 64 * kLdsItems) go(evict_select_kernel<16, Keys::lds>, 16);
+  else go(evict_select_kernel<16, Keys::made>, 16);
   RPTQ_HIP(hipGetLastError());
   if (p.few) return RPTQ_OK;
   const int rows = 4 * (256 / (2 * p.units)), chunks = std::min((p.most + rows - 1) / rows, kMoveChunks);
