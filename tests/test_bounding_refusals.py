@@ -109,8 +109,9 @@ def test_workspaces(lib):
     for a in ((-1, 1, 8, 2, 128), (4, 0, 8, 2, 128), (4, 65537, 8, 2, 128), (4, 1, 7, 2, 128), (4, 1, 8, 2, 100)):
         assert rp.rptq_attend_weights_paged_workspace_bytes(*a) == 0
     assert rp.rptq_evict_paged_workspace_bytes(4, 2, 48, 10) >= 4 * 8
-    few, many = (rp.rptq_evict_paged_workspace_bytes(4, 2, 100000, n) for n in (16, 50000))
-    assert few < 1 << 10 and many >= 4 * 8 * 2 * 50000
+    assert rp.rptq_evict_paged_workspace_bytes(4, 2, 4096, 16) < 1 << 10
+    few, many = (rp.rptq_evict_paged_workspace_bytes(400, 2, 100000, n) for n in (16, 50000))
+    assert few < 1 << 13 and many >= 4 * 800 * 2 * 50000
     for a in ((-1, 2, 48, 10), (4, 0, 48, 10), (4, 2, 0, 10), (4, 2, 48, 0), (32768, 65, 48, 10)):
         assert rp.rptq_evict_paged_workspace_bytes(*a) == 0
 

@@ -220,6 +220,14 @@ def test_long_sequences_cut(rp, n, budget):
         evicted(rp, b, budget, 0, 0, w, p, n, True)
 
 
+@pytest.mark.parametrize("n,budget", [(8300, 8200), (8400, 5000), (10000, 2)])
+def test_many_heads_of_long_sequences(rp, n, budget):
+    """As many heads as fill the chip with a workgroup each."""
+    b = Batch(rp, [n, n - 1, 64], 44, 32, 3, 128)
+    w, p = records(np.random.default_rng(n), 3, 44, n)
+    evicted(rp, b, budget, 0, budget // 3, w, p, n, n == 8400)
+
+
 @pytest.mark.parametrize("what", ["all equal", "all zero", "zeros of both signs", "infinities and nan", "negative", "ends of the range", "steps of the last bit", "steps of the last bits", "safe ones first"])
 def test_orders_of_weights(rp, what):
     rng = np.random.default_rng(6)
@@ -249,6 +257,13 @@ def test_orders_of_weights(rp, what):
         p[:] = np.arange(n)
     b = Batch(rp, [n, 300], 2, 64, 4, 16)
     evicted(rp, b, budget, 10, 40, w, p, n, True)
+    # the same tokens behind many others, in long sequences, and in sequences whose keys do not fit on the chip
+    for m in (12000, 34000):
+        more, where = records(rng, 1, 2, m)
+        more[0, :, -n:], where[0, :, -n:] = w[0], p[0]
+        if what == "all equal":
+            more[:] = 0.375
+        evicted(rp, Batch(rp, [m], 2, 64, 4, 128), m - 300, 10, 40, more, where, m, False)
 
 
 def test_positions_at_the_ends_of_their_type(rp):
