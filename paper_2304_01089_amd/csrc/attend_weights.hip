@@ -38,9 +38,14 @@ struct WeightPlan {
   double per_share, per_set;                   // 1 / share and 1 / set_tiles, a little more
 };
 
+// A weight: 2^(high * (digits 2, 3) - off + low * (digits 0, 1)) * rest.  The upper digits meet `off` first (what is left is small, and
+// rounded as such); rest is 2 to what `off` lost as it became fp32 (with lse about 16, 10^-6 of every weight).
 struct QueryRow {
-  float low, high, off;                        // a score in units of log2: low * (digits 0, 1) + high * (digits 2, 3) - off
-  int32_t end;                                 // tokens that the query sees
+  float low, high, off, rest;
+};
+struct TileRows {
+  QueryRow row[kRowHeads];
+  int32_t end[kRowHeads];                      // tokens that the query sees
 };
 
 typedef int i4v __attribute__((ext_vector_type(4)));
@@ -82,29 +87,33 @@ struct QueryDigits {
     return r;
   }
   // to: the tile's 16 rows, `stride` bytes apart
-  __device__ __forceinline__ QueryRow make(const Query& now, unsigned char* to, int stride) const {
-    const float to_log2 = a.scale * kLog2e;
-    float x[NB][8], top = 0.0f;
+  __device__ __forceinline__ void make(const Query& now, unsigned char* to, int stride, TileRows* rows) const {
+    // (in 64 bits up to the fixed point: an error of 2^-24 of q' would be one of score / 2^24 in a score's logarithm, and zero points far
+    // from the codes make scores large)
+    const double to_log2 = static_cast<double>(a.scale) * 1.4426950408889634074;
+    double x[NB][8], zterm = 0.0;
+    float top = 0.0f;
     bool bad = false;
-    double zterm = 0.0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float v = __uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16) * __int_as_float(kp[nb][e][2]) * to_log2;
-        x[nb][e] = now.own ? v : 0.0f;
-        top = fmaxf(top, fabsf(x[nb][e]));
-        bad = bad || !(fabsf(x[nb][e]) < __builtin_huge_valf());
-        zterm = fma(static_cast<double>(x[nb][e]), static_cast<double>(kp[nb][e][3]), zterm);
+        const double v = static_cast<double>(__uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16)) * static_cast<double>(__int_as_float(kp[nb][e][2])) * to_log2;
+        x[nb][e] = now.own ? v : 0.0;
+        const float size = fabsf(static_cast<float>(x[nb][e]));
+        top = fmaxf(top, size);
+        bad = bad || !(size < __builtin_huge_valf());
+        zterm = fma(x[nb][e], static_cast<double>(kp[nb][e][3]), zterm);
       }
     top = row16_max(top);
     zterm = row16_sum(zterm);
     const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;          // top < 2^ex
+    const double to_fixed = ldexp(1.0, 30 - ex);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       uint32_t d[8], plane[4][2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = digits(static_cast<int>(rintf(ldexpf(x[nb][e], 30 - ex))));
+      for (int e = 0; e < 8; ++e) d[e] = digits(static_cast<int>(rint(x[nb][e] * to_fixed)));
 #pragma unroll
       for (int f = 0; f < 2; ++f) {                        // (four numbers' bytes to four planes)
         const uint32_t l01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x05010400u), h01 = __builtin_amdgcn_perm(d[4 * f + 1], d[4 * f], 0x07030602u);
@@ -119,13 +128,20 @@ struct QueryDigits {
         *reinterpret_cast<uint2*>(to + (g4 * 4 + by) * stride + nb * kPageBlock + n16 * 8) = make_uint2(plane[by][0], plane[by][1]);
     }
     const float scale = (__ballot(bad) >> (g4 * 16) & 0xffffu) != 0 ? __builtin_nanf("") : ldexpf(1.0f, ex - 30 - kShift);
-    return QueryRow{scale, scale * 65536.0f, static_cast<float>(zterm + static_cast<double>(now.lse) * 1.4426950408889634074), now.end};
+    const double off = zterm + static_cast<double>(now.lse) * 1.4426950408889634074;
+    const float high = static_cast<float>(off);
+    // (an lse that is not finite: what is lost of it is nothing)
+    const float lost = fabsf(high) < __builtin_huge_valf() ? static_cast<float>(off - static_cast<double>(high)) : 0.0f;
+    if (n16 == 0) {
+      rows->row[g4] = QueryRow{scale, scale * 65536.0f, high, __builtin_amdgcn_exp2f(-lost)};
+      rows->end[g4] = now.end;
+    }
   }
 };
 
-// Workspace, where there are more than kFewTiles row tiles: per (sequence, unit, tile) 16 rows of P digits and four QueryRows.
+// Workspace, where there are more than kFewTiles row tiles: per (sequence, unit, tile) 16 rows of P digits and the TileRows.
 template <int NB>
-__host__ __device__ constexpr int made_bytes() { return NB * 16 * kPageBlock + static_cast<int>(kRowHeads * sizeof(QueryRow)); }
+__host__ __device__ constexpr int made_bytes() { return NB * 16 * kPageBlock + static_cast<int>(sizeof(TileRows)); }
 
 __device__ __forceinline__ int tokens_of(const WeightArgs& a, int length) {
   const int64_t room = min(static_cast<int64_t>(a.pages_per_seq) << a.g.page_shift, a.capacity);
@@ -147,8 +163,7 @@ __global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightP
     for (int e = 0; e < 8; ++e)
       maker.kp[nb][e] = *reinterpret_cast<const i4v*>(a.k_pos + unit * maker.P + nb * kPageBlock + n16 * 8 + e);
   unsigned char* to = static_cast<unsigned char*>(a.workspace) + ((static_cast<int64_t>(b) * gridDim.y + unit) * plan.tiles + tile) * made_bytes<NB>();
-  const QueryRow row = maker.make(maker.request(tile), to, maker.P);
-  if (n16 == 0) reinterpret_cast<QueryRow*>(to + 16 * maker.P)[g4] = row;
+  maker.make(maker.request(tile), to, maker.P, reinterpret_cast<TileRows*>(to + 16 * maker.P));
 }
 
 // NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace
@@ -159,7 +174,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
   constexpr int kDigitRow = P + 16;                        // (16 more: other banks)
   constexpr int kHeld = MADE ? held_tiles(NB) : kFewTiles;
   __shared__ __align__(16) unsigned char q_dig[kHeld * 16 * kDigitRow];
-  __shared__ __align__(16) QueryRow rows[kHeld * kRowHeads];
+  __shared__ __align__(16) TileRows rows[kHeld];
   __shared__ __align__(16) unsigned char table[MADE ? 16 : P / 8 * 144];         // eight positions' records, and 16 bytes (banks)
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -251,8 +266,9 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
       for (int k = 0; k < kEach; ++k) {
         const int i = k * 256 + static_cast<int>(threadIdx.x);
         const int tile = i / kPieces, at = i - tile * kPieces, row = at / (P / 16);
-        unsigned char* to = row < 16 ? q_dig + (tile * 16 + row) * kDigitRow : reinterpret_cast<unsigned char*>(rows + tile * kRowHeads);
-        if (i < pieces) *reinterpret_cast<i4v*>(to + (at & (P / 16 - 1)) * 16) = v[k];
+        unsigned char* to = row < 16 ? q_dig + (tile * 16 + row) * kDigitRow + (at & (P / 16 - 1)) * 16
+                                     : reinterpret_cast<unsigned char*>(rows + tile) + (at - P) * 16;
+        if (i < pieces) *reinterpret_cast<i4v*>(to) = v[k];
       }
     } else {
       *reinterpret_cast<i4v*>(table + (threadIdx.x & (P - 1)) * 16 + (threadIdx.x & (P - 1)) / 8 * 16) = record;
@@ -263,8 +279,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 8; ++e) maker.kp[nb][e] = *reinterpret_cast<const i4v*>(table + (nb * 16 + n16) * 144 + e * 16);
-        const QueryRow row = maker.make(maker.request(wave), q_dig + wave * 16 * kDigitRow, kDigitRow);
-        if (n16 == 0) rows[wave * kRowHeads + g4] = row;
+        maker.make(maker.request(wave), q_dig + wave * 16 * kDigitRow, kDigitRow, rows + wave);
       }
     }
     __syncthreads();
@@ -300,7 +315,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
         };
         auto fetch = [&](int i) __attribute__((always_inline)) {
           Operands o;
-          o.row = rows[i * kRowHeads + g4];
+          o.row = rows[i].row[g4];
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -335,9 +350,9 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
           for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              // (the small half and lse first: one rounding each)
-              const float low = fmaf(static_cast<float>(c[n][r][1] * 256 + c[n][r][0]), o[n].row.low, -o[n].row.off);
-              sum[r] += seen(__builtin_amdgcn_exp2f(fmaf(static_cast<float>(c[n][r][3] * 256 + c[n][r][2]), o[n].row.high, low)), r, o[n].row.end);
+              const float high = fmaf(static_cast<float>(c[n][r][3] * 256 + c[n][r][2]), o[n].row.high, -o[n].row.off);
+              const float p = __builtin_amdgcn_exp2f(fmaf(static_cast<float>(c[n][r][1] * 256 + c[n][r][0]), o[n].row.low, high));
+              sum[r] = fmaf(seen(p, r, i + n), o[n].row.rest, sum[r]);
             }
         };
         int i = from;
@@ -356,7 +371,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
         const int from = max(set * plan.set_tiles, tile0) - tile0, to = min((set + 1) * plan.set_tiles, tile1) - tile0;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (whole) add_up(from, to, sum, [&](float p, int, int) { return p; });
-        else add_up(from, to, sum, [&](float p, int r, int end) { return token_r[r] < end ? p : 0.0f; });
+        else add_up(from, to, sum, [&](float p, int r, int i) { return token_r[r] < rows[i].end[g4] ? p : 0.0f; });
         // the rows of a head together
         if (HEADS == 1 || group >= 2) {
 #pragma unroll
