@@ -550,10 +550,11 @@ int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t 
  * sequence may keep different tokens.  A sequence of no more tokens, or one of whose tokens' pages is not there, stays as it is,
  * lens_out[b] its number of tokens.  Attention over the result is attention over the kept tokens.
  *   weights_out, token_positions_out  the records of lens_out[b] tokens; may be weights and token_positions, and overlap them no other way
- *   lens_out  device int32 [B], must not be lens
+ *   lens_out  device int32 [B], must not overlap lens
  *   workspace device, rptq_evict_paged_workspace_bytes(B, n_kv_heads, capacity, budget) bytes, nothing to clear or keep
  *   budget >= 1; first, recent >= 0, first + recent <= budget; B * n_kv_heads <= RPTQ_MAX_TRACKED_HEADS
- * No page may belong to two sequences of the call, nor to one that lives on elsewhere: rows move in place.
+ * No page may belong to two sequences of the call, nor to one that lives on elsewhere: rows move in place.  Nothing else may write the
+ * records, lengths and page tables while the call runs.
  *
  * Both are asynchronous on `stream`, allocate nothing and may be recorded into a graph without a call before.
  * 1 <= capacity <= 2^29.

@@ -352,7 +352,7 @@ def attend_weights_paged(cache: PagedCache, q, page_table, lens, lse, track: Cac
     position being positions[b] (its index where None).  scale: attend_paged's."""
     cache._compared or cache.compare()
     n_q_heads = q.shape[1] // cache.head_dim
-    if workspace is None:
+    if workspace is None and queries * n_q_heads > 4 * cache.n_heads:          # (up to four queries of a key/value head need none)
         workspace = attend_weights_paged_workspace(cache, lens.shape[0], n_q_heads, queries)
     B.rptq_attend_weights_paged(q, queries, n_q_heads, cache.n_heads, cache.head_dim,
                                 cache.head_dim ** -0.5 if scale is None else scale, cache.k_table, cache.bits, cache.k_pages, cache.page_size,
