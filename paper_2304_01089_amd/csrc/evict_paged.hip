@@ -178,10 +178,11 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
   float w[kRun];
   int32_t pos[kRun];
   // (buffer loads: an item is 256 bytes from the last, which is part of the instruction, and what lies beyond the sequence reads as 0)
-  const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(weights), 0, 4 * n, 0x00020000);
-  const __amdgpu_buffer_rsrc_t p_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(positions), 0, 4 * n, 0x00020000);
+  const uint32_t record_bytes = 4u * static_cast<uint32_t>(n);       // (up to 2^31)
+  const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(weights), 0, record_bytes, 0x00020000);
+  const __amdgpu_buffer_rsrc_t p_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(positions), 0, record_bytes, 0x00020000);
   auto read = [&](int first) __attribute__((always_inline)) {
-    const int at = (start + first * 64 + lane) * 4;
+    const uint32_t at = static_cast<uint32_t>(start + first * 64 + lane) * 4u;
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
       pos[i] = static_cast<int32_t>(__builtin_amdgcn_raw_buffer_load_b32(p_rsrc, at + i * 256, 0, 0));
