@@ -138,16 +138,16 @@ def load_library():
 
 def _set_up_calls(lib):
     """Points the native marshalling (csrc/calls.cpp, built beside the library) at the loaded library.  Without it, or
-    without torch, the functions below marshal in Python."""
+    without torch, or with another torch than it was built with, the functions below marshal in Python."""
     global _CALLS, _CALLS_SOUGHT
     _CALLS, _CALLS_SOUGHT = None, True
     try:
         import torch
         from . import _calls
-        objects = dict(bfloat16=torch.bfloat16, float32=torch.float32, int32=torch.int32, int64=torch.int64,
-                       uint8=torch.uint8, float64=torch.float64, get_device=torch._C._cuda_getDevice,
-                       get_stream=torch._C._cuda_getCurrentRawStream)
+        objects = dict(get_device=torch._C._cuda_getDevice, get_stream=torch._C._cuda_getCurrentRawStream)
     except (ImportError, AttributeError):
+        return
+    if torch.__version__.split("+")[0] != getattr(_calls, "torch_version", None):   # (it reads tensors as the torch that it was built with lays them out)
         return
     names = ("rptq_ln_quant", "rptq_cluster_gemm", "rptq_cluster_gemm_quant", "rptq_cluster_rowsums", "rptq_cluster_gemm_cw",
              "rptq_kv_quant", "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",
@@ -162,8 +162,8 @@ def _set_up_calls(lib):
 # (These run several times per call and were most of what a short call cost: ctypes takes an integer address and a
 # bytes object as they are, so no pointer object is built, and a numpy table of a few dozen entries is cheaper to copy
 # than to ask for its address.  The entry points of a serving loop try the native marshalling first, which returns None
-# for arguments out of the ordinary: rptq_ln_quant + rptq_cluster_gemm take 9.78 us on the host, 4.91 + 4.66, instead of 15.0, 7.5 +
-# 6.8; a launch alone is about 3.)
+# for arguments out of the ordinary: rptq_ln_quant + rptq_cluster_gemm take 9.9 us on the host, 4.8 + 5.1, instead of 15.0, 7.5 +
+# 6.8; a launch alone is about 3.4.)
 def _dev(t, dtype=None, allow_none=False):
     """Device address of a torch tensor (None -> NULL)."""
     if t is None:

@@ -1,6 +1,7 @@
 """Builds librptq.so (gfx950) in-tree with hipcc.  `python -m paper_2304_01089_amd.build`."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -49,12 +50,16 @@ def _compile(src: str, objdir: str, verbose: bool) -> str:
 
 def build_calls() -> Optional[str]:
     """Compile the CPython module beside the library (host code only).  Where there is no C++ compiler of the host's, or no
-    header of this Python's, there is no module (None): the binding does the same in Python."""
+    header of this Python's or of torch's, there is no module (None): the binding does the same in Python."""
     untagged = os.path.join(os.path.dirname(CALLS), "_calls.so")
     if os.path.exists(untagged):                 # (any interpreter would load it)
         os.remove(untagged)
     include = sysconfig.get_paths()["include"]
-    lacks = [what for what, there in (("g++", shutil.which("g++")), ("Python.h", os.path.exists(os.path.join(include, "Python.h"))))
+    found = importlib.util.find_spec("torch")      # (torch itself is not loaded)
+    torch = found.submodule_search_locations[0] if found else ""
+    headers = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    lacks = [what for what, there in (("g++", shutil.which("g++")), ("Python.h", os.path.exists(os.path.join(include, "Python.h"))),
+                                      ("torch/version.h", os.path.exists(os.path.join(headers[1], "torch", "version.h"))))
              if not there]
     if lacks:
         sys.stderr.write("no native marshalling of calls: %s not found\n" % " and ".join(lacks))
@@ -62,8 +67,10 @@ def build_calls() -> Optional[str]:
             os.remove(CALLS)
         return None
     tmp = CALLS + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),
-           "-I", include, os.path.join(CSRC, "calls.cpp"), "-o", tmp]
+    # (torch's libraries are found by name: the module is imported once torch has loaded them)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", include,
+           *[o for h in headers for o in ("-isystem", h)], os.path.join(CSRC, "calls.cpp"), "-o", tmp,
+           "-L", os.path.join(torch, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed for calls.cpp:\n%s\n%s" % (res.stdout, res.stderr))
@@ -76,6 +83,7 @@ def build_library(verbose: bool = False, jobs: int = 6) -> str:
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as pool:
+        calls = pool.submit(build_calls)
         objs = list(pool.map(lambda s: _compile(s, objdir, verbose), SOURCES))
     lib = os.environ.get("RPTQ_LIBRARY_OUT", LIB)
     tmp = lib + ".tmp"
@@ -84,7 +92,7 @@ def build_library(verbose: bool = False, jobs: int = 6) -> str:
     if res.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (res.stdout, res.stderr))
     os.replace(tmp, lib)
-    build_calls()
+    calls.result()
     return lib
 
 

@@ -1,14 +1,19 @@
 // CPython module `_calls`: the argument marshalling of the entry points that a serving loop calls, in native code.
 //
-// A short call is paced by the host, and Python-level marshalling was half of its time there (one linear layer,
-// rptq_ln_quant + rptq_cluster_gemm: 15.0 us a pass with ctypes, of which 6.5 in the two launches, 9.78 with this).  Every function takes the binding's arguments by position and covers the ordinary case only:
-// contiguous device tensors of the right type, one-dimensional float32 / int32 tables that support the buffer protocol,
-// ints in range, the current stream.  For anything else it returns None without having called the library, and
+// A short call is paced by the host: a launch is 3.4 us of it, and marshalling in Python, with ctypes, was as much again (one linear
+// layer, rptq_ln_quant + rptq_cluster_gemm: 15.0 us a pass).  Every function takes the binding's arguments by position and covers the
+// ordinary case only: contiguous device tensors of the right type, one-dimensional float32 / int32 tables that support the buffer
+// protocol, ints in range, the current stream.  For anything else it returns None without having called the library, and
 // binding.py's own code converts, or raises, as it always has.  It keeps nothing between calls but the library's entry
-// points and torch's dtype objects and stream query.
+// points and torch's stream query.
+// Tensors are read through torch's C++ interface.  Asked for by their Python attributes, five of each, eleven tensors took 2.6 us more
+// (rptq_rope_quant_paged of one token 7.06 -> 4.48 us a pass, rptq_attend_weights_paged of one
+// sequence 7.13 -> 5.39, which the GPU takes, rptq_rope 5.16 -> 3.83, the linear layer for one row of 768 10.9 -> 9.9).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include "rptq.h"
 
@@ -30,8 +35,10 @@ decltype(&rptq_rope_quant_paged) f_rope_quant_paged;
 decltype(&rptq_attend_weights_paged) f_attend_weights_paged;
 decltype(&rptq_evict_paged) f_evict_paged;
 
-PyObject *n_is_cuda, *n_is_contiguous, *n_dtype, *n_data_ptr, *n_nbytes, *n_get_device, *n_shape, *n_stride;     // attribute names
-PyObject *t_bf16, *t_f32, *t_i32, *t_i64, *t_u8, *t_f64, *get_device, *get_stream;         // torch's objects
+PyObject *get_device, *get_stream;                       // torch's functions
+
+using at::ScalarType;
+constexpr ScalarType kAny = ScalarType::Undefined;       // (no tensor's type)
 
 // Each getter returns false, with no Python error set, where the ordinary case does not apply.
 bool no_error() {
@@ -65,47 +72,38 @@ bool get_flag(PyObject* o, int32_t* out) {
   return true;
 }
 
-bool is_true(PyObject* owned) {
-  if (owned == nullptr) return no_error();
-  const bool t = owned == Py_True;
-  Py_DECREF(owned);
-  return t;
-}
-
-PyObject* dtype_of(PyObject* t) {                        // (borrowed in effect: dtype objects live as long as torch)
-  PyObject* d = PyObject_GetAttr(t, n_dtype);
-  if (d == nullptr) {
-    PyErr_Clear();
-    return nullptr;
+// f of a tensor that is one of torch's own two classes; what has no address or no sizes throws, and is out of the ordinary.
+template <typename F>
+bool of_tensor(PyObject* o, F&& f) {
+  if (!THPVariable_CheckExact(o)) return false;
+  try {
+    return f(THPVariable_Unpack(o));
+  } catch (...) {
+    return false;
   }
-  Py_DECREF(d);
-  return d;
 }
 
-// Address of a contiguous device tensor of that dtype (any if NULL); None is NULL where it is allowed.
+bool is_type(const at::Tensor& t, ScalarType type) { return type == kAny || t.scalar_type() == type; }
+
+// Address of a contiguous device tensor of that dtype; None is NULL where it is allowed.
 template <typename T>
-bool get_tensor(PyObject* t, PyObject* dtype, bool allow_none, T** out) {
-  if (t == Py_None) {
+bool get_tensor(PyObject* o, ScalarType type, bool allow_none, T** out) {
+  if (o == Py_None) {
     *out = nullptr;
     return allow_none;
   }
-  if (!is_true(PyObject_GetAttr(t, n_is_cuda)) || !is_true(PyObject_CallMethodNoArgs(t, n_is_contiguous))) return false;
-  if (dtype != nullptr && dtype_of(t) != dtype) return false;
-  PyObject* p = PyObject_CallMethodNoArgs(t, n_data_ptr);
-  if (p == nullptr) return no_error();
-  void* v = PyLong_Check(p) ? PyLong_AsVoidPtr(p) : nullptr;
-  const bool ok = PyLong_Check(p) && !PyErr_Occurred();
-  Py_DECREF(p);
-  *out = static_cast<T*>(v);
-  return ok || no_error();
+  return of_tensor(o, [&](const at::Tensor& t) {
+    if (!t.is_cuda() || !t.is_contiguous() || !is_type(t, type)) return false;
+    *out = static_cast<T*>(t.data_ptr());
+    return true;
+  });
 }
 
-bool get_bytes(PyObject* t, int64_t* out) {
-  PyObject* b = PyObject_GetAttr(t, n_nbytes);
-  if (b == nullptr) return no_error();
-  const bool ok = get_i64(b, out) && *out >= 0;
-  Py_DECREF(b);
-  return ok;
+bool get_bytes(PyObject* o, int64_t* out) {
+  return of_tensor(o, [&](const at::Tensor& t) {
+    *out = static_cast<int64_t>(t.nbytes());
+    return true;
+  });
 }
 
 // A one-dimensional table of 4-byte elements ('f' or 'i'), borrowed for the call.
@@ -142,9 +140,10 @@ bool get_current_stream(PyObject* stream, void** out) {
 
 // Y's dtype as the library names it.
 bool get_y_dtype(PyObject* y, int32_t* out) {
-  PyObject* d = dtype_of(y);
-  *out = d == t_f32 ? RPTQ_DTYPE_F32 : RPTQ_DTYPE_BF16;
-  return d == t_f32 || d == t_bf16;
+  return of_tensor(y, [&](const at::Tensor& t) {
+    *out = t.scalar_type() == at::kFloat ? RPTQ_DTYPE_F32 : RPTQ_DTYPE_BF16;
+    return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
+  });
 }
 
 template <typename F>
@@ -163,11 +162,11 @@ PyObject* ln_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t *perm, *xsum, d, relu, bits;
   int64_t M;
   Table off, s, inv, z;
-  if (n != 17 || f_ln_quant == nullptr || !get_tensor(a[0], t_bf16, false, &x) || !get_i64(a[1], &M) || !get_i32(a[2], &d) ||
-      !get_tensor(a[3], t_f32, true, &gamma) || !get_tensor(a[4], t_f32, true, &beta) || !get_f32(a[5], &eps) ||
-      !get_flag(a[6], &relu) || !get_tensor(a[7], t_i32, false, &perm) || !off.get(a[8], 'i') || !s.get(a[9], 'f') ||
-      !inv.get(a[10], 'f') || !z.get(a[11], 'i') || !get_i32(a[12], &bits) || !get_tensor(a[13], nullptr, false, &codes) ||
-      !get_tensor(a[14], t_i32, true, &xsum) || !get_tensor(a[15], t_f32, true, &rowterm) || !get_current_stream(a[16], &stream))
+  if (n != 17 || f_ln_quant == nullptr || !get_tensor(a[0], at::kBFloat16, false, &x) || !get_i64(a[1], &M) || !get_i32(a[2], &d) ||
+      !get_tensor(a[3], at::kFloat, true, &gamma) || !get_tensor(a[4], at::kFloat, true, &beta) || !get_f32(a[5], &eps) ||
+      !get_flag(a[6], &relu) || !get_tensor(a[7], at::kInt, false, &perm) || !off.get(a[8], 'i') || !s.get(a[9], 'f') ||
+      !inv.get(a[10], 'f') || !z.get(a[11], 'i') || !get_i32(a[12], &bits) || !get_tensor(a[13], kAny, false, &codes) ||
+      !get_tensor(a[14], at::kInt, true, &xsum) || !get_tensor(a[15], at::kFloat, true, &rowterm) || !get_current_stream(a[16], &stream))
     Py_RETURN_NONE;
   return run([&] {
     return f_ln_quant(x, M, d, gamma, beta, eps, relu, perm, off.ints(), off.size() - 1, s.floats(), inv.floats(), z.ints(),
@@ -182,11 +181,11 @@ PyObject* cluster_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t *zw, bits, N, y_dtype;
   int64_t M;
   Table off, sx;
-  if (n != 13 || f_cluster_gemm == nullptr || !get_tensor(a[0], nullptr, false, &codes) || !get_i64(a[1], &M) ||
-      !get_i32(a[2], &bits) || !get_tensor(a[3], nullptr, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
-      !sx.get(a[6], 'f') || !get_tensor(a[7], t_f32, false, &sw) || !get_tensor(a[8], t_i32, false, &zw) ||
-      !get_tensor(a[9], t_f32, false, &colterm) || !get_tensor(a[10], t_f32, false, &rowterm) ||
-      !get_y_dtype(a[11], &y_dtype) || !get_tensor(a[11], nullptr, false, &y) || !get_current_stream(a[12], &stream))
+  if (n != 13 || f_cluster_gemm == nullptr || !get_tensor(a[0], kAny, false, &codes) || !get_i64(a[1], &M) ||
+      !get_i32(a[2], &bits) || !get_tensor(a[3], kAny, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
+      !sx.get(a[6], 'f') || !get_tensor(a[7], at::kFloat, false, &sw) || !get_tensor(a[8], at::kInt, false, &zw) ||
+      !get_tensor(a[9], at::kFloat, false, &colterm) || !get_tensor(a[10], at::kFloat, false, &rowterm) ||
+      !get_y_dtype(a[11], &y_dtype) || !get_tensor(a[11], kAny, false, &y) || !get_current_stream(a[12], &stream))
     Py_RETURN_NONE;
   return run([&] {
     return f_cluster_gemm(codes, M, bits, wq, N, off.ints(), off.size() - 1, sx.floats(), sw, zw, colterm, rowterm, y,
@@ -202,13 +201,13 @@ PyObject* cluster_gemm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t *zw, bits, N, relu, next_bits;
   int64_t M, bytes;
   Table off, sx, noff, ns, ni, nz;
-  if (n != 21 || f_cluster_gemm_quant == nullptr || !get_tensor(a[0], nullptr, false, &codes) || !get_i64(a[1], &M) ||
-      !get_i32(a[2], &bits) || !get_tensor(a[3], nullptr, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
-      !sx.get(a[6], 'f') || !get_tensor(a[7], t_f32, false, &sw) || !get_tensor(a[8], t_i32, false, &zw) ||
-      !get_tensor(a[9], t_f32, false, &colterm) || !get_tensor(a[10], t_f32, false, &rowterm) || !get_flag(a[11], &relu) ||
+  if (n != 21 || f_cluster_gemm_quant == nullptr || !get_tensor(a[0], kAny, false, &codes) || !get_i64(a[1], &M) ||
+      !get_i32(a[2], &bits) || !get_tensor(a[3], kAny, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
+      !sx.get(a[6], 'f') || !get_tensor(a[7], at::kFloat, false, &sw) || !get_tensor(a[8], at::kInt, false, &zw) ||
+      !get_tensor(a[9], at::kFloat, false, &colterm) || !get_tensor(a[10], at::kFloat, false, &rowterm) || !get_flag(a[11], &relu) ||
       !noff.get(a[12], 'i') || !ns.get(a[13], 'f') || !ni.get(a[14], 'f') || !nz.get(a[15], 'i') ||
-      !get_i32(a[16], &next_bits) || !get_tensor(a[17], nullptr, false, &next_codes) ||
-      !get_tensor(a[18], t_f32, false, &next_rowterm) || !get_tensor(a[19], nullptr, false, &workspace) ||
+      !get_i32(a[16], &next_bits) || !get_tensor(a[17], kAny, false, &next_codes) ||
+      !get_tensor(a[18], at::kFloat, false, &next_rowterm) || !get_tensor(a[19], kAny, false, &workspace) ||
       !get_bytes(a[19], &bytes) || !get_current_stream(a[20], &stream))
     Py_RETURN_NONE;
   return run([&] {
@@ -225,9 +224,9 @@ PyObject* cluster_rowsums(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t bits;
   int64_t M;
   Table off, sx, zx;
-  if (n != 8 || f_cluster_rowsums == nullptr || !get_tensor(a[0], nullptr, false, &codes) || !get_i64(a[1], &M) ||
+  if (n != 8 || f_cluster_rowsums == nullptr || !get_tensor(a[0], kAny, false, &codes) || !get_i64(a[1], &M) ||
       !get_i32(a[2], &bits) || !off.get(a[3], 'i') || !sx.get(a[4], 'f') || !zx.get(a[5], 'i') ||
-      !get_tensor(a[6], t_f32, false, &rowsums) || !get_current_stream(a[7], &stream))
+      !get_tensor(a[6], at::kFloat, false, &rowsums) || !get_current_stream(a[7], &stream))
     Py_RETURN_NONE;
   return run([&] { return f_cluster_rowsums(codes, M, bits, off.ints(), off.size() - 1, sx.floats(), zx.ints(), rowsums, stream); });
 }
@@ -239,11 +238,11 @@ PyObject* cluster_gemm_cw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t bits, N, y_dtype;
   int64_t M;
   Table off;
-  if (n != 12 || f_cluster_gemm_cw == nullptr || !get_tensor(a[0], nullptr, false, &codes) || !get_i64(a[1], &M) ||
-      !get_i32(a[2], &bits) || !get_tensor(a[3], nullptr, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
-      !get_tensor(a[6], t_f32, false, &scale) || !get_tensor(a[7], t_f32, false, &cross) ||
-      !get_tensor(a[8], t_f32, false, &colterm) || !get_tensor(a[9], t_f32, false, &rowsums) ||
-      !get_y_dtype(a[10], &y_dtype) || !get_tensor(a[10], nullptr, false, &y) || !get_current_stream(a[11], &stream))
+  if (n != 12 || f_cluster_gemm_cw == nullptr || !get_tensor(a[0], kAny, false, &codes) || !get_i64(a[1], &M) ||
+      !get_i32(a[2], &bits) || !get_tensor(a[3], kAny, false, &wq) || !get_i32(a[4], &N) || !off.get(a[5], 'i') ||
+      !get_tensor(a[6], at::kFloat, false, &scale) || !get_tensor(a[7], at::kFloat, false, &cross) ||
+      !get_tensor(a[8], at::kFloat, false, &colterm) || !get_tensor(a[9], at::kFloat, false, &rowsums) ||
+      !get_y_dtype(a[10], &y_dtype) || !get_tensor(a[10], kAny, false, &y) || !get_current_stream(a[11], &stream))
     Py_RETURN_NONE;
   return run([&] {
     return f_cluster_gemm_cw(codes, M, bits, wq, N, off.ints(), off.size() - 1, scale, cross, colterm, rowsums, y, y_dtype, stream);
@@ -256,9 +255,9 @@ PyObject* kv_call(PyObject* const* a, Py_ssize_t n, bool quant) {
   int32_t d, bits;
   int64_t T;
   if (n != 7 || (quant ? f_kv_quant == nullptr : f_kv_dequant == nullptr) ||
-      !get_tensor(a[0], quant ? t_bf16 : nullptr, false, &from) || !get_i64(a[1], &T) || !get_i32(a[2], &d) ||
-      !get_tensor(a[3], nullptr, false, &table) || !get_i32(a[4], &bits) ||
-      !get_tensor(a[5], quant ? nullptr : t_bf16, false, &to) || !get_current_stream(a[6], &stream))
+      !get_tensor(a[0], quant ? at::kBFloat16 : kAny, false, &from) || !get_i64(a[1], &T) || !get_i32(a[2], &d) ||
+      !get_tensor(a[3], kAny, false, &table) || !get_i32(a[4], &bits) ||
+      !get_tensor(a[5], quant ? kAny : at::kBFloat16, false, &to) || !get_current_stream(a[6], &stream))
     Py_RETURN_NONE;
   return run([&] { return quant ? f_kv_quant(from, T, d, table, bits, to, stream) : f_kv_dequant(from, T, d, table, bits, to, stream); });
 }
@@ -279,53 +278,43 @@ bool get_place(PyObject* stream, int64_t* device, void** out) {
   return (ok && !PyErr_Occurred()) || no_error();
 }
 
-bool int_of(PyObject* owned, int64_t* out) {
-  if (owned == nullptr) return no_error();
-  const bool ok = get_i64(owned, out);
-  Py_DECREF(owned);
-  return ok;
-}
-
-// Address of a tensor of that dtype (any if NULL) on that device.
+// Whether a tensor is of that dtype on that device, and its address.
 template <typename T>
-bool get_on(PyObject* t, PyObject* dtype, int64_t device, T** out) {
-  int64_t at;
-  if (!int_of(PyObject_CallMethodNoArgs(t, n_get_device), &at) || at != device || at < 0) return false;
-  if (dtype != nullptr && dtype_of(t) != dtype) return false;
-  PyObject* p = PyObject_CallMethodNoArgs(t, n_data_ptr);
-  if (p == nullptr) return no_error();
-  *out = static_cast<T*>(PyLong_Check(p) ? PyLong_AsVoidPtr(p) : nullptr);
-  Py_DECREF(p);
-  return !PyErr_Occurred() || no_error();
+bool is_on(const at::Tensor& t, ScalarType type, int64_t device, T** out) {
+  if (!t.is_cuda() || t.get_device() != device || !is_type(t, type)) return false;
+  *out = static_cast<T*>(t.data_ptr());
+  return true;
 }
 
-// The same of a contiguous one with `bytes` bytes.
+// A contiguous one, and how many bytes it has.
 template <typename T>
-bool get_whole(PyObject* t, PyObject* dtype, int64_t device, T** out, int64_t* bytes) {
-  return get_on(t, dtype, device, out) && is_true(PyObject_CallMethodNoArgs(t, n_is_contiguous)) && get_bytes(t, bytes);
+bool get_whole(PyObject* o, ScalarType type, int64_t device, T** out, int64_t* bytes) {
+  return of_tensor(o, [&](const at::Tensor& t) {
+    *bytes = static_cast<int64_t>(t.nbytes());
+    return is_on(t, type, device, out) && t.is_contiguous();
+  });
 }
 
-// The first `n` entries of a tuple of exactly so many.
-bool get_sizes(PyObject* owned, int n, int64_t* out) {
-  if (owned == nullptr) return no_error();
-  bool ok = PyTuple_Check(owned) && PyTuple_GET_SIZE(owned) == n;
-  for (int i = 0; ok && i < n; ++i) ok = get_i64(PyTuple_GET_ITEM(owned, i), out + i);
-  Py_DECREF(owned);
-  return ok;
+// The sizes of a tensor of exactly so many.
+bool get_sizes(PyObject* o, int n, int64_t* out) {
+  return of_tensor(o, [&](const at::Tensor& t) {
+    if (t.dim() != n) return false;
+    for (int i = 0; i < n; ++i) out[i] = t.size(i);
+    return true;
+  });
 }
 
 // A two-dimensional tensor with contiguous rows, at least one of them.
 struct Rows {
   void* at;
   int64_t rows, cols, ld;
-  bool get(PyObject* t, PyObject* dtype, int64_t device) {
-    int64_t size[2], step[2];
-    if (!get_on(t, dtype, device, &at) || !get_sizes(PyObject_GetAttr(t, n_shape), 2, size) ||
-        !get_sizes(PyObject_CallMethodNoArgs(t, n_stride), 2, step))
-      return false;
-    rows = size[0], cols = size[1];
-    ld = rows > 1 ? step[0] : cols;
-    return rows >= 1 && cols >= 1 && cols <= INT32_MAX && (cols == 1 || step[1] == 1);
+  bool get(PyObject* o, ScalarType type, int64_t device) {
+    return of_tensor(o, [&](const at::Tensor& t) {
+      if (t.dim() != 2 || !is_on(t, type, device, &at)) return false;
+      rows = t.size(0), cols = t.size(1);
+      ld = rows > 1 ? t.stride(0) : cols;
+      return rows >= 1 && cols >= 1 && cols <= INT32_MAX && (cols == 1 || t.stride(1) == 1);
+    });
   }
 };
 
@@ -339,16 +328,16 @@ struct Pages {
     int64_t kb, vb, ktb, vtb;
     if (d < 1 || d > RPTQ_MAX_CHANNELS) return false;
     const int64_t size = static_cast<int64_t>(f_kv_page_bytes(static_cast<int32_t>(d), page_size, bits));
-    if (size == 0 || !get_whole(kp, t_u8, device, &k, &kb) || !get_whole(vp, t_u8, device, &v, &vb) || kb != vb || kb < size || kb % size != 0)
+    if (size == 0 || !get_whole(kp, at::kByte, device, &k, &kb) || !get_whole(vp, at::kByte, device, &v, &vb) || kb != vb || kb < size || kb % size != 0)
       return false;
     n = kb / size;
-    return get_whole(kt, nullptr, device, &k_table, &ktb) && get_whole(vt, nullptr, device, &v_table, &vtb) && ktb == 16 * d && vtb == 16 * d;
+    return get_whole(kt, kAny, device, &k_table, &ktb) && get_whole(vt, kAny, device, &v_table, &vtb) && ktb == 16 * d && vtb == 16 * d;
   }
 };
 
 bool get_slots(PyObject* t, int64_t device, int64_t rows, int64_t** out) {
   int64_t bytes, size;
-  return get_whole(t, t_i64, device, out, &bytes) && get_sizes(PyObject_GetAttr(t, n_shape), 1, &size) && size == rows;
+  return get_whole(t, at::kLong, device, out, &bytes) && get_sizes(t, 1, &size) && size == rows;
 }
 
 // (k, v, slots, k_table, v_table, bits, k_pages, v_pages, page_size, stream)
@@ -359,7 +348,7 @@ PyObject* kv_quant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t bits, page_size;
   void* stream;
   if (n != 10 || f_kv_quant_paged == nullptr || !get_place(a[9], &device, &stream) || !get_i32(a[5], &bits) || !get_i32(a[8], &page_size) ||
-      !k.get(a[0], t_bf16, device) || !v.get(a[1], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !k.get(a[0], at::kBFloat16, device) || !v.get(a[1], at::kBFloat16, device) || k.rows != v.rows || k.cols != v.cols ||
       !get_slots(a[2], device, k.rows, &slots) || !p.get(a[6], a[7], a[3], a[4], device, k.cols, page_size, bits))
     Py_RETURN_NONE;
   return run([&] {
@@ -376,7 +365,7 @@ PyObject* kv_dequant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t bits, page_size;
   void* stream;
   if (n != 10 || f_kv_dequant_paged == nullptr || !get_place(a[9], &device, &stream) || !get_i32(a[3], &bits) || !get_i32(a[2], &page_size) ||
-      !k.get(a[7], t_bf16, device) || !v.get(a[8], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !k.get(a[7], at::kBFloat16, device) || !v.get(a[8], at::kBFloat16, device) || k.rows != v.rows || k.cols != v.cols ||
       !get_slots(a[4], device, k.rows, &slots) || !p.get(a[0], a[1], a[5], a[6], device, k.cols, page_size, bits))
     Py_RETURN_NONE;
   return run([&] {
@@ -395,14 +384,14 @@ PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *workspace, *stream;
   if (n != 17 || f_attend_paged == nullptr || !get_place(a[16], &device, &stream) || !get_i32(a[1], &n_q) || !get_i32(a[2], &n_kv) ||
       !get_i32(a[3], &hd) || !get_f32(a[4], &scale) || !get_i32(a[7], &bits) || !get_i32(a[10], &page_size) || n_q < 1 || n_kv < 1 || hd < 1 ||
-      !q.get(a[0], t_bf16, device) || q.cols != static_cast<int64_t>(n_q) * hd || q.rows > INT32_MAX)
+      !q.get(a[0], at::kBFloat16, device) || q.cols != static_cast<int64_t>(n_q) * hd || q.rows > INT32_MAX)
     Py_RETURN_NONE;
   if (!p.get(a[8], a[9], a[5], a[6], device, static_cast<int64_t>(n_kv) * hd, page_size, bits) || !get_y_dtype(a[13], &out_dtype) ||
-      !out.get(a[13], nullptr, device) || out.rows != q.rows || out.cols != q.cols || !table.get(a[11], t_i32, device) ||
-      table.rows != q.rows || !get_whole(a[12], t_i32, device, &lens, &lens_bytes) ||
-      !get_sizes(PyObject_GetAttr(a[12], n_shape), 1, &b) || b != q.rows || !get_whole(a[15], nullptr, device, &workspace, &ws_bytes))
+      !out.get(a[13], kAny, device) || out.rows != q.rows || out.cols != q.cols || !table.get(a[11], at::kInt, device) ||
+      table.rows != q.rows || !get_whole(a[12], at::kInt, device, &lens, &lens_bytes) ||
+      !get_sizes(a[12], 1, &b) || b != q.rows || !get_whole(a[15], kAny, device, &workspace, &ws_bytes))
     Py_RETURN_NONE;
-  if (a[14] != Py_None && (!get_whole(a[14], t_f32, device, &lse, &lse_bytes) || lse_bytes < 4 * q.rows * n_q)) Py_RETURN_NONE;
+  if (a[14] != Py_None && (!get_whole(a[14], at::kFloat, device, &lse, &lse_bytes) || lse_bytes < 4 * q.rows * n_q)) Py_RETURN_NONE;
   return run([&] {
     return f_attend_paged(q.at, q.ld, static_cast<int32_t>(q.rows), n_q, n_kv, hd, scale, p.k_table, p.v_table, bits, p.k, p.v, p.n,
                           page_size, static_cast<int32_t*>(table.at), table.ld, static_cast<int32_t>(table.cols), lens, out.at, out.ld,
@@ -418,9 +407,9 @@ bool get_f64(PyObject* o, double* out) {
 
 // A contiguous tensor with one entry of that type per row.
 template <typename T>
-bool get_column(PyObject* t, PyObject* dtype, int64_t device, int64_t rows, T** out) {
+bool get_column(PyObject* t, ScalarType dtype, int64_t device, int64_t rows, T** out) {
   int64_t bytes, size;
-  return get_whole(t, dtype, device, out, &bytes) && get_sizes(PyObject_GetAttr(t, n_shape), 1, &size) && size == rows;
+  return get_whole(t, dtype, device, out, &bytes) && get_sizes(t, 1, &size) && size == rows;
 }
 
 // The arguments of a rotation: (head_dim, rotary_dim, interleaved, freqs, amplitude).
@@ -429,7 +418,7 @@ struct Turn {
   double *freqs, amplitude;
   bool get(PyObject* const* a, int64_t device) {
     return get_i32(a[0], &hd) && get_i32(a[1], &rot) && get_flag(a[2], &interleaved) && hd >= 1 && rot >= 2 && rot % 2 == 0 &&
-           get_column(a[3], t_f64, device, rot / 2, &freqs) && get_f64(a[4], &amplitude);
+           get_column(a[3], at::kDouble, device, rot / 2, &freqs) && get_f64(a[4], &amplitude);
   }
 };
 
@@ -441,8 +430,8 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t *positions, x_dtype, y_dtype;
   void* stream;
   if (n != 9 || f_rope == nullptr || !get_place(a[8], &device, &stream) || !get_y_dtype(a[0], &x_dtype) || !get_y_dtype(a[1], &y_dtype) ||
-      !x.get(a[0], nullptr, device) || !y.get(a[1], nullptr, device) || x.rows != y.rows || x.cols != y.cols ||
-      !get_column(a[2], t_i32, device, x.rows, &positions) || !t.get(a + 3, device) || x.cols % t.hd != 0)
+      !x.get(a[0], kAny, device) || !y.get(a[1], kAny, device) || x.rows != y.rows || x.cols != y.cols ||
+      !get_column(a[2], at::kInt, device, x.rows, &positions) || !t.get(a + 3, device) || x.cols % t.hd != 0)
     Py_RETURN_NONE;
   return run([&] {
     return f_rope(x.at, x_dtype, x.ld, y.at, y_dtype, y.ld, positions, x.rows, static_cast<int32_t>(x.cols / t.hd), t.hd, t.rot, t.interleaved,
@@ -460,12 +449,12 @@ PyObject* rope_quant_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t *positions, bits, page_size;
   void* stream;
   if (n != 18 || f_rope_quant_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[13], &bits) || !get_i32(a[16], &page_size) ||
-      !k.get(a[2], t_bf16, device) || !v.get(a[3], t_bf16, device) || k.rows != v.rows || k.cols != v.cols ||
-      !get_column(a[4], t_i32, device, k.rows, &positions) || !get_slots(a[5], device, k.rows, &slots) || !t.get(a + 6, device) ||
+      !k.get(a[2], at::kBFloat16, device) || !v.get(a[3], at::kBFloat16, device) || k.rows != v.rows || k.cols != v.cols ||
+      !get_column(a[4], at::kInt, device, k.rows, &positions) || !get_slots(a[5], device, k.rows, &slots) || !t.get(a + 6, device) ||
       k.cols % t.hd != 0 || !p.get(a[14], a[15], a[11], a[12], device, k.cols, page_size, bits))
     Py_RETURN_NONE;
   if (a[0] != Py_None || a[1] != Py_None) {
-    if (!q.get(a[0], t_bf16, device) || !out.get(a[1], t_bf16, device) || q.rows != k.rows || out.rows != q.rows || out.cols != q.cols ||
+    if (!q.get(a[0], at::kBFloat16, device) || !out.get(a[1], at::kBFloat16, device) || q.rows != k.rows || out.rows != q.rows || out.cols != q.cols ||
         q.cols % t.hd != 0)
       Py_RETURN_NONE;
   }
@@ -483,8 +472,8 @@ struct Records {
   int64_t capacity;
   bool get(PyObject* w, PyObject* pos, int64_t device, int64_t B, int64_t heads) {
     int64_t bytes, a[3], b[3];
-    if (!get_whole(w, t_f32, device, &weights, &bytes) || !get_whole(pos, t_i32, device, &positions, &bytes) ||
-        !get_sizes(PyObject_GetAttr(w, n_shape), 3, a) || !get_sizes(PyObject_GetAttr(pos, n_shape), 3, b))
+    if (!get_whole(w, at::kFloat, device, &weights, &bytes) || !get_whole(pos, at::kInt, device, &positions, &bytes) ||
+        !get_sizes(w, 3, a) || !get_sizes(pos, 3, b))
       return false;
     capacity = a[2];
     return a[0] == B && a[1] == heads && b[0] == B && b[1] == heads && b[2] == capacity && capacity >= 1;
@@ -503,15 +492,15 @@ PyObject* attend_weights_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *stream, *workspace = nullptr;
   if (n != 19 || f_attend_weights_paged == nullptr || !get_place(a[18], &device, &stream) || !get_i32(a[1], &queries) || !get_i32(a[2], &n_q) ||
       !get_i32(a[3], &n_kv) || !get_i32(a[4], &hd) || !get_f32(a[5], &scale) || !get_i32(a[7], &bits) || !get_i32(a[9], &page_size) ||
-      !get_i32(a[14], &fresh) || queries < 1 || n_q < 1 || n_kv < 1 || hd < 1 || !q.get(a[0], t_bf16, device) ||
-      q.cols != static_cast<int64_t>(n_q) * hd || !table.get(a[10], t_i32, device) || table.rows > INT32_MAX || q.rows != table.rows * queries)
+      !get_i32(a[14], &fresh) || queries < 1 || n_q < 1 || n_kv < 1 || hd < 1 || !q.get(a[0], at::kBFloat16, device) ||
+      q.cols != static_cast<int64_t>(n_q) * hd || !table.get(a[10], at::kInt, device) || table.rows > INT32_MAX || q.rows != table.rows * queries)
     Py_RETURN_NONE;
-  if (!p.get(a[8], a[8], a[6], a[6], device, static_cast<int64_t>(n_kv) * hd, page_size, bits) || !get_column(a[11], t_i32, device, table.rows, &lens) ||
-      !get_whole(a[12], t_f32, device, &lse, &lse_bytes) || !get_sizes(PyObject_GetAttr(a[12], n_shape), 2, shape) || shape[0] != q.rows ||
+  if (!p.get(a[8], a[8], a[6], a[6], device, static_cast<int64_t>(n_kv) * hd, page_size, bits) || !get_column(a[11], at::kInt, device, table.rows, &lens) ||
+      !get_whole(a[12], at::kFloat, device, &lse, &lse_bytes) || !get_sizes(a[12], 2, shape) || shape[0] != q.rows ||
       shape[1] != n_q || !w.get(a[15], a[16], device, table.rows, n_kv))
     Py_RETURN_NONE;
-  if (a[13] != Py_None && !get_column(a[13], t_i32, device, table.rows, &positions)) Py_RETURN_NONE;
-  if (a[17] != Py_None && !get_whole(a[17], nullptr, device, &workspace, &ws_bytes)) Py_RETURN_NONE;
+  if (a[13] != Py_None && !get_column(a[13], at::kInt, device, table.rows, &positions)) Py_RETURN_NONE;
+  if (a[17] != Py_None && !get_whole(a[17], kAny, device, &workspace, &ws_bytes)) Py_RETURN_NONE;
   return run([&] {
     return f_attend_weights_paged(q.at, q.ld, static_cast<int32_t>(table.rows), queries, n_q, n_kv, hd, scale, p.k_table, bits, p.k, p.n, page_size,
                                   static_cast<int32_t*>(table.at), table.ld, static_cast<int32_t>(table.cols), lens, lse, positions, fresh,
@@ -530,13 +519,13 @@ PyObject* evict_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *workspace, *stream;
   if (n != 18 || f_evict_paged == nullptr || !get_place(a[17], &device, &stream) || !get_i32(a[0], &n_kv) || !get_i32(a[1], &hd) ||
       !get_i32(a[2], &bits) || !get_i32(a[5], &page_size) || !get_i32(a[10], &budget) || !get_i32(a[11], &first) || !get_i32(a[12], &recent) ||
-      n_kv < 1 || hd < 1 || static_cast<int64_t>(n_kv) * hd > RPTQ_MAX_CHANNELS || !table.get(a[6], t_i32, device) || table.rows > INT32_MAX)
+      n_kv < 1 || hd < 1 || static_cast<int64_t>(n_kv) * hd > RPTQ_MAX_CHANNELS || !table.get(a[6], at::kInt, device) || table.rows > INT32_MAX)
     Py_RETURN_NONE;
   const int64_t size = static_cast<int64_t>(f_kv_page_bytes(n_kv * hd, page_size, bits));
-  if (size == 0 || !get_whole(a[3], t_u8, device, &k, &kb) || !get_whole(a[4], t_u8, device, &v, &vb) || kb != vb || kb < size || kb % size != 0 ||
-      !get_column(a[7], t_i32, device, table.rows, &lens) || !get_column(a[15], t_i32, device, table.rows, &lens_out) ||
+  if (size == 0 || !get_whole(a[3], at::kByte, device, &k, &kb) || !get_whole(a[4], at::kByte, device, &v, &vb) || kb != vb || kb < size || kb % size != 0 ||
+      !get_column(a[7], at::kInt, device, table.rows, &lens) || !get_column(a[15], at::kInt, device, table.rows, &lens_out) ||
       !w.get(a[8], a[9], device, table.rows, n_kv) || !out.get(a[13], a[14], device, table.rows, n_kv) || out.capacity != w.capacity ||
-      !get_whole(a[16], nullptr, device, &workspace, &ws_bytes))
+      !get_whole(a[16], kAny, device, &workspace, &ws_bytes))
     Py_RETURN_NONE;
   return run([&] {
     return f_evict_paged(static_cast<int32_t>(table.rows), n_kv, hd, bits, k, v, kb / size, page_size, static_cast<int32_t*>(table.at), table.ld,
@@ -561,9 +550,7 @@ bool set_entry(PyObject* addresses, const char* name, F* f) {
 PyObject* setup(PyObject*, PyObject* args) {
   PyObject *addresses, *objects;
   if (!PyArg_ParseTuple(args, "O!O!", &PyDict_Type, &addresses, &PyDict_Type, &objects)) return nullptr;
-  const struct { const char* name; PyObject** at; } wanted[] = {
-      {"bfloat16", &t_bf16}, {"float32", &t_f32}, {"int32", &t_i32}, {"int64", &t_i64}, {"uint8", &t_u8}, {"float64", &t_f64},
-      {"get_device", &get_device}, {"get_stream", &get_stream}};
+  const struct { const char* name; PyObject** at; } wanted[] = {{"get_device", &get_device}, {"get_stream", &get_stream}};
   for (const auto& w : wanted) {
     PyObject* o = PyDict_GetItemString(objects, w.name);
     if (o == nullptr) return PyErr_Format(PyExc_KeyError, "%s", w.name);
@@ -595,14 +582,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 }  // namespace
 
 PyMODINIT_FUNC PyInit__calls(void) {
-  n_is_cuda = PyUnicode_InternFromString("is_cuda");
-  n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  n_dtype = PyUnicode_InternFromString("dtype");
-  n_data_ptr = PyUnicode_InternFromString("data_ptr");
-  n_nbytes = PyUnicode_InternFromString("nbytes");
-  n_get_device = PyUnicode_InternFromString("get_device");
-  n_shape = PyUnicode_InternFromString("shape");
-  n_stride = PyUnicode_InternFromString("stride");
-  if (!n_is_cuda || !n_is_contiguous || !n_dtype || !n_data_ptr || !n_nbytes || !n_get_device || !n_shape || !n_stride) return nullptr;
-  return PyModule_Create(&module);
+  PyObject* m = PyModule_Create(&module);
+  if (m != nullptr && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) != 0) Py_CLEAR(m);
+  return m;
 }
