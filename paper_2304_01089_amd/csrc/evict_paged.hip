@@ -75,9 +75,9 @@ __device__ __forceinline__ void move_records(const EvictArgs& a, int64_t base, c
 }
 
 // Rows number first, first + step, ... of the lists: the thread's `which`-th of 2 units pieces.  page_of: a page's number.
-template <typename V, typename P>
-__device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h, P&& page_of, const int32_t* to, const int32_t* from, int first, int end,
-                                            int step, int which) {
+template <typename V, typename P, typename L>
+__device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h, P&& page_of, L to, L from, int first, int end, int step,
+                                            int which) {
   const int row_bytes = 16 * a.bits, head_bytes = a.hd * a.bits / 8;
   const bool values = which >= units;
   const int off = (which - (values ? units : 0)) * static_cast<int>(sizeof(V));       // of the head's row
@@ -109,9 +109,8 @@ __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h
   for (; i < end; i += 4 * step) some(std::integral_constant<int, 4>{}, i);
 }
 
-template <int THREADS, typename P>
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictPlan& p, int h, P&& page_of, const int32_t* to, const int32_t* from, int moves,
-                                          int begin) {
+template <int THREADS, typename P, typename L>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictPlan& p, int h, P&& page_of, L to, L from, int moves, int begin) {
   const int each = 2 * p.units, rows = THREADS / each, row = static_cast<int>(threadIdx.x) / each, which = static_cast<int>(threadIdx.x) - row * each;
   if (row >= rows) return;
   if (p.vec == 16) move_pieces<Bytes16>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
@@ -119,10 +118,28 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictPlan& p
   else move_pieces<uint32_t>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
 }
 
-__device__ __forceinline__ int wave_max_int(int v) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v = max(v, __shfl_xor(v, s, kWave));
-  return v;
+// A list of one token.
+struct One {
+  int token;
+  __device__ __forceinline__ int operator[](int) const { return token; }
+};
+
+// The wave's largest, in every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_larger(uint32_t v) {
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ uint32_t wave_largest(uint32_t v) {
+  v = dpp_larger<0x111, 0xf>(v);
+  v = dpp_larger<0x112, 0xf>(v);
+  v = dpp_larger<0x114, 0xf>(v);
+  v = dpp_larger<0x118, 0xf>(v);
+  v = dpp_larger<0x142, 0xa>(v);
+  v = dpp_larger<0x143, 0xc>(v);
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ int wave_largest_int(int v) {
+  return static_cast<int>(wave_largest(static_cast<uint32_t>(v) ^ 0x80000000u) ^ 0x80000000u);
 }
 
 // Over the 16 lanes of a row.
@@ -215,7 +232,7 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
           if (start + (first + i) * 64 + lane < end) newest = max(newest, pos[i]);
       }
     }
-    newest = wave_max_int(newest);
+    newest = wave_largest_int(newest);
   }
   const bool wave_gone = __ballot(gone) != 0;
   if (lane == 0) sums[0][0][wave] = newest, sums[0][1][wave] = wave_gone;
@@ -224,7 +241,7 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     leave();
     return;
   }
-  if (a.recent > 0) newest = wave_max_int(sums[0][0][lane & (WAVES - 1)]);
+  if (a.recent > 0) newest = wave_largest_int(sums[0][0][lane & (WAVES - 1)]);
 
   // The run's keys from its records: 0 where no token of the wave's is.  (A weight's is at least 0x007fffff, minus infinity's.)
   uint32_t keys[kRun];
@@ -263,8 +280,11 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     }
   };
   auto count = [&](int32_t* mine, uint32_t k, int shift, uint32_t size) __attribute__((always_inline)) { atomicAdd(&mine[k >> shift & (size - 1)], 1); };
-  // Every key once: to where it will be looked at again, and counted by its first eleven bits.  Records go to their place (where a
-  // token leaves, the one that comes is written later).
+  // Every key once: to where it will be looked at again, and counted by its first twelve bits - or, where only one token leaves,
+  // compared with the smallest so far.  Records go to their place (where a token leaves, the one that comes is written later).
+  const bool one = n - a.budget == 1;
+  uint32_t least = ~0u;                                        // the lane's smallest key, and the last token that has it
+  int leaves = -1;
 #pragma unroll 1
   for (int first = 0; first < items; first += kRun) {
     if (KEYS == Keys::made ? items > kRun : KEYS == Keys::lds) read(first);
@@ -272,6 +292,12 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
       if (first + i >= items) continue;
+      if (one) {
+        const bool less = keys[i] != 0 && keys[i] <= least;
+        least = less ? keys[i] : least;
+        leaves = less ? start + (first + i) * 64 + lane : leaves;
+        continue;
+      }
       if (KEYS == Keys::lds) key_lds[(wave * kLdsItems + first + i) * 64 + lane] = keys[i];
       if (keys[i] != 0) count(bins, keys[i], 20, kFirstBins);
     }
@@ -285,6 +311,30 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
       }
     }
     if (KEYS == Keys::registers) break;
+  }
+
+  if (one) {
+    // The smallest key leaves, of equal ones the last token's; the sequence's last token comes into its place.
+    const uint32_t mine = ~wave_largest(~least);
+    const int last = wave_largest_int(least == mine ? leaves : -1);
+    if (lane == 0) sums[1][0][wave] = static_cast<int32_t>(mine), sums[1][1][wave] = last;
+    __syncthreads();
+    const uint32_t of_wave = static_cast<uint32_t>(sums[1][0][lane & (WAVES - 1)]);
+    const int hole = wave_largest_int(of_wave == ~wave_largest(~of_wave) ? sums[1][1][lane & (WAVES - 1)] : -1);
+    if (hole < a.budget) {
+      const One to{hole}, from{a.budget};
+      if (pages <= kHeldPages) move_rows<kThreads>(a, plan, h, [&](int page) { return ids[page]; }, to, from, 1, 0);
+      else move_rows<kThreads>(a, plan, h, [&](int page) { return pt[page]; }, to, from, 1, 0);
+      if (tid == kThreads - 1) {
+        const float weight = weights[a.budget];
+        const int32_t position = positions[a.budget];
+        weights_out[hole] = weight;
+        positions_out[hole] = position;
+      }
+    }
+    if (!plan.few && tid == 0) workspace[blockIdx.x] = 0;
+    if (h == 0 && tid == 0) a.lens_out[b] = a.budget;
+    return;
   }
 
   // ---- the budget-th largest key, from the top: twelve bits, ten and ten ----------------------------------------------

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import bounding
-from test_gpu_bounding import records, window
+from test_gpu_bounding import evicted, records, window
 from test_gpu_paged import Batch, dev, dev_bf16
 
 pytestmark = pytest.mark.gpu
@@ -162,3 +162,27 @@ def test_eviction_from_as_many_tokens_as_there_may_be(rp):
     for now, was in zip((b.cache.k_pages, b.cache.v_pages), before):
         was[ids[hole // 4096 % 2], :, hole % 4096] = was[ids[1], :, 4095].clone()
         assert torch.equal(now, was)
+
+
+@pytest.mark.parametrize("what", ["random", "ties", "all equal", "the last one", "nan and infinities", "all safe", "none safe"])
+@pytest.mark.parametrize("n", [2, 65, 700, 4097, 8193, 20000, 32769])
+def test_one_token_leaves(rp, n, what):
+    """A batch at its budget and a token more, for every way of holding the keys: the smallest weight's leaves, of equal ones the last."""
+    b = Batch(rp, [n, n - 1, n], 2, 64, 3, 64)
+    rng = np.random.default_rng(n)
+    w, p = records(rng, 3, 2, n + 3, ties=what == "ties")
+    first, recent = (0, n // 2) if n > 2 else (0, 1)
+    if what == "all equal":
+        w[:] = 0.25
+    elif what == "the last one":
+        w[:, :, n - 1] = -1.0
+        first = recent = 0
+    elif what == "nan and infinities":
+        w[:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0], np.float32), w.shape)
+    elif what == "all safe":
+        p[:] = np.arange(n + 3)
+        first, recent = 0, n - 1
+        p[:, 1, 0] = n                                                  # (the second head: the one that is not safe is another)
+    elif what == "none safe":
+        first = recent = 0
+    evicted(rp, b, n - 1, first, recent, w, p, n + 3, what in ("random", "all equal"))
