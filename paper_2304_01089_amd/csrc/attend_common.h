@@ -51,6 +51,12 @@ __device__ __forceinline__ int wave_prefix(int v) {                      // incl
   return dpp_plus<0x143, 0xc>(v);
 }
 
+// A lane's 64 bits in every lane.  (readlane gives a signed number: its lower half must not fill the upper with its sign.)
+__device__ __forceinline__ uint64_t of_lane(uint32_t lo, uint32_t hi, int lane) {
+  const uint32_t l = __builtin_amdgcn_readlane(lo, lane), h = __builtin_amdgcn_readlane(hi, lane);
+  return static_cast<uint64_t>(h) << 32 | l;
+}
+
 // Four lanes' four bytes transposed: lane i's byte b becomes lane b's byte i.  (Two exchanges, of neighbours and of pairs.)
 struct QuadSel {
   uint32_t s0, s1;

@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(256, part_waves(BITS, NB, RT)) attend_part_ker
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int at = (k & 15) * 4 + r;
-      const uint64_t row = static_cast<uint64_t>(__builtin_amdgcn_readlane(rows_at.hi, at)) << 32 | __builtin_amdgcn_readlane(rows_at.lo, at);
+      const uint64_t row = of_lane(rows_at.lo, rows_at.hi, at);
       const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<uint8_t*>(pages) + row, 0, (NB - 1) * block_bytes + 16 * kRow, 0x00020000);
 #pragma unroll

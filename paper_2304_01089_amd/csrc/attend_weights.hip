@@ -211,8 +211,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
     const uint64_t at = ((static_cast<uint64_t>(max(id, 0)) * (a.g.d / kPageBlock) + unit * NB) * block_rows + t) * kRow;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const uint64_t row = static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(at >> 32), r)) << 32 |
-                           __builtin_amdgcn_readlane(static_cast<uint32_t>(at), r);
+      const uint64_t row = of_lane(static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32), r);
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.k_pages) + row, 0,
                                                                             (NB - 1) * block_bytes + 16 * kRow, 0x00020000);
 #pragma unroll
