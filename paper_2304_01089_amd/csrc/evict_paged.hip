@@ -24,6 +24,7 @@ namespace rptq {
 constexpr int kFirstBins = 4096, kLaterBins = 1024;              // of twelve and of ten bits of a key
 constexpr int kFewItems = 8;                   // of a lane whose keys stay in registers
 constexpr int kLdsItems = 32;                  // of a lane whose keys lie in LDS
+constexpr int kFewMovers = 16;                 // of an item, up to which a lane writes them down by itself
 constexpr int kHeldPages = 1024;               // page numbers of a sequence that are kept at hand
 constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them
 constexpr int kMoveChunks = 1024;              // workgroups of a head there at most
@@ -75,7 +76,7 @@ __device__ __forceinline__ void move_records(const EvictArgs& a, int64_t base, c
 }
 
 // Rows number first, first + step, ... of the lists: the thread's `which`-th of 2 units pieces.  page_of: a page's number.
-template <typename V, typename P, typename L>
+template <bool MANY, typename V, typename P, typename L>
 __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h, P&& page_of, L to, L from, int first, int end, int step,
                                             int which) {
   const int row_bytes = 16 * a.bits, head_bytes = a.hd * a.bits / 8;
@@ -84,11 +85,12 @@ __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h
   // heads over 128 wide: the row lies in several blocks; others share one
   const int64_t place = static_cast<int64_t>(h) * head_bytes + off;
   const int block = static_cast<int>(place / row_bytes), in_row = static_cast<int>(place - static_cast<int64_t>(block) * row_bytes);
-  uint8_t* pages = (values ? a.v_pages : a.k_pages) + in_row;
-  const int blocks = a.g.d / kPageBlock, shift = a.g.page_shift;
-  auto at = [&](int t) __attribute__((always_inline)) {
-    const int64_t row = ((static_cast<int64_t>(page_of(t >> shift)) * blocks + block) << shift) + (t & ((1 << shift) - 1));
-    return reinterpret_cast<V*>(pages + row * row_bytes);
+  const int shift = a.g.page_shift, block_bytes = row_bytes << shift;            // (below 2^20)
+  const uint64_t pages = reinterpret_cast<uint64_t>(values ? a.v_pages : a.k_pages) + static_cast<uint64_t>(block * block_bytes + in_row);
+  const uint32_t page_bytes = static_cast<uint32_t>(a.g.d / kPageBlock * block_bytes);
+  auto at = [&](int t) __attribute__((always_inline)) {        // (one wide product and one narrow one: addresses are what a row costs)
+    const uint64_t page = pages + static_cast<uint64_t>(static_cast<uint32_t>(page_of(t >> shift))) * page_bytes;
+    return reinterpret_cast<V*>(page + __umul24(t & ((1 << shift) - 1), row_bytes));
   };
   // (N at a time; the last row several times, if need be: the same bytes)
   auto some = [&](auto count, int i) __attribute__((always_inline)) {
@@ -105,17 +107,18 @@ __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h
     for (int k = 0; k < N; ++k) *y[k] = x[k];
   };
   int i = first;
-  for (; i + 4 * step < end; i += 8 * step) some(std::integral_constant<int, 8>{}, i);
+  if constexpr (MANY)
+    for (; i + 4 * step < end; i += 8 * step) some(std::integral_constant<int, 8>{}, i);
   for (; i < end; i += 4 * step) some(std::integral_constant<int, 4>{}, i);
 }
 
-template <int THREADS, typename P, typename L>
+template <int THREADS, bool MANY, typename P, typename L>
 __device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictPlan& p, int h, P&& page_of, L to, L from, int moves, int begin) {
   const int each = 2 * p.units, rows = THREADS / each, row = static_cast<int>(threadIdx.x) / each, which = static_cast<int>(threadIdx.x) - row * each;
   if (row >= rows) return;
-  if (p.vec == 16) move_pieces<Bytes16>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
-  else if (p.vec == 8) move_pieces<Bytes8>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
-  else move_pieces<uint32_t>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
+  if (p.vec == 16) move_pieces<MANY, Bytes16>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
+  else if (p.vec == 8) move_pieces<MANY, Bytes8>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
+  else move_pieces<MANY, uint32_t>(a, p.units, h, page_of, to, from, begin + row, moves, rows, which);
 }
 
 // A list of one token.
@@ -323,8 +326,8 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     const int hole = wave_largest_int(of_wave == ~wave_largest(~of_wave) ? sums[1][1][lane & (WAVES - 1)] : -1);
     if (hole < a.budget) {
       const One to{hole}, from{a.budget};
-      if (pages <= kHeldPages) move_rows<kThreads>(a, plan, h, [&](int page) { return ids[page]; }, to, from, 1, 0);
-      else move_rows<kThreads>(a, plan, h, [&](int page) { return pt[page]; }, to, from, 1, 0);
+      if (pages <= kHeldPages) move_rows<kThreads, false>(a, plan, h, [&](int page) { return ids[page]; }, to, from, 1, 0);
+      else move_rows<kThreads, false>(a, plan, h, [&](int page) { return pt[page]; }, to, from, 1, 0);
       if (tid == kThreads - 1) {
         const float weight = weights[a.budget];
         const int32_t position = positions[a.budget];
@@ -476,6 +479,14 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
       uint64_t come = (static_cast<uint64_t>(votes_hi) << 32 | votes_lo) & ~front;
       const int n_come = __builtin_popcountll(come);
       int r = movers + wave_prefix(n_come) - n_come;
+      // (an item with many - the newest are - is written down by all lanes)
+      for (uint64_t full = __ballot(n_come > kFewMovers); full != 0; full &= full - 1) {
+        const int item = __builtin_ctzll(full);
+        const uint64_t votes = of_lane(static_cast<uint32_t>(come), static_cast<uint32_t>(come >> 32), item);
+        const int place = __builtin_amdgcn_readlane(r, item) + rank_in(votes);
+        if (__builtin_amdgcn_inverse_ballot_w64(votes) && place < moves) from[place] = start + item * 64 + lane;
+        if (lane == item) come = 0;
+      }
       while (__ballot(come != 0) != 0) {
         if (come != 0) {
           if (r < moves) from[r] = t0 + __builtin_ctzll(come);
@@ -510,8 +521,8 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
     if (any > 0) write_lists(bins, bins + kFewMoves);
     __syncthreads();
     // (records by the last threads, rows by the first: few of both go side by side)
-    if (pages <= kHeldPages) move_rows<kThreads>(a, plan, h, [&](int page) { return ids[page]; }, bins, bins + kFewMoves, moves, 0);
-    else move_rows<kThreads>(a, plan, h, [&](int page) { return pt[page]; }, bins, bins + kFewMoves, moves, 0);
+    if (pages <= kHeldPages) move_rows<kThreads, true>(a, plan, h, [&](int page) { return ids[page]; }, bins, bins + kFewMoves, moves, 0);
+    else move_rows<kThreads, true>(a, plan, h, [&](int page) { return pt[page]; }, bins, bins + kFewMoves, moves, 0);
     move_records<kThreads>(a, base, bins, bins + kFewMoves, moves);
   } else {
     int32_t* to = workspace + list_start(static_cast<int64_t>(a.B) * a.n_kv) + static_cast<int64_t>(blockIdx.x) * 2 * plan.most;
@@ -531,7 +542,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a, EvictPlan 
   const int32_t* pt = a.page_table + b * a.ld_pt;
   const int moves = workspace[blockIdx.x], rows = 4 * (256 / (2 * plan.units));
   for (int begin = blockIdx.y * rows; begin < moves; begin += gridDim.y * rows)
-    move_rows<256>(a, plan, h, [&](int page) { return pt[page]; }, to, to + plan.most, min(begin + rows, moves), begin);
+    move_rows<256, false>(a, plan, h, [&](int page) { return pt[page]; }, to, to + plan.most, min(begin + rows, moves), begin);
 }
 
 static int64_t most_moves(int64_t capacity, int64_t budget) { return std::max<int64_t>(0, std::min(budget, capacity - budget)); }
