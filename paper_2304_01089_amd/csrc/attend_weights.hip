@@ -23,6 +23,8 @@ namespace rptq {
 constexpr int kTileTokens = 4 * kTile;         // of a workgroup's four waves
 constexpr int kSeenWorkgroups = 2048;          // as many parts as make this many workgroups, where there are tokens for them
 
+constexpr int64_t kStreamBytes = INT64_C(256) << 20;             // keys of larger caches, values included, are read past the last-level cache
+
 constexpr int kFewTiles = 4;                   // row tiles of which each wave of a workgroup makes one
 
 constexpr int kSide = 2;                       // row tiles that a wave works on side by side
@@ -57,14 +59,17 @@ struct QueryDigits {
   static constexpr int P = NB * kPageBlock, kHd = P / HEADS;
   const WeightArgs& a;
   const WeightPlan& plan;
-  int b, unit, len, group, g4, n16;
+  static constexpr int kRaw = kHd * 2 + 16;                // bytes of a query in its own order, and 16 (banks)
+  static constexpr int kScratch = kRowHeads * kRaw;        // of a wave
+  int b, unit, group, g4, n16;
   i4v kp[NB][8];                                           // the lane's positions' records
   struct Query {
-    int end;                                               // 0: no query
+    int back;                                              // newer queries of the sequence; -1: no query
     bool own;                                              // whether the lane's positions are its head's
     float lse;
-    uint16_t raw[NB][8];
+    i4v raw[NB];                                           // channels 8 n16 .. of every 128
   };
+  // (in the queries' own order: nothing of it waits for the positions' records)
   __device__ __forceinline__ Query request(int tile) const {
     // (pairs and tiles are below 2^31, a quotient's fraction is a multiple of its divisor's inverse or 0: 2^-50 of it does not reach the next number)
     auto quotient = [](int n, double per) { return static_cast<int>(n * per); };
@@ -79,15 +84,17 @@ struct QueryDigits {
     const uint16_t* q = a.q + q_row * a.ld_q + q_head * kHd;
     r.lse = a.lse[q_row * a.n_q + q_head];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r.raw[nb][e] = q[kp[nb][e][0] & (kHd - 1)];
-    r.end = there ? len - (a.queries - 1 - query) : 0;
+    for (int nb = 0; nb < NB; ++nb) r.raw[nb] = *reinterpret_cast<const i4v*>(q + nb * kPageBlock + (n16 & (kHd / 8 - 1)) * 8);
+    r.back = there ? a.queries - 1 - query : -1;
     r.own = there && (NB == 2 || n16 * 8 / kHd == head);
     return r;
   }
-  // to: the tile's 16 rows, `stride` bytes apart
-  __device__ __forceinline__ void make(const Query& now, unsigned char* to, int stride, TileRows* rows) const {
+  // scratch: kScratch bytes of LDS, `to` may be the same;  to: the tile's 16 rows, `stride` bytes apart
+  __device__ __forceinline__ void make(const Query& now, int len, unsigned char* scratch, unsigned char* to, int stride, TileRows* rows) const {
+    unsigned char* mine = scratch + g4 * kRaw;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) *reinterpret_cast<i4v*>(mine + nb * (2 * kPageBlock) + (n16 & (kHd / 8 - 1)) * 16) = now.raw[nb];
+    wave_lds_fence();
     // (in 64 bits up to the fixed point: an error of 2^-24 of q' would be one of score / 2^24 in a score's logarithm, and zero points far
     // from the codes make scores large)
     const double to_log2 = static_cast<double>(a.scale) * 1.4426950408889634074;
@@ -98,13 +105,14 @@ struct QueryDigits {
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double v = static_cast<double>(__uint_as_float(static_cast<uint32_t>(now.raw[nb][e]) << 16)) * static_cast<double>(__int_as_float(kp[nb][e][2])) * to_log2;
+        const double v = static_cast<double>(__uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(mine + (kp[nb][e][0] & (kHd - 1)) * 2)) << 16)) * static_cast<double>(__int_as_float(kp[nb][e][2])) * to_log2;
         x[nb][e] = now.own ? v : 0.0;
         const float size = fabsf(static_cast<float>(x[nb][e]));
         top = fmaxf(top, size);
         bad = bad || !(size < __builtin_huge_valf());
         zterm = fma(x[nb][e], static_cast<double>(kp[nb][e][3]), zterm);
       }
+    wave_lds_fence();                                      // (digits may take the queries' place)
     top = row16_max(top);
     zterm = row16_sum(zterm);
     const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;          // top < 2^ex
@@ -134,7 +142,7 @@ struct QueryDigits {
     const float lost = fabsf(high) < __builtin_huge_valf() ? static_cast<float>(off - static_cast<double>(high)) : 0.0f;
     if (n16 == 0) {
       rows->row[g4] = QueryRow{scale, scale * 65536.0f, high, __builtin_amdgcn_exp2f(-lost)};
-      rows->end[g4] = now.end;
+      rows->end[g4] = now.back < 0 ? 0 : len - now.back;
     }
   }
 };
@@ -153,22 +161,26 @@ template <int BITS, int NB, int HEADS>
 __global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightPlan plan) {
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int tile = static_cast<int>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = blockIdx.y, b = blockIdx.z;
+  using Maker = QueryDigits<BITS, NB, HEADS>;
+  __shared__ __align__(16) unsigned char scratch[4 * Maker::kScratch];
   if (tile >= plan.tiles) return;
-  const int len = tokens_of(a, a.lens[b]);
-  if (len == 0) return;
-  QueryDigits<BITS, NB, HEADS> maker{a, plan, b, unit, len, HEADS == 1 ? 4 : plan.group, g4, n16, {}};
+  Maker maker{a, plan, b, unit, HEADS == 1 ? 4 : plan.group, g4, n16, {}};
+  const auto query = maker.request(tile);
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       maker.kp[nb][e] = *reinterpret_cast<const i4v*>(a.k_pos + unit * maker.P + nb * kPageBlock + n16 * 8 + e);
+  const int len = tokens_of(a, a.lens[b]);
+  if (len == 0) return;
   unsigned char* to = static_cast<unsigned char*>(a.workspace) + ((static_cast<int64_t>(b) * gridDim.y + unit) * plan.tiles + tile) * made_bytes<NB>();
-  maker.make(maker.request(tile), to, maker.P, reinterpret_cast<TileRows*>(to + 16 * maker.P));
+  maker.make(query, len, scratch + (threadIdx.x >> 6) * Maker::kScratch, to, maker.P, reinterpret_cast<TileRows*>(to + 16 * maker.P));
 }
 
-// NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace
-template <int BITS, int NB, int HEADS, bool MADE>
-__global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
+// NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace; STREAM: keys are read past the
+// last-level cache
+template <int BITS, int NB, int HEADS, bool MADE, bool STREAM>
+__global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 32) ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
   constexpr int kDigitRow = P + 16;                        // (16 more: other banks)
@@ -179,7 +191,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = blockIdx.x, unit = blockIdx.y, b = blockIdx.z;
-  // (requested first, all at once: the length, the first two tiles' pages, the positions' records)
+  // (requested first, all at once: the length, the first two tiles' pages, the positions' records, the queries)
   const int length = a.lens[b];
   const int32_t* pt = a.page_table + b * a.ld_pt;
   auto token_of = [&](int k) { return (part + k * plan.parts) * kTileTokens + wave * kTile; };
@@ -187,11 +199,16 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
   const int page0 = page_at(0), page1 = page_at(1);
   i4v record;
   if (!MADE) record = reinterpret_cast<const i4v*>(a.k_pos + unit * P)[threadIdx.x & (P - 1)];
+  const int group = HEADS == 1 ? 4 : plan.group, group_shift = group >> 1;                 // (log2 of 1, 2, 4)
+  using Maker = QueryDigits<BITS, NB, HEADS>;
+  static_assert(Maker::kScratch <= 16 * kDigitRow, "a tile's queries take the place of its digits");
+  Maker maker{a, plan, b, unit, group, g4, n16, {}};
+  typename Maker::Query query;
+  if (!MADE && wave < plan.tiles) query = maker.request(wave);
   const int len = tokens_of(a, length);
   if (part * kTileTokens >= len) return;
 
   const int share = plan.share, pairs = share * a.queries;
-  const int group = HEADS == 1 ? 4 : plan.group, group_shift = group >> 1;                 // (log2 of 1, 2, 4)
   const int set_heads = kRowHeads / group;
   const bool full_rows = pairs % group == 0;               // (no row without a query)
 
@@ -203,6 +220,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
   auto page_of = [&](int k, int id) { return token_of(k) + (lane & 3) * 16 < len && id >= 0 && id < a.g.n_pages ? id : -1; };
   const uint32_t k_off = n16 * kRow + g4 * (4 * BITS);
   const int block_bytes = block_rows * kRow;
+  constexpr int kAux = STREAM ? 2 : 0;                     // (2: non-temporal)
   uint32_t kr[4][NB][BITS];
   auto load_keys = [&](int k, int id) __attribute__((always_inline)) {
     typedef unsigned u3v __attribute__((ext_vector_type(3)));
@@ -217,13 +235,13 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if constexpr (BITS == 3) {
-          const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rsrc, k_off, nb * block_bytes, 0);
+          const u3v v = __builtin_amdgcn_raw_buffer_load_b96(rsrc, k_off, nb * block_bytes, kAux);
 #pragma unroll
           for (int e = 0; e < 3; ++e) kr[r][nb][e] = v[e];
         } else {
 #pragma unroll
           for (int h = 0; h < BITS / 4; ++h) {
-            const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_off + 16 * h, nb * block_bytes, 0);
+            const u4v v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_off + 16 * h, nb * block_bytes, kAux);
 #pragma unroll
             for (int e = 0; e < 4; ++e) kr[r][nb][4 * h + e] = v[e];
           }
@@ -273,12 +291,12 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS == 32 ? 2 : 3) at
       *reinterpret_cast<i4v*>(table + (threadIdx.x & (P - 1)) * 16 + (threadIdx.x & (P - 1)) / 8 * 16) = record;
       __syncthreads();
       if (wave < tile1) {
-        QueryDigits<BITS, NB, HEADS> maker{a, plan, b, unit, len, group, g4, n16, {}};
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 8; ++e) maker.kp[nb][e] = *reinterpret_cast<const i4v*>(table + (nb * 16 + n16) * 144 + e * 16);
-        maker.make(maker.request(wave), q_dig + wave * 16 * kDigitRow, kDigitRow, rows + wave);
+        unsigned char* to = q_dig + wave * 16 * kDigitRow;
+        maker.make(query, len, to, to, kDigitRow, rows + wave);
       }
     }
     __syncthreads();
@@ -431,16 +449,19 @@ int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st)
   const int64_t runs = (most + kTileTokens - 1) / kTileTokens, each = static_cast<int64_t>(a.B) * units;
   p.parts = static_cast<int32_t>(std::min<int64_t>(runs, std::max<int64_t>(1, (kSeenWorkgroups + each - 1) / each)));
   const dim3 grid(p.parts, units, a.B), makers((p.tiles + 3) / 4, units, a.B);
-  auto go = [&](auto digits, auto made, auto alone) {
+  const int64_t pages = std::min<int64_t>(a.g.n_pages, static_cast<int64_t>(a.B) * a.pages_per_seq);
+  const bool stream = pages * 2 * (static_cast<int64_t>(a.g.d) * bits / 8 << a.g.page_shift) > kStreamBytes;
+  auto go = [&](auto digits, auto made, auto alone, auto streamed) {
     if (p.tiles > kFewTiles) {
       hipLaunchKernelGGL(digits, makers, dim3(256), 0, st, a, p);
       hipLaunchKernelGGL(made, grid, dim3(256), 0, st, a, p);
     } else {
-      hipLaunchKernelGGL(alone, grid, dim3(256), 0, st, a, p);
+      hipLaunchKernelGGL(stream ? streamed : alone, grid, dim3(256), 0, st, a, p);
     }
   };
 #define RPTQ_GO(BITS, NB, HEADS) \
-  go(query_digits_kernel<BITS, NB, HEADS>, attend_weights_kernel<BITS, NB, HEADS, true>, attend_weights_kernel<BITS, NB, HEADS, false>)
+  go(query_digits_kernel<BITS, NB, HEADS>, attend_weights_kernel<BITS, NB, HEADS, true, false>, attend_weights_kernel<BITS, NB, HEADS, false, false>, \
+     attend_weights_kernel<BITS, NB, HEADS, false, BITS < 8>)
 #define RPTQ_BY_BITS(NB, HEADS)                 \
   do {                                          \
     if (bits == 3) RPTQ_GO(3, NB, HEADS);       \
