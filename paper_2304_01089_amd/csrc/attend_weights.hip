@@ -3,12 +3,22 @@
 // a as in the attention itself (q' = scale log2(e) q s, minus the keys' zero points), lse the logarithm of the sum that it left.
 // The keys' codes are read once more, and no value.
 //
-// Scores come from the int8 matrix cores as there: a query head of a query is four rows of digits, four of them a row tile, 64
-// tokens a wave's tile.  A row tile's four belong to one key/value head where it has three pairs (query, head) or more; two pairs
+// Scores come from the int8 matrix cores as there: a query head of a query is four rows of digits to the base 256, four of them a row
+// tile, 64 tokens a wave's tile, 256 a workgroup's.  q' and the zero points' term are formed in 64 bits up to the fixed point of
+// 30 bits below the head's largest |q'|; sums of digits are exact; a weight is rounded as its upper digits' sum becomes fp32 and
+// meets lse, as the lower ones' comes to it, by 2^x and by the sum over pairs (6e-8 to 6e-7 of the weights in all).
+// A row tile's four belong to one key/value head where it has three pairs (query, head) or more; two pairs
 // share a tile with another head's two, single ones with three other heads' (heads under 128 wide).  A lane adds up its tokens'
 // weights over the row tiles in fp32 in their order, the four rows' sums come together by two exchanges, and each weight is read and
 // written by one lane: no order of adding depends on anything but the call.
-// What bounds it: memory with few queries; with many, the vector instructions that make weights of digits' sums.
+//
+// Up to kFewTiles row tiles each wave makes one tile's digits itself: queries are requested with the first loads, in their own order,
+// and gathered in LDS (gathered from memory, behind the positions' records: 1 x 257 tokens 5.23 us, now 4.96).  More are made once by a
+// launch of their own, into the workspace, instead of by each of a sequence's workgroups (5 x 8191 tokens, 32 queries: 29.6 -> 23.7 us).
+// What bounds it: with few queries memory, and the start of every workgroup (length, page number, codes, one after the other, while
+// its digits are made): 32 sequences of up to 4096 tokens, 40 heads of 128 at 4 bits take 43.8 us for 195 MB, 4.5 TB/s; one short
+// sequence 5, of which a launch is 1.8.  With many queries the vector instructions that make a weight of four sums of digits, about
+// seven and an exponential, beside two matrix instructions for sixteen tokens of four pairs: 23.6 us for 3.4 GFLOP, digits 4 of them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -21,15 +31,18 @@
 namespace rptq {
 
 constexpr int kTileTokens = 4 * kTile;         // of a workgroup's four waves
-constexpr int kSeenWorkgroups = 2048;          // as many parts as make this many workgroups, where there are tokens for them
+// As many parts as make this many workgroups, where there are tokens for them (1024 | 2048 | 4096: 32 x 4096 of 40 heads 51.9 | 47.9 | 50.0 us,
+// 5 x 8191 of 32 on 8 with 32 queries 28.6 | 26.4 | 26.2).
+constexpr int kSeenWorkgroups = 2048;
 
-constexpr int64_t kStreamBytes = INT64_C(256) << 20;             // keys of larger caches, values included, are read past the last-level cache
-
+// Keys of larger caches, values included, are read past the last-level cache, at 3 and 4 bits (an ordinary | such a load: 32 x 4096 of 40
+// heads 46.1 | 43.8 us, 16 x 8192 at 3 bits 66.3 | 63.0; smaller caches, 5 x 8191, 23.4 | 24.0).
+constexpr int64_t kStreamBytes = INT64_C(256) << 20;
 constexpr int kFewTiles = 4;                   // row tiles of which each wave of a workgroup makes one
+constexpr int kSide = 2;                       // row tiles that a wave works on side by side (1 | 2 | 4: 5 x 8191, 32 queries, 27.7 | 26.4 | 29.4 us)
 
-constexpr int kSide = 2;                       // row tiles that a wave works on side by side
-
-// Row tiles whose digits lie in LDS at one time; more go through the tokens several times.
+// Row tiles whose digits lie in LDS at one time; more go through the tokens several times (16 | 32, and two workgroups per compute
+// unit instead of three: 5 x 8191, 32 queries, 23.7 | 29.2 us).
 __host__ __device__ constexpr int held_tiles(int blocks) { return blocks == 2 ? 8 : 16; }
 
 struct WeightPlan {
@@ -178,7 +191,9 @@ __global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightP
 }
 
 // NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace; STREAM: keys are read past the
-// last-level cache
+// last-level cache.  Three waves per SIMD where their registers suffice, nearly (four instead: spills, or 23.4 -> 29.5 us); digits made, several
+// heads: two (16 x 2048 of 32 heads of 32, 8 queries, 30.2 -> 24.6 us; 8 x 4096 of 12 of 64, 16 queries, 8 bits 20.1 -> 18.6), made here: three (20.0,
+// two 21.4).
 template <int BITS, int NB, int HEADS, bool MADE, bool STREAM>
 __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 32) ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block

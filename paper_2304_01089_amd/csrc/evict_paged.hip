@@ -5,11 +5,16 @@
 // the order of the tokens; a token's position is in its record.)
 //
 // One workgroup per (sequence, head) finds the threshold: a token's key is its weight's bits in an order of whole numbers, and the
-// budget-th largest key is found two bits at a time, every wave counting its tokens' keys that reach the three candidates by votes;
-// a count that hits the budget ends it.  A wave has a run of consecutive tokens, so the order among equal keys and the
-// places in the lists of holes and movers are counts of votes, too.  Keys stay in registers up to 32 per lane.
+// budget-th largest key is found from the top, twelve bits, ten and ten: the workgroup counts its keys in bins in LDS, sums them in 64
+// groups, and every wave finds by itself the group and in it the bin where the sum from the top reaches the budget.  A bin of up to 64
+// keys ends the search: they are compared with each other.  Where only one token leaves - a step of a batch at its budget - the
+// smallest key is found by maxima over lanes and waves and no threshold (32 x 2049 tokens of 8 heads 9.6 -> 5.4 us).  A wave has a run
+// of consecutive tokens, so the order among equal keys and the places in the lists of holes and movers are counts of votes.
 // Few moves are done by the same workgroup, many by a second launch over the whole chip.
-// What bounds it: a chain of short steps, some of them across the workgroup's waves; long prompts: memory.
+// What bounds it: a chain of short steps, each of one to three thousand cycles and most of them across the workgroup's waves: 7
+// sequences of 1531 tokens, 2 heads of 256, budget 700 take 10.3 us (moves 6300 of 18500 cycles, keys and bins 2400, the search
+// 3400).  Long sequences: one compute unit's LDS and instructions per head: 4 of 32768 tokens, 8 heads, budget 4096 take 36.5 us, 28 in
+// the first kernel (of 47000 cycles 11000 are keys and bins, 7000 the later looks, 19000 votes and lists), 7.8 in the moves.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,11 +27,13 @@
 namespace rptq {
 
 constexpr int kFirstBins = 4096, kLaterBins = 1024;              // of twelve and of ten bits of a key
-constexpr int kFewItems = 8;                   // of a lane whose keys stay in registers
-constexpr int kLdsItems = 32;                  // of a lane whose keys lie in LDS
-constexpr int kFewMovers = 16;                 // of an item, up to which a lane writes them down by itself
+// Keys stay in registers up to eight of a lane, with eight waves up to 4096 tokens (four | eight up to 2048: 7 x 1531 11.2 | 10.3 us) and
+// sixteen up to 8192; they lie in LDS up to 32 of a lane (32768 tokens); longer sequences' are made anew from their records.
+constexpr int kFewItems = 8;
+constexpr int kLdsItems = 32;
+constexpr int kFewMovers = 16;                 // of an item, up to which a lane writes them down by itself (always: 4 x 32768 38.9 us; up to 8, 16 or 32: 36.7)
 constexpr int kHeldPages = 1024;               // page numbers of a sequence that are kept at hand
-constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them
+constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them (512 | 2048: 16 x 4000 to 2000, 8 heads, 18.7 | 16.7 us)
 constexpr int kMoveChunks = 1024;              // workgroups of a head there at most
 constexpr uint32_t kSafe = 0xffffffffu, kNanKey = 0xfffffffeu;
 
@@ -75,7 +82,8 @@ __device__ __forceinline__ void move_records(const EvictArgs& a, int64_t base, c
   }
 }
 
-// Rows number first, first + step, ... of the lists: the thread's `which`-th of 2 units pieces.  page_of: a page's number.
+// Rows number first, first + step, ... of the lists: the thread's `which`-th of 2 units pieces.  page_of: a page's number.  MANY: eight rows
+// at a time (eight | sixteen: 7 x 1531 10.3 | 12.0 us, whose last rows are moved several times).
 template <bool MANY, typename V, typename P, typename L>
 __device__ __forceinline__ void move_pieces(const EvictArgs& a, int units, int h, P&& page_of, L to, L from, int first, int end, int step,
                                             int which) {
@@ -158,7 +166,7 @@ enum class Keys { registers, lds, made };      // where a token's key is when it
 // WAVES: of the workgroup
 template <int WAVES, Keys KEYS>
 __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, EvictPlan plan) {
-  constexpr int kRun = KEYS == Keys::registers ? kFewItems : 16;             // of its items a lane works on so many together
+  constexpr int kRun = KEYS == Keys::registers ? kFewItems : 16;             // of its items a lane works on so many together (8 | 16 | 32: 4 x 32768 40.1 | 38.7 | 40.6 us)
   constexpr int kThreads = WAVES * 64, kKeys = KEYS == Keys::lds ? kThreads * kLdsItems : 1;
   constexpr int kAllBins = kFirstBins + 2 * kLaterBins;
   __shared__ __align__(16) int32_t bins[kAllBins];             // (later the lists of a few moves)

@@ -4,7 +4,10 @@
 // Keys and values go as there: a wave has 1024 channels of a row, moves them to cluster order through a piece of LDS of its own,
 // and has the constants of its 16 positions in registers.  A lane loads two pieces of eight channels that rotate together (half
 // style: eight and their partners; interleaved: sixteen side by side), takes the eight cosines and sines from LDS, where the
-// wave has put the row's, one pair per lane, and writes fp32.  What bounds it: memory, as without the rotation.
+// wave has put the row's, one pair per lane and once for the wave's heads, and writes fp32.
+// What bounds it: memory, as without the rotation: 8192 tokens of 40 heads of 128, queries included, take 82 us for 378 MB at 4 bits,
+// 4.6 TB/s.  One token: 3.9 us, a launch and a chain of dependent loads (slot and table, rows, positions); the host takes 4.5.
+// (76 registers; held to four workgroups per compute unit it spills: 163 us.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

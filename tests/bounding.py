@@ -44,7 +44,7 @@ def rope32(x, positions, hd, rot, interleaved, freqs, amplitude=1.0):
 def weights64(q, lse, k_codes, at, n, hc, n_q, scale, queries, tensor=0):
     """What the tokens at indices `at` (k_codes: their rows) of a sequence of n got of `queries` queries: (sums [H, len(at)], bound).
 
-    In units of log2 a score's error is at most 8 U (S1 + SZ): q' has four roundings, which count once for the codes' sum
+    In units of log2 a score's error is at most 8 U (S1 + SZ), with every step in fp32: q' has four roundings, which count once for the codes' sum
     (S1 = sum |q'_j c_j|) and once for the zero points' (SZ = sum |q'_j z_j|), its fixed point half a unit 30 bits below the largest, the digits'
     sums two half steps, the difference from lse one; lse in these units one of its own, one as it joins the zero points' term
     and one in the difference.  2^x adds a step, the sum over p pairs (p / 4 + 6) half steps."""
