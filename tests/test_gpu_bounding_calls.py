@@ -1,5 +1,10 @@
 """Calls of the cache-bounding operators that their documentation allows and a program may come to: recorded graphs that share their
-workspaces, records half in place, rows and tables inside larger tensors, one token, token numbers at the limit."""
+workspaces, a process's first call, recorded, records half in place, rows and tables inside larger tensors, one token, token numbers at the
+limit."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -10,6 +15,50 @@ from test_gpu_paged import Batch, dev, dev_bf16
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 TOP = 1 << 29
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PROGRAM = r"""
+import sys
+sys.path.insert(0, "tests")
+import numpy as np, torch
+import paper_2304_01089_amd as rp
+from test_gpu_bounding import records
+from test_gpu_paged import Batch, dev, dev_bf16
+n, budget, queries = (int(a) for a in sys.argv[1:])
+b = Batch(rp, [n, 30], 2, 64, 4, 16)
+w, p = records(np.random.default_rng(0), 2, 2, n)
+q = dev_bf16(b.queries(4)).repeat_interleave(queries, 0)
+lse = torch.full((2 * queries, 4), 3.0, device="cuda")
+start = [b.cache.k_pages.clone(), b.cache.v_pages.clone(), dev(w), dev(p)]
+track, lens = rp.CacheTrack(dev(w), dev(p)), torch.zeros(2, dtype=torch.int32, device="cuda")
+work = rp.attend_weights_paged_workspace(b.cache, 2, 4, queries), rp.evict_paged_workspace(b.cache, 2, n, budget)
+
+def go():
+    rp.attend_weights_paged(b.cache, q, b.page_table, b.dev_lens, lse, track, queries=queries, workspace=work[0])
+    rp.evict_paged(b.cache, b.page_table, b.dev_lens, track, budget, recent=9, lens_out=lens, workspace=work[1])
+
+state = [b.cache.k_pages, b.cache.v_pages, track.weights, track.positions]
+def restore():
+    for t, s in zip(state, start):
+        t.copy_(s)
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    go()
+outs = []
+for _ in range(3):
+    restore()
+    graph.replay()
+    torch.cuda.synchronize()
+    outs.append([t.clone() for t in state + [lens]])
+restore()
+go()
+torch.cuda.synchronize()
+for o in outs:
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(o, state + [lens]))
+print("ok")
+"""
 
 
 @pytest.fixture(scope="module")
@@ -72,6 +121,12 @@ def test_graphs_that_share_their_workspaces(rp):
         torch.cuda.synchronize()
         for side, w in zip(sides, want):
             assert all(torch.equal(a, b) for a, b in zip(state(side), w)), turn
+
+
+@pytest.mark.parametrize("n,budget,queries", [(300, 100, 1), (6000, 5999, 3), (9000, 4200, 12), (33000, 700, 1)])
+def test_recording_the_first_calls_of_a_process(n, budget, queries):
+    r = subprocess.run([sys.executable, "-u", "-c", PROGRAM, str(n), str(budget), str(queries)], cwd=ROOT, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stdout + r.stderr
 
 
 @pytest.mark.parametrize("n,budget", [(300, 100), (9000, 4200)])
