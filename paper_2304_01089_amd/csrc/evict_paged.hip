@@ -480,35 +480,32 @@ __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, E
   const int moves = min(min(__builtin_amdgcn_readlane(s.all, 0), __builtin_amdgcn_readlane(s.all, 16)), plan.most);
   auto write_lists = [&](int32_t* to, int32_t* from) __attribute__((always_inline)) {
     if constexpr (KEYS == Keys::lds) {
-      // Lane i has item i's votes and writes its movers down one after the other (there are few of an item as a rule).
+      // Lane i has item i's votes and writes its tokens down one after the other; an item with many - holes, the newest - is written down by
+      // all lanes.
       static_assert(kLdsItems <= 64, "a lane has one item");
-      const int t0 = start + lane * 64, in_front = a.budget - t0;
-      const uint64_t front = in_front >= 64 ? ~0ull : (in_front > 0 ? (1ull << in_front) - 1 : 0ull);
-      uint64_t come = (static_cast<uint64_t>(votes_hi) << 32 | votes_lo) & ~front;
-      const int n_come = __builtin_popcountll(come);
-      int r = movers + wave_prefix(n_come) - n_come;
-      // (an item with many - the newest are - is written down by all lanes)
-      for (uint64_t full = __ballot(n_come > kFewMovers); full != 0; full &= full - 1) {
-        const int item = __builtin_ctzll(full);
-        const uint64_t votes = of_lane(static_cast<uint32_t>(come), static_cast<uint32_t>(come >> 32), item);
-        const int place = __builtin_amdgcn_readlane(r, item) + rank_in(votes);
-        if (__builtin_amdgcn_inverse_ballot_w64(votes) && place < moves) from[place] = start + item * 64 + lane;
-        if (lane == item) come = 0;
-      }
-      while (__ballot(come != 0) != 0) {
-        if (come != 0) {
-          if (r < moves) from[r] = t0 + __builtin_ctzll(come);
-          ++r;
-          come &= come - 1;
+      auto write_down = [&](uint64_t who, int before, int32_t* list) __attribute__((always_inline)) {
+        const int many = __builtin_popcountll(who);
+        int r = before + wave_prefix(many) - many;
+        for (uint64_t full = __ballot(many > kFewMovers); full != 0; full &= full - 1) {
+          const int item = __builtin_ctzll(full);
+          const uint64_t votes = of_lane(static_cast<uint32_t>(who), static_cast<uint32_t>(who >> 32), item);
+          const int place = __builtin_amdgcn_readlane(r, item) + rank_in(votes);
+          if (__builtin_amdgcn_inverse_ballot_w64(votes) && place < moves) list[place] = start + item * 64 + lane;
+          if (lane == item) who = 0;
         }
-      }
-      if (start < a.budget)
-        each_item([&](int first, uint64_t before, uint64_t kept) __attribute__((always_inline)) {
-          const uint64_t go = before & ~kept;
-          const int at = holes + rank_in(go);
-          if (__builtin_amdgcn_inverse_ballot_w64(go) && at < moves) to[at] = first + lane;
-          holes += __builtin_popcountll(go);
-        });
+        while (__ballot(who != 0) != 0) {
+          if (who != 0) {
+            if (r < moves) list[r] = start + lane * 64 + __builtin_ctzll(who);
+            ++r;
+            who &= who - 1;
+          }
+        }
+      };
+      const int in_front = a.budget - (start + lane * 64);
+      const uint64_t front = in_front >= 64 ? ~0ull : (in_front > 0 ? (1ull << in_front) - 1 : 0ull);
+      const uint64_t kept = static_cast<uint64_t>(votes_hi) << 32 | votes_lo;
+      write_down(kept & ~front, movers, from);
+      if (start < a.budget) write_down(lane < items ? front & ~kept : 0ull, holes, to);
       return;
     }
     each_item([&](int t0, uint64_t front, uint64_t kept) __attribute__((always_inline)) {
