@@ -31,8 +31,8 @@
 namespace rptq {
 
 constexpr int kTileTokens = 4 * kTile;         // of a workgroup's four waves
-// As many parts as make this many workgroups, where there are tokens for them (1024 | 2048 | 4096: 32 x 4096 of 40 heads 51.9 | 47.9 | 50.0 us,
-// 5 x 8191 of 32 on 8 with 32 queries 28.6 | 26.4 | 26.2).
+// As many parts as make this many workgroups, where there are tokens for them (1024 | 2048 | 5000: 32 x 4096 of 40 heads 47.5 | 43.8 | 45.0 us,
+// 16 x 8192 of 40 at 3 bits 72.1 | 63.1 | 63.8, 5 x 8191 of 32 on 8 with 32 queries 26.1 | 23.3 | 23.3, 16 x 4096 of 32 heads of 32 17.4 | 19.8 | 19.8).
 constexpr int kSeenWorkgroups = 2048;
 
 // Keys of larger caches, values included, are read past the last-level cache, at 3 and 4 bits (an ordinary | such a load: 32 x 4096 of 40
