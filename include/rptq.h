@@ -509,6 +509,7 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
  *
  * Both are asynchronous on `stream` and allocate nothing; rptq_rope needs no call before it is recorded into a graph,
  * rptq_rope_quant_paged the first one on the device.
+ * T <= 2^40; 2^23 workgroups are a launch (of one narrow head 2^25 rows), more rows take several.
  */
 #define RPTQ_MAX_ROTARY_HEAD 1024
 enum { RPTQ_ROPE_PLAIN = 0, RPTQ_ROPE_LINEAR = 1, RPTQ_ROPE_BASE = 2, RPTQ_ROPE_PARTS = 3 };

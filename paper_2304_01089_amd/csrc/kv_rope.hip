@@ -164,25 +164,29 @@ int32_t launch_rope_quant_paged(const RopeArgs* q, const RopeArgs& k, const Page
                                 const PagedGeom& g, int32_t bits, hipStream_t st) {
   if (k.T == 0) return RPTQ_OK;
   RopeQuantLaunch l;
-  unsigned grid = 0;
-  if (int32_t s = paged_launch(kt, vt, slots, k.T, g, st, &l.kv, &grid)) return s;
   l.q.groups = 0;
-  if (q != nullptr) {
-    const bool same = q->x == q->y && q->ld_x == q->ld_y;
-    if (int32_t s = plan_rope(*q, 8, same, &l.q)) return s;
-  }
-  if (static_cast<int64_t>(l.q.groups) + grid > INT32_MAX) return RPTQ_ERR_SHAPE;
-  l.positions = k.positions;
-  l.freqs = k.freqs;
   l.amplitude = k.amplitude;
+  l.freqs = k.freqs;
   l.rot = k.rot;
   l.hd_shift = __builtin_ctz(static_cast<unsigned>(k.hd));
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(l.q.groups + grid), dim3(256), 0, st, l); };
-  const bool half = k.interleaved == 0;
-  if (bits == 3) half ? go(rope_quant_paged_kernel<3, true>) : go(rope_quant_paged_kernel<3, false>);
-  else if (bits == 4) half ? go(rope_quant_paged_kernel<4, true>) : go(rope_quant_paged_kernel<4, false>);
-  else half ? go(rope_quant_paged_kernel<8, true>) : go(rope_quant_paged_kernel<8, false>);
-  RPTQ_HIP(hipGetLastError());
+  int64_t most = k.T;                                // (rows of a launch: keys and values need no more workgroups for more rows)
+  if (q != nullptr) most = std::min(most, plan_rope(*q, 8, q->x == q->y && q->ld_x == q->ld_y, &l.q));
+  for (int64_t first = 0; first < k.T; first += most) {
+    const int64_t rows = std::min(most, k.T - first);
+    PagedTensor kp = kt, vp = vt;
+    kp.x += first * kt.ld;
+    vp.x += first * vt.ld;
+    unsigned grid = 0;
+    if (int32_t s = paged_launch(kp, vp, slots + first, rows, g, st, &l.kv, &grid)) return s;
+    if (q != nullptr) rope_part(*q, first, rows, &l.q);
+    l.positions = k.positions + first;
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(l.q.groups + grid), dim3(256), 0, st, l); };
+    const bool half = k.interleaved == 0;
+    if (bits == 3) half ? go(rope_quant_paged_kernel<3, true>) : go(rope_quant_paged_kernel<3, false>);
+    else if (bits == 4) half ? go(rope_quant_paged_kernel<4, true>) : go(rope_quant_paged_kernel<4, false>);
+    else half ? go(rope_quant_paged_kernel<8, true>) : go(rope_quant_paged_kernel<8, false>);
+    RPTQ_HIP(hipGetLastError());
+  }
   return RPTQ_OK;
 }
 

@@ -2,6 +2,8 @@
 #pragma once
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace rptq {
 
 // Columns of 64 x 256 tiles at a product's end that go out as 64 x 128 tiles, two for one, in the launch of the others; 0: none.
@@ -83,6 +85,36 @@ inline int ln_rows_per_workgroup(int64_t M, int waves, int units, int cus, int b
   if (ln && bits > 3 && waves == 2 && (per == 11 || per == 12)) return 1;      // (a sixth workgroup of two rows costs a round)
   const Lines& at = (ln ? (bits > 3 ? kNorm : kNorm3) : (bits > 3 ? kPlain : kPlain3))[waves - 2];
   return per <= at.one ? 1 : (per <= at.two ? 2 : 4);
+}
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopePairs = 1024;               // cosines of a workgroup at most
+constexpr int kRopeRows = 4;                   // rows of a workgroup at most
+constexpr int kRopeWorkgroups = 1024;          // as many at least, where there is work for them
+constexpr int kRopeMost = 1 << 16;             // pieces of a workgroup, so that a division is one product
+constexpr int kRopeLaunch = 1 << 23;           // workgroups of a launch at most: it counts its threads in 32 bits
+
+// How rows are shared out that turn by their positions (rope.hip).
+struct RopeShares {
+  int32_t rows, heads;                         // of a workgroup
+  int32_t head_groups;                         // workgroups per `rows` rows
+  int64_t launch_rows;                         // rows of a launch at most (a multiple of `rows`)
+};
+
+// Rows of a workgroup: as few as make its cosines worth their time, as many as leave enough workgroups; heads are shared out
+// where there are few rows.  half: pairs of a head; units: pieces of a head.
+inline RopeShares rope_shares(int64_t T, int32_t n_heads, int32_t half, int32_t units) {
+  RopeShares s;
+  const int64_t row = static_cast<int64_t>(n_heads) * units;                            // pieces
+  const int64_t most_rows = std::max<int64_t>(1, std::min<int64_t>({kRopePairs / half, kRopeRows, kRopeMost / row}));
+  s.rows = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most_rows, T / kRopeWorkgroups)));
+  const int64_t row_groups = (T + s.rows - 1) / s.rows;
+  const int64_t want = std::max<int64_t>(1, kRopeWorkgroups / row_groups), fill = (row + kRopeThreads - 1) / kRopeThreads;
+  const int64_t groups = std::max<int64_t>(std::min(want, fill), (row + kRopeMost - 1) / kRopeMost);
+  s.heads = static_cast<int32_t>((n_heads + groups - 1) / groups);
+  s.head_groups = (n_heads + s.heads - 1) / s.heads;
+  s.launch_rows = static_cast<int64_t>(kRopeLaunch / s.head_groups) * s.rows;
+  return s;
 }
 
 }  // namespace rptq

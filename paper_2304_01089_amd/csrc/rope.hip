@@ -33,24 +33,25 @@ static void launch_types(const RopeLaunch& l, hipStream_t st) {
   else yf ? go(rope_kernel<W, HALF, __bf16, float>) : go(rope_kernel<W, HALF, __bf16, __bf16>);
 }
 
-// Rows of a workgroup: as few as make its cosines worth their time, as many as leave enough workgroups; heads are shared out
-// where there are few rows.  W: channels of a piece.
-int32_t plan_rope(const RopeArgs& a, int W, bool same, RopeLaunch* l) {
+int64_t plan_rope(const RopeArgs& a, int W, bool same, RopeLaunch* l) {
   const int half = a.rot / 2;
-  l->a = a;
   l->turned = a.interleaved && W > 1 ? a.rot / W : half / W;
   l->units = l->turned + (same ? 0 : (a.hd - a.rot) / W);
-  const int64_t row = static_cast<int64_t>(a.n_heads) * l->units;                       // pieces
-  const int64_t most_rows = std::max<int64_t>(1, std::min<int64_t>({kRopePairs / half, kRopeRows, kRopeMost / row}));
-  l->rows = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most_rows, a.T / kRopeWorkgroups)));
-  const int64_t row_groups = (a.T + l->rows - 1) / l->rows;
-  const int64_t want = std::max<int64_t>(1, kRopeWorkgroups / row_groups), fill = (row + kRopeThreads - 1) / kRopeThreads;
-  const int64_t groups = std::max<int64_t>(std::min(want, fill), (row + kRopeMost - 1) / kRopeMost);
-  l->heads = static_cast<int32_t>((a.n_heads + groups - 1) / groups);
-  l->head_groups = (a.n_heads + l->heads - 1) / l->heads;
-  if (row_groups * l->head_groups > INT32_MAX) return RPTQ_ERR_SHAPE;
-  l->groups = static_cast<int32_t>(row_groups * l->head_groups);
-  return RPTQ_OK;
+  const RopeShares s = rope_shares(a.T, a.n_heads, half, l->units);
+  l->rows = s.rows;
+  l->heads = s.heads;
+  l->head_groups = s.head_groups;
+  return s.launch_rows;
+}
+
+void rope_part(const RopeArgs& a, int64_t first, int64_t rows, RopeLaunch* l) {
+  const int x_size = a.x_dtype == RPTQ_DTYPE_F32 ? 4 : 2, y_size = a.y_dtype == RPTQ_DTYPE_F32 ? 4 : 2;
+  l->a = a;
+  l->a.x = static_cast<const uint8_t*>(a.x) + first * a.ld_x * x_size;
+  l->a.y = static_cast<uint8_t*>(a.y) + first * a.ld_y * y_size;
+  l->a.positions = a.positions + first;
+  l->a.T = rows;
+  l->groups = static_cast<int32_t>((rows + l->rows - 1) / l->rows * l->head_groups);
 }
 
 int32_t launch_rope(const RopeArgs& a, hipStream_t st) {
@@ -65,12 +66,15 @@ int32_t launch_rope(const RopeArgs& a, hipStream_t st) {
   int W = 8;
   while (W > 1 && !fits(W)) W /= 2;
   RopeLaunch l;
-  if (int32_t s = plan_rope(a, W, same, &l)) return s;
-  if (W == 8) halves ? launch_types<8, true>(l, st) : launch_types<8, false>(l, st);
-  else if (W == 4) halves ? launch_types<4, true>(l, st) : launch_types<4, false>(l, st);
-  else if (W == 2) halves ? launch_types<2, true>(l, st) : launch_types<2, false>(l, st);
-  else halves ? launch_types<1, true>(l, st) : launch_types<1, false>(l, st);
-  RPTQ_HIP(hipGetLastError());
+  const int64_t most = plan_rope(a, W, same, &l);
+  for (int64_t first = 0; first < a.T; first += most) {
+    rope_part(a, first, std::min(most, a.T - first), &l);
+    if (W == 8) halves ? launch_types<8, true>(l, st) : launch_types<8, false>(l, st);
+    else if (W == 4) halves ? launch_types<4, true>(l, st) : launch_types<4, false>(l, st);
+    else if (W == 2) halves ? launch_types<2, true>(l, st) : launch_types<2, false>(l, st);
+    else halves ? launch_types<1, true>(l, st) : launch_types<1, false>(l, st);
+    RPTQ_HIP(hipGetLastError());
+  }
   return RPTQ_OK;
 }
 

@@ -3,23 +3,21 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "launch_rules.h"
 #include "rptq_internal.h"
 
 namespace rptq {
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopePairs = 1024;               // cosines of a workgroup at most
-constexpr int kRopeRows = 4;                   // rows of a workgroup at most
-constexpr int kRopeWorkgroups = 1024;          // as many at least, where there is work for them
-constexpr int kRopeMost = 1 << 16;             // pieces of a workgroup, so that a division is one product
-
 struct RopeLaunch {
   RopeArgs a;
   int32_t rows, heads;                         // of a workgroup
-  int32_t head_groups, groups;                 // workgroups per row, and all
+  int32_t head_groups, groups;                 // workgroups per `rows` rows, and of this launch
   int32_t turned, units;                       // pieces of a head's rotated channels, and all that are moved
 };
-int32_t plan_rope(const RopeArgs& a, int W, bool same, RopeLaunch* l);         // (rope.hip)
+// The launch of all rows but for their number; how many rows one launch takes.  W: channels of a piece.
+int64_t plan_rope(const RopeArgs& a, int W, bool same, RopeLaunch* l);         // (rope.hip)
+// Rows first .. first + rows - 1 of `a` into *l.
+void rope_part(const RopeArgs& a, int64_t first, int64_t rows, RopeLaunch* l);
 
 // (cos, sin) of an angle, times `amplitude`, rounded once to fp32.  In 64 bits: at position 10^6 the angle of the fastest pair has
 // 20 bits in front of the point, of which fp32 would leave four behind it.  k = round(2 theta / pi); theta - k pi / 2 by two fused

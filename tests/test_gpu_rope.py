@@ -288,3 +288,43 @@ def test_refusals(rp):
     none = x[:0]
     assert rp.rope(r, none, pos[:0], 64).shape == (0, 128)
     assert rp.rope_quant_paged(cache, r, none, none, none, pos[:0], slots[:0]).shape == (0, 128) and not cache.k_pages.any()
+
+
+def test_more_rows_than_a_launch_has_room_for(rp):
+    """2^26 rows at four a workgroup would be 2^32 threads: they go in parts."""
+    T = (1 << 26) + 5
+    if torch.cuda.mem_get_info()[0] < 4 << 30:
+        pytest.skip("not enough free memory")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randint(-100, 100, (T, 2), generator=gen, device="cuda", dtype=torch.int8).to(BF16)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    r = handle(rp, 2, False)
+    y = rp.rope(r, x, pos, 2)
+    for i in range(0, T, 1 << 24):
+        assert torch.equal(y[i:i + (1 << 24)], rp.rope(r, x[i:i + (1 << 24)], pos[i:i + (1 << 24)], 2)), i
+    rp.rope(r, x, pos, 2, out=x)
+    assert torch.equal(x, y)
+
+
+def test_more_rows_written_than_a_launch_has_room_for(rp):
+    H, hd, bits, page, T = 4, 32, 4, 16, (1 << 26) + 5
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough free memory")
+    _, _, kt, vt = site(H, hd, bits)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    k = torch.empty(T, H * hd, dtype=BF16, device="cuda")
+    some = torch.randn(1 << 16, H * hd, generator=gen, device="cuda").to(BF16)
+    for i in range(0, T, 1 << 16):
+        k[i:i + (1 << 16)] = some[:min(1 << 16, T - i)]
+    q = k[:, :hd]
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    slots = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    kept = torch.tensor([0, 1, 1000, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 26) - 1, 1 << 26, T - 1], device="cuda")
+    slots[kept] = torch.arange(len(kept), device="cuda") * 3
+    r = handle(rp, 32, True)
+    big, small = (rp.paged_cache(2, page, H, hd, bits, kt, vt) for _ in range(2))
+    got = rp.rope_quant_paged(big, r, q, k, k, pos, slots)
+    want = rp.rope_quant_paged(small, r, q[kept].contiguous(), k[kept].contiguous(), k[kept].contiguous(), pos[kept], slots[kept])
+    assert torch.equal(big.k_pages, small.k_pages) and torch.equal(big.v_pages, small.v_pages) and torch.equal(got[kept], want)
+    for i in range(0, T, 1 << 24):
+        assert torch.equal(got[i:i + (1 << 24)], rp.rope(r, q[i:i + (1 << 24)], pos[i:i + (1 << 24)], hd)), i
