@@ -541,7 +541,7 @@ int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t 
  *   workspace device, rptq_attend_weights_paged_workspace_bytes(B, queries, n_q_heads, n_kv_heads, head_dim) bytes, nothing to clear or keep;
  *           that may be none (a few queries), then it may be NULL
  *   1 <= queries <= RPTQ_MAX_WINDOW; fresh >= 0; the others as for rptq_attend_paged.  Sums are fp32, in an order that the call alone
- *   decides.  A NaN or infinity in q makes the weights of the tokens that it sees NaN.  Sequences that share pages keep records of their own.
+ *   decides, and off by at most 45 half steps beside the errors of what they add up, however many the queries.  A NaN or infinity in q makes the weights of the tokens that it sees NaN.  Sequences that share pages keep records of their own.
  *
  * rptq_evict_paged: every key/value head of every sequence of more than `budget` tokens keeps `budget` of them: those at positions
  * below `first`, those at positions beyond the head's largest minus `recent`, then those of the largest weight, equal ones

@@ -6,7 +6,7 @@
 // Scores come from the int8 matrix cores as there: a query head of a query is four rows of digits to the base 256, four of them a row
 // tile, 64 tokens a wave's tile, 256 a workgroup's.  q' and the zero points' term are formed in 64 bits up to the fixed point of
 // 30 bits below the head's largest |q'|; sums of digits are exact; a weight is rounded as its upper digits' sum becomes fp32 and
-// meets lse, as the lower ones' comes to it, by 2^x and by the sum over pairs (6e-8 to 6e-7 of the weights in all).
+// meets lse, as the lower ones' comes to it, by 2^x and by the sum over pairs (6e-8 to 6e-7 of the weights in all, in long windows too: kPasses).
 // A row tile's four belong to one key/value head where it has three pairs (query, head) or more; two pairs
 // share a tile with another head's two, single ones with three other heads' (heads under 128 wide).  A lane adds up its tokens'
 // weights over the row tiles in fp32 in their order, the four rows' sums come together by two exchanges, and each weight is read and
@@ -44,6 +44,13 @@ constexpr int kSide = 2;                       // row tiles that a wave works on
 // Row tiles whose digits lie in LDS at one time; more go through the tokens several times (16 | 32, and two workgroups per compute
 // unit instead of three: 5 x 8191, 32 queries, 23.7 | 29.2 us).
 __host__ __device__ constexpr int held_tiles(int blocks) { return blocks == 2 ? 8 : 16; }
+
+// A token's weight is rounded to fp32 once for every time that its head's row tiles go through LDS.  In windows of more such passes (half a step
+// each, 1.4e-6 at most) what that loses is kept in LDS and added at the end; a workgroup goes through all row tiles with so many token
+// tiles of a wave before it turns to the next ones.  (Without | with it, 16384 queries alike, 32 heads on 4 of 32: off by 2.6e-5 | 1.5e-7,
+// 48.7 | 52.5 ms; 32 on 8 of 128: 1.0e-5 | 1.7e-7, 5.45 | 5.77 ms.)
+constexpr int kPasses = 24;
+__host__ __device__ constexpr int carried_tiles(int heads) { return 8 / heads; }
 
 struct WeightPlan {
   int32_t group;                               // rows of a tile that belong to one key/value head: 1, 2 or 4
@@ -191,10 +198,10 @@ __global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightP
 }
 
 // NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace; STREAM: keys are read past the
-// last-level cache.  Three waves per SIMD where their registers suffice, nearly (four instead: spills, or 23.4 -> 29.5 us); digits made, several
-// heads: two (16 x 2048 of 32 heads of 32, 8 queries, 30.2 -> 24.6 us; 8 x 4096 of 12 of 64, 16 queries, 8 bits 20.1 -> 18.6), made here: three (20.0,
-// two 21.4).
-template <int BITS, int NB, int HEADS, bool MADE, bool STREAM>
+// last-level cache; CARRY: what sums lose is kept (in the kernel of all windows it cost registers, and spills in three of them).  Three waves per
+// SIMD where their registers suffice, nearly (four instead: spills, or 23.4 -> 29.5 us); digits made, several heads: two (16 x 2048 of 32 heads
+// of 32, 8 queries, 30.2 -> 24.6 us; 8 x 4096 of 12 of 64, 16 queries, 8 bits 20.1 -> 18.6), made here: three (20.0, two 21.4).
+template <int BITS, int NB, int HEADS, bool MADE, bool STREAM, bool CARRY>
 __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 32) ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
   constexpr int P = NB * kPageBlock;                       // positions of the unit
@@ -203,6 +210,8 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
   __shared__ __align__(16) unsigned char q_dig[kHeld * 16 * kDigitRow];
   __shared__ __align__(16) TileRows rows[kHeld];
   __shared__ __align__(16) unsigned char table[MADE ? 16 : P / 8 * 144];         // eight positions' records, and 16 bytes (banks)
+  constexpr int kCarried = carried_tiles(HEADS);
+  __shared__ float lost[CARRY ? 4 * kCarried * HEADS * kTile : 1];               // [wave][token tile][slot][lane]
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = blockIdx.x, unit = blockIdx.y, b = blockIdx.z;
@@ -276,12 +285,16 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
     for (int e = 0; e < HEADS; ++e) old_next[e] = a.weights[first_at + slot_head(e) * a.capacity + min(slot_token(k, e), len - 1)];
   };
 
+  // (CARRY: the wave's tiles from `reached` on, kCarried of them, and round again with the next ones; the first wave has the most)
+  const int most_tiles = CARRY ? (len - part * kTileTokens + step - 1) / step : 0;
+  int reached = 0;
   for (int tile0 = 0; tile0 < plan.tiles; tile0 += kHeld) {
     const int tile1 = min(tile0 + kHeld, plan.tiles);
-    int id = page_of(0, page0), next_page = page1;
-    if (my_tiles > 0) {
-      load_old(0);
-      load_keys(0, id);
+    const int k0 = CARRY ? reached : 0, k1 = CARRY ? min(k0 + kCarried, my_tiles) : my_tiles;
+    int id = page_of(k0, CARRY ? page_at(k0) : page0), next_page = CARRY ? page_at(k0 + 1) : page1;
+    if (k0 < k1) {
+      load_old(k0);
+      load_keys(k0, id);
     }
     if constexpr (MADE) {
       // 16 bytes of a row at a time, rows P apart there and kDigitRow apart here
@@ -293,7 +306,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
       i4v v[kEach];
 #pragma unroll
       for (int k = 0; k < kEach; ++k) v[k] = from[min(k * 256 + static_cast<int>(threadIdx.x), pieces - 1)];
-      if (tile0 > 0) __syncthreads();                      // (the digits before have been read)
+      if (tile0 > 0 || k0 > 0) __syncthreads();            // (the digits before have been read)
 #pragma unroll
       for (int k = 0; k < kEach; ++k) {
         const int i = k * 256 + static_cast<int>(threadIdx.x);
@@ -316,7 +329,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
     }
     __syncthreads();
 
-    for (int k = 0; k < my_tiles; ++k) {
+    for (int k = k0; k < k1; ++k) {
       const int token = token_of(k);
       const uint64_t here = __ballot(id >= 0);             // (bit r: the tile's r-th 16 tokens)
       uint32_t kw[4][NB][8];
@@ -327,9 +340,9 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
 #pragma unroll
       for (int e = 0; e < HEADS; ++e) old[e] = old_next[e];
       // (the next tile's: weights first, loads come back in order)
-      if (k + 1 < my_tiles) {
+      if (k + 1 < k1) {
         id = page_of(k + 1, next_page);
-        if (k + 2 < my_tiles) next_page = page_at(k + 2);
+        if (k + 2 < k1) next_page = page_at(k + 2);
         load_old(k + 1);
         load_keys(k + 1, id);
       }
@@ -428,9 +441,24 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
         const bool first = set * plan.set_tiles >= tile0, any = first ? set * plan.set_tiles < tile1 : (set + 1) * plan.set_tiles > tile0;
         const bool starts = first && t >= len - a.fresh;
         if (!any || t >= len) continue;
-        a.weights[at] = (starts ? 0.0f : old[e]) + got[e];
+        const float before = starts ? 0.0f : old[e];
+        float sum = before + got[e];
+        if constexpr (CARRY) {
+          // (what the sum of two loses is a number of fp32 itself)
+          float* mine = lost + ((wave * kCarried + (k - k0)) * HEADS + e) * kTile + lane;
+          const float second = sum - before;
+          float all = fabsf(sum) < __builtin_huge_valf() ? (before - (sum - second)) + (got[e] - second) : 0.0f;
+          if (!first) all += *mine;
+          if ((set + 1) * plan.set_tiles <= tile1) sum += all;
+          else *mine = all;
+        }
+        a.weights[at] = sum;
         if (starts) a.token_positions[at] = a.positions ? a.positions[b] - (len - 1 - t) : t;
       }
+    }
+    if (CARRY && tile1 == plan.tiles && k0 + kCarried < most_tiles) {
+      reached = k0 + kCarried;
+      tile0 = -kHeld;
     }
   }
 }
@@ -466,17 +494,19 @@ int32_t launch_attend_weights(const WeightArgs& a, int32_t bits, hipStream_t st)
   const dim3 grid(p.parts, units, a.B), makers((p.tiles + 3) / 4, units, a.B);
   const int64_t pages = std::min<int64_t>(a.g.n_pages, static_cast<int64_t>(a.B) * a.pages_per_seq);
   const bool stream = pages * 2 * (static_cast<int64_t>(a.g.d) * bits / 8 << a.g.page_shift) > kStreamBytes;
-  auto go = [&](auto digits, auto made, auto alone, auto streamed) {
+  const bool carry = p.set_tiles > kPasses * held_tiles(P / kPageBlock);
+  auto go = [&](auto digits, auto made, auto carried, auto alone, auto streamed) {
     if (p.tiles > kFewTiles) {
       hipLaunchKernelGGL(digits, makers, dim3(256), 0, st, a, p);
-      hipLaunchKernelGGL(made, grid, dim3(256), 0, st, a, p);
+      hipLaunchKernelGGL(carry ? carried : made, grid, dim3(256), 0, st, a, p);
     } else {
       hipLaunchKernelGGL(stream ? streamed : alone, grid, dim3(256), 0, st, a, p);
     }
   };
 #define RPTQ_GO(BITS, NB, HEADS) \
-  go(query_digits_kernel<BITS, NB, HEADS>, attend_weights_kernel<BITS, NB, HEADS, true, false>, attend_weights_kernel<BITS, NB, HEADS, false, false>, \
-     attend_weights_kernel<BITS, NB, HEADS, false, BITS < 8>)
+  go(query_digits_kernel<BITS, NB, HEADS>, attend_weights_kernel<BITS, NB, HEADS, true, false, false>,                  \
+     attend_weights_kernel<BITS, NB, HEADS, true, false, true>, attend_weights_kernel<BITS, NB, HEADS, false, false, false>, \
+     attend_weights_kernel<BITS, NB, HEADS, false, BITS < 8, false>)
 #define RPTQ_BY_BITS(NB, HEADS)                 \
   do {                                          \
     if (bits == 3) RPTQ_GO(3, NB, HEADS);       \
