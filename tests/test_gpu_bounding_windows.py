@@ -115,3 +115,25 @@ def test_sums_that_are_not_finite(rp):
     same = torch.ones(H, n, dtype=torch.bool, device="cuda")
     same[0, 3:5], same[1, 5] = False, False
     assert torch.equal(track.weights[0][same], clean.weights[0][same])
+
+
+def test_the_attention_of_a_window_leaves_its_sums(rp):
+    """lse from attend_paged: a row per query of the window, over the tokens that it sees.  What a sequence's tokens get of a query head adds up
+    to the number of queries that see any."""
+    H, share, hd, n = 2, 3, 64, 7
+    lens = [1000, 64, 1, 333, 0, 7]
+    b = Batch(rp, lens, H, hd, 4, 16)
+    q = queries_for(b, len(lens) * n * share).reshape(len(lens) * n, -1)
+    back = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    seen = (b.dev_lens[:, None] - back).reshape(-1).contiguous()
+    _, lse = rp.attend_paged(b.cache, q, b.page_table.repeat_interleave(n, 0), seen, want_lse=True)
+    track = rp.cache_track(b.cache, len(lens), 1000)
+    rp.attend_weights_paged(b.cache, q, b.page_table, b.dev_lens, lse, track, queries=n, fresh=1000)
+    got, ls, qn = track.weights.double().cpu().numpy(), lse.cpu().numpy(), q.float().cpu().numpy()
+    for i, length in enumerate(lens):
+        rows = slice(i * n, (i + 1) * n)
+        sums, tol = bounding.weights64(qn[rows], ls[rows], b.k[i], np.arange(length), length, b.hk, H * share, hd ** -0.5, n)
+        assert (np.abs(got[i, :, :length] - sums) <= tol).all()
+        # (every weight's error bound, and the logarithm's own, as where one query's weights add up)
+        assert np.abs(got[i].sum(-1) - share * min(n, length)).max() < 2e-4 * n
+        assert (got[i, :, length:] == 0).all()
