@@ -482,7 +482,8 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
  *     (a, b)  ->  (c a - s b, c b + s a),   c = amplitude cos(theta), s = amplitude sin(theta)
  * Pair j, 0 <= j < rotary_dim / 2, is channels (j, j + rotary_dim / 2) of the head, or (2 j, 2 j + 1) with `interleaved`;
  * the channels from rotary_dim on are not touched.  theta, its cosine and sine and their products with amplitude are
- * 64-bit numbers, c and s are rounded once to fp32, the two products and their sum to fp32 each.
+ * 64-bit numbers, c and s are rounded once to fp32, the two products and their sum to fp32 each.  Angles are turned by up to 2^47 in
+ * size (at the farthest positions 65536 radians each); a pair whose angle is larger or no number becomes NaN.
  *
  * rptq_rope_freqs (host): frequencies in radians per position and the amplitude that goes with them.
  *   RPTQ_ROPE_PLAIN   freqs[j] = base^(-2 j / rotary_dim), amplitude 1
@@ -491,13 +492,13 @@ int32_t rptq_attend_paged(const void* q, int64_t ld_q, int32_t B, int32_t n_q_he
  *   RPTQ_ROPE_PARTS   f = base^(-2 j / rotary_dim) turns w = f * trained / (2 pi) times over the trained length; with
  *                     u = (w - slow) / (fast - slow) held in [0, 1]: freqs[j] = u f + (1 - u) f / factor,
  *                     amplitude = 0.1 log(factor) + 1
- *   base > 0, factor >= 1; parts: trained > 0, 0 <= slow < fast.   freqs host out [rotary_dim / 2], amplitude host out.
+ *   base > 0 (not so near 0 that a frequency is infinite), factor >= 1; parts: trained > 0, 0 <= slow < fast.   freqs host out [rotary_dim / 2], amplitude host out.
  *
  * rptq_rope: rows of n_heads heads rotated, y = x turned.
  *   x, y    device, RPTQ_DTYPE_BF16 or RPTQ_DTYPE_F32 each (y is rounded once), rows of n_heads * head_dim values, ld_x and
  *           ld_y apart, on the type's own alignment; they may be columns of wider tensors.  y may be x (same type and stride), and
  *           may overlap it no other way.
- *   positions device int32 [T]: any number, also below zero;  freqs device double [rotary_dim / 2], any finite
+ *   positions device int32 [T]: any number, also below zero;  freqs device double [rotary_dim / 2]
  *   rotary_dim even, 2 .. head_dim; head_dim <= RPTQ_MAX_ROTARY_HEAD; n_heads * head_dim <= 2 RPTQ_MAX_CHANNELS
  *
  * rptq_rope_quant_paged: one launch for a step's queries, keys and values.  Queries are rotated as by rptq_rope (bf16 in and

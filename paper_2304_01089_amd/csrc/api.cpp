@@ -465,6 +465,7 @@ int32_t rptq_rope_freqs(int32_t rotary_dim, double base, int32_t scaling, double
     const double f = std::pow(used, -2.0 * j / rotary_dim);
     const double turns = f * trained / 6.283185307179586477, keep = parts ? std::fmin(1.0, std::fmax(0.0, (turns - slow) / (fast - slow))) : 0.0;
     freqs[j] = !scaled || scaling == RPTQ_ROPE_BASE ? f : f * keep + f / factor * (1.0 - keep);
+    if (!std::isfinite(freqs[j])) return RPTQ_ERR_RANGE;
   }
   *amplitude = parts ? 0.1 * std::log(factor) + 1.0 : 1.0;
   return RPTQ_OK;

@@ -22,8 +22,10 @@ void rope_part(const RopeArgs& a, int64_t first, int64_t rows, RopeLaunch* l);
 // (cos, sin) of an angle, times `amplitude`, rounded once to fp32.  In 64 bits: at position 10^6 the angle of the fastest pair has
 // 20 bits in front of the point, of which fp32 would leave four behind it.  k = round(2 theta / pi); theta - k pi / 2 by two fused
 // products with pi / 2 in two pieces (the first is exact); Taylor's series of sine and cosine to the 15th and 16th power, whose next
-// terms are below 2^-53 of the result for |r| <= pi / 4.  What is rounded to fp32 is thus within 2^-51 or so of the exact value, and the fp32
-// number is the nearest one but for one angle in 2^27 or so.
+// terms are below 2^-53 of the result for |r| <= pi / 4.  What is rounded to fp32 is thus within 2^-51 or so of the exact value, or 2^-62 of
+// the amplitude (pi / 2's next piece, next to a zero of a far angle), and the fp32 number is the nearest one but for one angle in 2^27 or so.
+// This holds up to angles of 2^47 (65536 a position at position 2^31), where k is up to 0.02 off and |r| up to 0.81.  Beyond 2^48 k's own
+// rounding leaves ever larger r, and the series soon no cosine: larger angles, and what is no number, become NaN.
 __device__ __forceinline__ float2 rope_turn(double theta, double amplitude) {
   const double k = rint(theta * 0.63661977236758134308);
   double r = fma(-k, 1.57079632679489661923, theta);
@@ -49,7 +51,8 @@ __device__ __forceinline__ float2 rope_turn(double theta, double amplitude) {
   const int quarter = static_cast<int>(fma(-4.0, floor(k * 0.25), k));
   const double a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
   const double cos_t = quarter == 1 || quarter == 2 ? -a : a, sin_t = quarter >= 2 ? -b : b;
-  return make_float2(static_cast<float>(cos_t * amplitude), static_cast<float>(sin_t * amplitude));
+  const double size = fabs(theta) <= 0x1p47 ? amplitude : __builtin_nan("");
+  return make_float2(static_cast<float>(cos_t * size), static_cast<float>(sin_t * size));
 }
 
 // (a, b) turned: two products and their sum, each rounded (the order that decides a code).
