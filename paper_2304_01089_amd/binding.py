@@ -147,7 +147,8 @@ def _set_up_calls(lib):
         objects = dict(get_device=torch._C._cuda_getDevice, get_stream=torch._C._cuda_getCurrentRawStream)
     except (ImportError, AttributeError):
         return
-    if torch.__version__.split("+")[0] != getattr(_calls, "torch_version", None):   # (it reads tensors as the torch that it was built with lays them out)
+    # (it reads tensors as the torch that it was built with lays them out)
+    if torch.__version__.partition("+")[::2] != (getattr(_calls, "torch_version", None), getattr(_calls, "torch_local", None)):
         return
     names = ("rptq_ln_quant", "rptq_cluster_gemm", "rptq_cluster_gemm_quant", "rptq_cluster_rowsums", "rptq_cluster_gemm_cw",
              "rptq_kv_quant", "rptq_kv_dequant", "rptq_kv_page_bytes", "rptq_kv_quant_paged", "rptq_kv_dequant_paged",

@@ -55,22 +55,30 @@ def build_calls() -> Optional[str]:
     if os.path.exists(untagged):                 # (any interpreter would load it)
         os.remove(untagged)
     include = sysconfig.get_paths()["include"]
-    found = importlib.util.find_spec("torch")      # (torch itself is not loaded)
-    torch = found.submodule_search_locations[0] if found else ""
-    headers = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    found = importlib.util.find_spec("torch")
+    folder = found.submodule_search_locations[0] if found else ""
+    headers = [os.path.join(folder, "include"), os.path.join(folder, "include", "torch", "csrc", "api", "include")]
     lacks = [what for what, there in (("g++", shutil.which("g++")), ("Python.h", os.path.exists(os.path.join(include, "Python.h"))),
                                       ("torch/version.h", os.path.exists(os.path.join(headers[1], "torch", "version.h"))))
              if not there]
+    if not lacks:
+        try:
+            import torch                         # (whose full name and C++ ABI no header says)
+        except (ImportError, OSError) as e:
+            lacks = ["torch (%s)" % e]
     if lacks:
         sys.stderr.write("no native marshalling of calls: %s not found\n" % " and ".join(lacks))
         if os.path.exists(CALLS):                # (of an older source)
             os.remove(CALLS)
         return None
     tmp = CALLS + ".tmp"
+    version, _, local = torch.__version__.partition("+")
     # (torch's libraries are found by name: the module is imported once torch has loaded them)
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", include,
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           '-DRPTQ_TORCH_VERSION="%s"' % version, '-DRPTQ_TORCH_LOCAL="%s"' % local,
            *[o for h in headers for o in ("-isystem", h)], os.path.join(CSRC, "calls.cpp"), "-o", tmp,
-           "-L", os.path.join(torch, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
+           "-L", os.path.join(folder, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed for calls.cpp:\n%s\n%s" % (res.stdout, res.stderr))

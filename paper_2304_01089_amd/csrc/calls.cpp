@@ -13,7 +13,6 @@
 #include <Python.h>
 #include <stdint.h>
 #include <torch/csrc/autograd/python_variable.h>
-#include <torch/version.h>
 
 #include "rptq.h"
 
@@ -583,6 +582,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 
 PyMODINIT_FUNC PyInit__calls(void) {
   PyObject* m = PyModule_Create(&module);
-  if (m != nullptr && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) != 0) Py_CLEAR(m);
+  // (torch.__version__ of the torch that it was built with, before and behind the plus)
+  if (m != nullptr && (PyModule_AddStringConstant(m, "torch_version", RPTQ_TORCH_VERSION) != 0 ||
+                       PyModule_AddStringConstant(m, "torch_local", RPTQ_TORCH_LOCAL) != 0))
+    Py_CLEAR(m);
   return m;
 }
