@@ -165,6 +165,13 @@ def _set_up_calls(lib):
 # than to ask for its address.  The entry points of a serving loop try the native marshalling first, which returns None
 # for arguments out of the ordinary: rptq_ln_quant + rptq_cluster_gemm take 9.9 us on the host, 4.8 + 5.1, instead of 15.0, 7.5 +
 # 6.8; a launch alone is about 3.4.)
+def _own_attributes():
+    """Within it a tensor's attributes are read as they are: a subclass is otherwise asked for each through its __torch_function__
+    (rptq_rope with three such tensors 59 us on the host, 10 within this)."""
+    import torch
+    return torch._C.DisableTorchFunctionSubclass()
+
+
 def _dev(t, dtype=None, allow_none=False):
     """Device address of a torch tensor (None -> NULL)."""
     if t is None:
@@ -347,15 +354,16 @@ def rptq_ln_quant(x, M: int, d: int, gamma_pad, beta_pad, eps: float, relu: bool
     st = None if _CALLS is None else _CALLS.ln_quant(
         x, M, d, gamma_pad, beta_pad, eps, relu, perm_pad, cluster_off, s, inv_s, z, bits, codes_packed, xsum, rowterm, stream)
     if st is None:
-        import torch
-        off, poff = _host(cluster_off, np.int32)
-        sa, ps = _host(s, np.float32)
-        ia, pi = _host(inv_s, np.float32)
-        za, pz = _host(z, np.int32)
-        st = load_library().rptq_ln_quant(
-            _dev(x, torch.bfloat16), M, d, _dev(gamma_pad, torch.float32, True), _dev(beta_pad, torch.float32, True),
-            float(eps), int(bool(relu)), _dev(perm_pad, torch.int32), poff, len(off) - 1, ps, pi, pz, bits,
-            _dev(codes_packed), _dev(xsum, torch.int32, True), _dev(rowterm, torch.float32, True), _stream(stream))
+        with _own_attributes():
+            import torch
+            off, poff = _host(cluster_off, np.int32)
+            sa, ps = _host(s, np.float32)
+            ia, pi = _host(inv_s, np.float32)
+            za, pz = _host(z, np.int32)
+            st = load_library().rptq_ln_quant(
+                _dev(x, torch.bfloat16), M, d, _dev(gamma_pad, torch.float32, True), _dev(beta_pad, torch.float32, True),
+                float(eps), int(bool(relu)), _dev(perm_pad, torch.int32), poff, len(off) - 1, ps, pi, pz, bits,
+                _dev(codes_packed), _dev(xsum, torch.int32, True), _dev(rowterm, torch.float32, True), _stream(stream))
     _check(st, "rptq_ln_quant")
 
 
@@ -412,19 +420,20 @@ def rptq_cluster_gemm(codes_packed, M: int, bits: int, Wq_packed, N: int, cluste
     st = None if _CALLS is None else _CALLS.cluster_gemm(
         codes_packed, M, bits, Wq_packed, N, cluster_off, sX, sW, zW, colterm, rowterm, y, stream)
     if st is None:
-        import torch
-        off, poff = _host(cluster_off, np.int32)
-        sx, psx = _host(sX, np.float32)
-        if y.dtype == torch.float32:
-            y_dtype = DTYPE_F32
-        elif y.dtype == torch.bfloat16:
-            y_dtype = DTYPE_BF16
-        else:
-            raise ValueError("y must be bf16 or fp32")
-        st = load_library().rptq_cluster_gemm(
-            _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, psx,
-            _dev(sW, torch.float32), _dev(zW, torch.int32), _dev(colterm, torch.float32),
-            _dev(rowterm, torch.float32), _dev(y), y_dtype, _stream(stream))
+        with _own_attributes():
+            import torch
+            off, poff = _host(cluster_off, np.int32)
+            sx, psx = _host(sX, np.float32)
+            if y.dtype == torch.float32:
+                y_dtype = DTYPE_F32
+            elif y.dtype == torch.bfloat16:
+                y_dtype = DTYPE_BF16
+            else:
+                raise ValueError("y must be bf16 or fp32")
+            st = load_library().rptq_cluster_gemm(
+                _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, psx,
+                _dev(sW, torch.float32), _dev(zW, torch.int32), _dev(colterm, torch.float32),
+                _dev(rowterm, torch.float32), _dev(y), y_dtype, _stream(stream))
     _check(st, "rptq_cluster_gemm")
 
 
@@ -439,19 +448,20 @@ def rptq_cluster_gemm_quant(codes_packed, M: int, bits: int, Wq_packed, N: int, 
         codes_packed, M, bits, Wq_packed, N, cluster_off, sX, sW, zW, colterm, rowterm, relu, next_cluster_off, next_s,
         next_inv_s, next_z, next_bits, next_codes, next_rowterm, workspace, stream)
     if st is None:
-        import torch
-        off, poff = _host(cluster_off, np.int32)
-        sx, psx = _host(sX, np.float32)
-        noff, pnoff = _host(next_cluster_off, np.int32)
-        ns, pns = _host(next_s, np.float32)
-        ni, pni = _host(next_inv_s, np.float32)
-        nz, pnz = _host(next_z, np.int32)
-        st = load_library().rptq_cluster_gemm_quant(
-            _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, psx,
-            _dev(sW, torch.float32), _dev(zW, torch.int32), _dev(colterm, torch.float32),
-            _dev(rowterm, torch.float32), int(bool(relu)), pnoff, len(noff) - 1, pns, pni, pnz, next_bits,
-            _dev(next_codes), _dev(next_rowterm, torch.float32), _dev(workspace),
-            workspace.numel() * workspace.element_size(), _stream(stream))
+        with _own_attributes():
+            import torch
+            off, poff = _host(cluster_off, np.int32)
+            sx, psx = _host(sX, np.float32)
+            noff, pnoff = _host(next_cluster_off, np.int32)
+            ns, pns = _host(next_s, np.float32)
+            ni, pni = _host(next_inv_s, np.float32)
+            nz, pnz = _host(next_z, np.int32)
+            st = load_library().rptq_cluster_gemm_quant(
+                _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, psx,
+                _dev(sW, torch.float32), _dev(zW, torch.int32), _dev(colterm, torch.float32),
+                _dev(rowterm, torch.float32), int(bool(relu)), pnoff, len(noff) - 1, pns, pni, pnz, next_bits,
+                _dev(next_codes), _dev(next_rowterm, torch.float32), _dev(workspace),
+                workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "rptq_cluster_gemm_quant")
 
 
@@ -523,12 +533,13 @@ def rptq_cluster_rowsums(codes_packed, M: int, bits: int, cluster_off, sX, zX, r
     st = None if _CALLS is None else _CALLS.cluster_rowsums(
         codes_packed, M, bits, cluster_off, sX, zX, rowsums, stream)
     if st is None:
-        import torch
-        off, poff = _host(cluster_off, np.int32)
-        sx, psx = _host(sX, np.float32)
-        zx, pzx = _host(zX, np.int32)
-        st = load_library().rptq_cluster_rowsums(_dev(codes_packed), M, bits, poff, len(off) - 1, psx, pzx,
-                                                 _dev(rowsums, torch.float32), _stream(stream))
+        with _own_attributes():
+            import torch
+            off, poff = _host(cluster_off, np.int32)
+            sx, psx = _host(sX, np.float32)
+            zx, pzx = _host(zX, np.int32)
+            st = load_library().rptq_cluster_rowsums(_dev(codes_packed), M, bits, poff, len(off) - 1, psx, pzx,
+                                                     _dev(rowsums, torch.float32), _stream(stream))
     _check(st, "rptq_cluster_rowsums")
 
 
@@ -537,18 +548,19 @@ def rptq_cluster_gemm_cw(codes_packed, M: int, bits: int, Wq_packed, N: int, clu
     st = None if _CALLS is None else _CALLS.cluster_gemm_cw(
         codes_packed, M, bits, Wq_packed, N, cluster_off, scale_tab, cross_tab, colterm, rowsums, y, stream)
     if st is None:
-        import torch
-        off, poff = _host(cluster_off, np.int32)
-        if y.dtype == torch.float32:
-            y_dtype = DTYPE_F32
-        elif y.dtype == torch.bfloat16:
-            y_dtype = DTYPE_BF16
-        else:
-            raise ValueError("y must be bf16 or fp32")
-        st = load_library().rptq_cluster_gemm_cw(
-            _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, _dev(scale_tab, torch.float32),
-            _dev(cross_tab, torch.float32), _dev(colterm, torch.float32), _dev(rowsums, torch.float32), _dev(y), y_dtype,
-            _stream(stream))
+        with _own_attributes():
+            import torch
+            off, poff = _host(cluster_off, np.int32)
+            if y.dtype == torch.float32:
+                y_dtype = DTYPE_F32
+            elif y.dtype == torch.bfloat16:
+                y_dtype = DTYPE_BF16
+            else:
+                raise ValueError("y must be bf16 or fp32")
+            st = load_library().rptq_cluster_gemm_cw(
+                _dev(codes_packed), M, bits, _dev(Wq_packed), N, poff, len(off) - 1, _dev(scale_tab, torch.float32),
+                _dev(cross_tab, torch.float32), _dev(colterm, torch.float32), _dev(rowsums, torch.float32), _dev(y), y_dtype,
+                _stream(stream))
     _check(st, "rptq_cluster_gemm_cw")
 
 
@@ -605,8 +617,9 @@ def rptq_kv_quant(x, T: int, d: int, table, bits: int, codes, stream=None):
     st = None if _CALLS is None else _CALLS.kv_quant(
         x, T, d, table, bits, codes, stream)
     if st is None:
-        import torch
-        st = load_library().rptq_kv_quant(_dev(x, torch.bfloat16), T, d, _dev(table), bits, _dev(codes), _stream(stream))
+        with _own_attributes():
+            import torch
+            st = load_library().rptq_kv_quant(_dev(x, torch.bfloat16), T, d, _dev(table), bits, _dev(codes), _stream(stream))
     _check(st, "rptq_kv_quant")
 
 
@@ -614,8 +627,9 @@ def rptq_kv_dequant(codes, T: int, d: int, table, bits: int, out, stream=None):
     st = None if _CALLS is None else _CALLS.kv_dequant(
         codes, T, d, table, bits, out, stream)
     if st is None:
-        import torch
-        st = load_library().rptq_kv_dequant(_dev(codes), T, d, _dev(table), bits, _dev(out, torch.bfloat16), _stream(stream))
+        with _own_attributes():
+            import torch
+            st = load_library().rptq_kv_dequant(_dev(codes), T, d, _dev(table), bits, _dev(out, torch.bfloat16), _stream(stream))
     _check(st, "rptq_kv_dequant")
 
 
@@ -689,13 +703,14 @@ def rptq_kv_quant_paged(k, v, slots, k_table, v_table, bits: int, k_pages, v_pag
     """k, v: bf16 [T, d], rows of any stride; slots: int64 [T]; tables: 16 d bytes; pages: uint8, a whole number of pages."""
     st = None if _CALLS is None else _CALLS.kv_quant_paged(k, v, slots, k_table, v_table, bits, k_pages, v_pages, page_size, stream)
     if st is None:
-        import torch
-        T, d = _tokens(k, v, slots)
-        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
-        st = load_library().rptq_kv_quant_paged(
-            ka, ld_k, va, ld_v, T, d, _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), bits,
-            _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
+        with _own_attributes():
+            import torch
+            T, d = _tokens(k, v, slots)
+            kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+            (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+            st = load_library().rptq_kv_quant_paged(
+                ka, ld_k, va, ld_v, T, d, _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), bits,
+                _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size, _stream(stream)) if T else 0
     _check(st, "rptq_kv_quant_paged")
 
 
@@ -703,14 +718,15 @@ def rptq_kv_dequant_paged(k_pages, v_pages, page_size: int, bits: int, slots, k_
     """k, v: bf16 [T, d] out, rows of any stride; slots: int64 [T]."""
     st = None if _CALLS is None else _CALLS.kv_dequant_paged(k_pages, v_pages, page_size, bits, slots, k_table, v_table, k, v, stream)
     if st is None:
-        import torch
-        T, d = _tokens(k, v, slots)
-        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
-        st = load_library().rptq_kv_dequant_paged(
-            kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
-            _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), ka, ld_k, va, ld_v,
-            _stream(stream)) if T else 0
+        with _own_attributes():
+            import torch
+            T, d = _tokens(k, v, slots)
+            kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+            (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+            st = load_library().rptq_kv_dequant_paged(
+                kp, vp, n_pages, page_size, bits, _whole(slots, torch.int64, "slots", 0), T, d,
+                _position_table(k_table, "k_table", d), _position_table(v_table, "v_table", d), ka, ld_k, va, ld_v,
+                _stream(stream)) if T else 0
     _check(st, "rptq_kv_dequant_paged")
 
 
@@ -726,26 +742,27 @@ def rptq_attend_paged(q, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: 
         q, n_q_heads, n_kv_heads, head_dim, scale, k_table, v_table, bits, k_pages, v_pages, page_size, page_table, lens, out, lse,
         workspace, stream)
     if st is None:
-        import torch
-        B, d = q.shape[0], n_kv_heads * head_dim
-        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-        if out.dtype == torch.float32:
-            out_dtype = DTYPE_F32
-        elif out.dtype == torch.bfloat16:
-            out_dtype = DTYPE_BF16
-        else:
-            raise ValueError("out must be bf16 or fp32")
-        if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != B:
-            raise ValueError("expected page_table [B, pages] and lens [B]")
-        qa, ld_q = _matrix(q, torch.bfloat16, "q", (B, n_q_heads * head_dim))
-        oa, ld_out = _matrix(out, None, "out", (B, n_q_heads * head_dim))
-        pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
-        la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
-        st = load_library().rptq_attend_paged(
-            qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d),
-            _position_table(v_table, "v_table", d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
-            _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
-            workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+        with _own_attributes():
+            import torch
+            B, d = q.shape[0], n_kv_heads * head_dim
+            kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+            if out.dtype == torch.float32:
+                out_dtype = DTYPE_F32
+            elif out.dtype == torch.bfloat16:
+                out_dtype = DTYPE_BF16
+            else:
+                raise ValueError("out must be bf16 or fp32")
+            if page_table.dim() != 2 or lens.dim() != 1 or lens.shape[0] != B:
+                raise ValueError("expected page_table [B, pages] and lens [B]")
+            qa, ld_q = _matrix(q, torch.bfloat16, "q", (B, n_q_heads * head_dim))
+            oa, ld_out = _matrix(out, None, "out", (B, n_q_heads * head_dim))
+            pa, ld_pt = _matrix(page_table, torch.int32, "page_table", (B, page_table.shape[1]))
+            la = None if lse is None else _whole(lse, torch.float32, "lse", 4 * B * n_q_heads)
+            st = load_library().rptq_attend_paged(
+                qa, ld_q, B, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d),
+                _position_table(v_table, "v_table", d), bits, kp, vp, n_pages, page_size, pa, ld_pt, page_table.shape[1],
+                _whole(lens, torch.int32, "lens", 0), oa, ld_out, out_dtype, la, _whole(workspace, None, "workspace", 0),
+                workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_paged")
 
 
@@ -789,12 +806,13 @@ def rptq_rope(x, y, positions, head_dim: int, rotary_dim: int, interleaved: bool
     """x, y: bf16 or fp32 [T, n_heads * head_dim], rows of any stride (y may be x); positions: int32 [T]; freqs: float64."""
     st = None if _CALLS is None else _CALLS.rope(x, y, positions, head_dim, rotary_dim, interleaved, freqs, amplitude, stream)
     if st is None:
-        if x.dim() != 2 or head_dim < 1 or x.shape[1] % head_dim != 0:
-            raise ValueError("x: expected [T, n_heads * %d]" % head_dim)
-        (xa, ld_x), (ya, ld_y) = _matrix(x, None, "x", x.shape), _matrix(y, None, "y", x.shape)
-        st = load_library().rptq_rope(xa, _float_type(x, "x"), ld_x, ya, _float_type(y, "y"), ld_y, _row_positions(positions, x.shape[0]),
-                                      x.shape[0], x.shape[1] // head_dim, head_dim, rotary_dim, int(interleaved),
-                                      _frequencies(freqs, rotary_dim), amplitude, _stream(stream)) if x.shape[0] else 0
+        with _own_attributes():
+            if x.dim() != 2 or head_dim < 1 or x.shape[1] % head_dim != 0:
+                raise ValueError("x: expected [T, n_heads * %d]" % head_dim)
+            (xa, ld_x), (ya, ld_y) = _matrix(x, None, "x", x.shape), _matrix(y, None, "y", x.shape)
+            st = load_library().rptq_rope(xa, _float_type(x, "x"), ld_x, ya, _float_type(y, "y"), ld_y, _row_positions(positions, x.shape[0]),
+                                          x.shape[0], x.shape[1] // head_dim, head_dim, rotary_dim, int(interleaved),
+                                          _frequencies(freqs, rotary_dim), amplitude, _stream(stream)) if x.shape[0] else 0
     _check(st, "rptq_rope")
 
 
@@ -805,26 +823,27 @@ def rptq_rope_quant_paged(q, q_out, k, v, positions, slots, head_dim: int, rotar
         q, q_out, k, v, positions, slots, head_dim, rotary_dim, interleaved, freqs, amplitude, k_table, v_table, bits, k_pages, v_pages,
         page_size, stream)
     if st is None:
-        import torch
-        T, d = _tokens(k, v, slots)
-        if head_dim < 1 or d % head_dim != 0:
-            raise ValueError("k and v: expected [T, n_kv_heads * %d]" % head_dim)
-        kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
-        (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
-        (qa, ld_q), (oa, ld_out), n_q = (None, 0), (None, 0), 0
-        if (q is None) != (q_out is None):
-            raise ValueError("q and q_out: expected both or none")
-        if q is not None:
-            if q.dim() != 2 or q.shape[1] % head_dim != 0:
-                raise ValueError("q: expected [T, n_q_heads * %d]" % head_dim)
-            n_q = q.shape[1] // head_dim
-            qa, ld_q = _matrix(q, torch.bfloat16, "q", (T, n_q * head_dim))
-            oa, ld_out = _matrix(q_out, torch.bfloat16, "q_out", (T, n_q * head_dim))
-        st = load_library().rptq_rope_quant_paged(
-            qa, ld_q, oa, ld_out, n_q, ka, ld_k, va, ld_v, T, d // head_dim, head_dim, _row_positions(positions, T), rotary_dim,
-            int(interleaved), _frequencies(freqs, rotary_dim), amplitude, _position_table(k_table, "k_table", d),
-            _position_table(v_table, "v_table", d), bits, _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size,
-            _stream(stream)) if T else 0
+        with _own_attributes():
+            import torch
+            T, d = _tokens(k, v, slots)
+            if head_dim < 1 or d % head_dim != 0:
+                raise ValueError("k and v: expected [T, n_kv_heads * %d]" % head_dim)
+            kp, vp, n_pages = _pages(k_pages, v_pages, d, page_size, bits)
+            (ka, ld_k), (va, ld_v) = _matrix(k, torch.bfloat16, "k", (T, d)), _matrix(v, torch.bfloat16, "v", (T, d))
+            (qa, ld_q), (oa, ld_out), n_q = (None, 0), (None, 0), 0
+            if (q is None) != (q_out is None):
+                raise ValueError("q and q_out: expected both or none")
+            if q is not None:
+                if q.dim() != 2 or q.shape[1] % head_dim != 0:
+                    raise ValueError("q: expected [T, n_q_heads * %d]" % head_dim)
+                n_q = q.shape[1] // head_dim
+                qa, ld_q = _matrix(q, torch.bfloat16, "q", (T, n_q * head_dim))
+                oa, ld_out = _matrix(q_out, torch.bfloat16, "q_out", (T, n_q * head_dim))
+            st = load_library().rptq_rope_quant_paged(
+                qa, ld_q, oa, ld_out, n_q, ka, ld_k, va, ld_v, T, d // head_dim, head_dim, _row_positions(positions, T), rotary_dim,
+                int(interleaved), _frequencies(freqs, rotary_dim), amplitude, _position_table(k_table, "k_table", d),
+                _position_table(v_table, "v_table", d), bits, _whole(slots, torch.int64, "slots", 0), kp, vp, n_pages, page_size,
+                _stream(stream)) if T else 0
     _check(st, "rptq_rope_quant_paged")
 
 
@@ -860,20 +879,21 @@ def rptq_attend_weights_paged(q, queries: int, n_q_heads: int, n_kv_heads: int, 
         q, queries, n_q_heads, n_kv_heads, head_dim, scale, k_table, bits, k_pages, page_size, page_table, lens, lse, positions, fresh,
         weights, token_positions, workspace, stream)
     if st is None:
-        import torch
-        d = n_kv_heads * head_dim
-        pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
-        kp, _, n_pages = _pages(k_pages, k_pages, d, page_size, bits)
-        qa, ld_q = _matrix(q, torch.bfloat16, "q", (B * queries, n_q_heads * head_dim))
-        if tuple(lse.shape) != (B * queries, n_q_heads):
-            raise ValueError("lse: expected shape %s, got %s" % ((B * queries, n_q_heads), tuple(lse.shape)))
-        wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
-        st = load_library().rptq_attend_weights_paged(
-            qa, ld_q, B, queries, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d), bits, kp, n_pages,
-            page_size, pa, ld_pt, per_seq, la, _whole(lse, torch.float32, "lse", 0),
-            None if positions is None else _row_positions(positions, B), fresh, wa, ta, capacity,
-            None if workspace is None else _whole(workspace, None, "workspace", 0),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+        with _own_attributes():
+            import torch
+            d = n_kv_heads * head_dim
+            pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
+            kp, _, n_pages = _pages(k_pages, k_pages, d, page_size, bits)
+            qa, ld_q = _matrix(q, torch.bfloat16, "q", (B * queries, n_q_heads * head_dim))
+            if tuple(lse.shape) != (B * queries, n_q_heads):
+                raise ValueError("lse: expected shape %s, got %s" % ((B * queries, n_q_heads), tuple(lse.shape)))
+            wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
+            st = load_library().rptq_attend_weights_paged(
+                qa, ld_q, B, queries, n_q_heads, n_kv_heads, head_dim, float(scale), _position_table(k_table, "k_table", d), bits, kp, n_pages,
+                page_size, pa, ld_pt, per_seq, la, _whole(lse, torch.float32, "lse", 0),
+                None if positions is None else _row_positions(positions, B), fresh, wa, ta, capacity,
+                None if workspace is None else _whole(workspace, None, "workspace", 0),
+                0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_attend_weights_paged")
 
 
@@ -889,19 +909,20 @@ def rptq_evict_paged(n_kv_heads: int, head_dim: int, bits: int, k_pages, v_pages
         n_kv_heads, head_dim, bits, k_pages, v_pages, page_size, page_table, lens, weights, token_positions, budget, first, recent,
         weights_out, token_positions_out, lens_out, workspace, stream)
     if st is None:
-        import torch
-        pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
-        kp, vp, n_pages = _pages(k_pages, v_pages, n_kv_heads * head_dim, page_size, bits)
-        wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
-        wo, to, cap_out = _records(weights_out, token_positions_out, B, n_kv_heads, "the new ")
-        if cap_out != capacity:
-            raise ValueError("the new weights and positions: expected the old ones' shape")
-        if lens_out.dim() != 1 or lens_out.shape[0] != B:
-            raise ValueError("lens_out: expected one per sequence")
-        st = load_library().rptq_evict_paged(
-            B, n_kv_heads, head_dim, bits, kp, vp, n_pages, page_size, pa, ld_pt, per_seq, la, wa, ta, capacity, budget, first, recent,
-            wo, to, _whole(lens_out, torch.int32, "lens_out", 0), _whole(workspace, None, "workspace", 0),
-            workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
+        with _own_attributes():
+            import torch
+            pa, ld_pt, per_seq, la, B = _sequences(page_table, lens)
+            kp, vp, n_pages = _pages(k_pages, v_pages, n_kv_heads * head_dim, page_size, bits)
+            wa, ta, capacity = _records(weights, token_positions, B, n_kv_heads)
+            wo, to, cap_out = _records(weights_out, token_positions_out, B, n_kv_heads, "the new ")
+            if cap_out != capacity:
+                raise ValueError("the new weights and positions: expected the old ones' shape")
+            if lens_out.dim() != 1 or lens_out.shape[0] != B:
+                raise ValueError("lens_out: expected one per sequence")
+            st = load_library().rptq_evict_paged(
+                B, n_kv_heads, head_dim, bits, kp, vp, n_pages, page_size, pa, ld_pt, per_seq, la, wa, ta, capacity, budget, first, recent,
+                wo, to, _whole(lens_out, torch.int32, "lens_out", 0), _whole(workspace, None, "workspace", 0),
+                workspace.numel() * workspace.element_size(), _stream(stream)) if B else 0
     _check(st, "rptq_evict_paged")
 
 
