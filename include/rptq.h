@@ -529,7 +529,8 @@ int32_t rptq_rope_quant_paged(const void* q, int64_t ld_q, void* q_out, int64_t 
  * A program that drops tokens keeps a record of every token of every key/value head: weights, fp32 [B, n_kv_heads, capacity], what
  * the token got of the attention so far, and token_positions, int32 of the same shape, where in the text it stands.  Entry
  * [b, h, t] belongs to token t of sequence b as the page table numbers them.  Both contiguous; entries behind the
- * sequence's length are neither read nor written.  A sequence has min(lens[b], pages_per_seq * page_size, capacity) tokens.
+ * sequence's length are neither read nor written.  A sequence has min(lens[b], pages_per_seq * page_size, capacity) tokens
+ * (lens[b] below 0 counts as 0), and lens[b] stands for that number in what follows.
  *
  * rptq_attend_weights_paged: the last `queries` tokens of every sequence have attended to the cache (rptq_attend_paged, one row
  * each); with a_git query head g's score of token t for query i and lse_gi what that call left,

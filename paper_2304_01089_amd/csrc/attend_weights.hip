@@ -13,12 +13,14 @@
 // written by one lane: no order of adding depends on anything but the call.
 //
 // Up to kFewTiles row tiles each wave makes one tile's digits itself: queries are requested with the first loads, in their own order,
-// and gathered in LDS (gathered from memory, behind the positions' records: 1 x 257 tokens 5.23 us, now 4.96).  More are made once by a
-// launch of their own, into the workspace, instead of by each of a sequence's workgroups (5 x 8191 tokens, 32 queries: 29.6 -> 23.7 us).
+// and gathered in LDS (from memory, behind the positions' records, took 1 x 257 tokens a quarter of a microsecond more).  More are made once
+// by a launch of their own, into the workspace, instead of by each of a sequence's workgroups (a fifth off 5 x 8191 tokens, 32 queries).
 // What bounds it: with few queries memory, and the start of every workgroup (length, page number, codes, one after the other, while
-// its digits are made): 32 sequences of up to 4096 tokens, 40 heads of 128 at 4 bits take 43.8 us for 195 MB, 4.5 TB/s; one short
-// sequence 5, of which a launch is 1.8.  With many queries the vector instructions that make a weight of four sums of digits, about
-// seven and an exponential, beside two matrix instructions for sixteen tokens of four pairs: 23.6 us for 3.4 GFLOP, digits 4 of them.
+// its digits are made): 32 sequences of up to 4096 tokens, 40 heads of 128 at 4 bits take 43.7 us for 195 MB, 4.5 TB/s; one short
+// sequence 5, of which a launch is 1.8.  With many queries waits: 5 x 8191 tokens, 32 on 8 heads, 32 queries take 23.4 us for 3.4 GFLOP, digits
+// 4 of them.  Of the 19 of this kernel vector instructions (about seven and an exponential for a weight) fill 7 on every SIMD and matrix
+// instructions 3.4 beside them; 1.4 waves are there on average, and wait for a third of their time: row tiles go through LDS in two passes,
+// each with its digits, keys and weights requested anew behind a barrier, and a tile's operands are read from LDS as they are used.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,18 +33,21 @@
 namespace rptq {
 
 constexpr int kTileTokens = 4 * kTile;         // of a workgroup's four waves
-// As many parts as make this many workgroups, where there are tokens for them (1024 | 2048 | 5000: 32 x 4096 of 40 heads 47.5 | 43.8 | 45.0 us,
-// 16 x 8192 of 40 at 3 bits 72.1 | 63.1 | 63.8, 5 x 8191 of 32 on 8 with 32 queries 26.1 | 23.3 | 23.3, 16 x 4096 of 32 heads of 32 17.4 | 19.8 | 19.8).
+// As many parts as make this many workgroups, where there are tokens for them (1024 | 2048 | 5000: 32 x 4096 of 40 heads 47.3 | 43.7 | 44.8 us,
+// 16 x 8192 of 40 at 3 bits 72.5 | 63.2 | 63.0, 5 x 8191 of 32 on 8 with 32 queries 25.7 | 23.4 | 23.3, 16 x 4096 of 12 14.0 | 14.5 | 15.4, of 32 heads of
+// 32 17.2 | 19.8 | 19.8).
 constexpr int kSeenWorkgroups = 2048;
 
 // Keys of larger caches, values included, are read past the last-level cache, at 3 and 4 bits (an ordinary | such a load: 32 x 4096 of 40
-// heads 46.1 | 43.8 us, 16 x 8192 at 3 bits 66.3 | 63.0; smaller caches, 5 x 8191, 23.4 | 24.0).
+// heads 46.2 | 43.7 us, 16 x 8192 at 3 bits 67.2 | 63.2; a smaller cache, 16 x 4096 of 12, 14.5 | 15.7).
 constexpr int64_t kStreamBytes = INT64_C(256) << 20;
 constexpr int kFewTiles = 4;                   // row tiles of which each wave of a workgroup makes one
-constexpr int kSide = 2;                       // row tiles that a wave works on side by side (1 | 2 | 4: 5 x 8191, 32 queries, 27.7 | 26.4 | 29.4 us)
+// Row tiles that a wave works on side by side (1 | 2 | 4: 5 x 8191, 32 queries, 25.1 | 23.4 | 35.3 us, 16 x 2048 of 32 heads of 32, 8 queries,
+// 24.9 | 24.4 | 28.1, 8 x 4096 of 12 of 64, 16 queries, 8 bits, 16.0 | 18.5 | 18.4).
+constexpr int kSide = 2;
 
 // Row tiles whose digits lie in LDS at one time; more go through the tokens several times (16 | 32, and two workgroups per compute
-// unit instead of three: 5 x 8191, 32 queries, 23.7 | 29.2 us).
+// unit instead of three: 5 x 8191, 32 queries, 23.4 | 29.8 us).
 __host__ __device__ constexpr int held_tiles(int blocks) { return blocks == 2 ? 8 : 16; }
 
 // A token's weight is rounded to fp32 once for every time that its head's row tiles go through LDS.  In windows of more such passes (half a step
@@ -199,8 +204,9 @@ __global__ void __launch_bounds__(256) query_digits_kernel(WeightArgs a, WeightP
 
 // NB: blocks of a unit; HEADS: key/value heads of a unit; MADE: the queries' digits are in the workspace; STREAM: keys are read past the
 // last-level cache; CARRY: what sums lose is kept (in the kernel of all windows it cost registers, and spills in three of them).  Three waves per
-// SIMD where their registers suffice, nearly (four instead: spills, or 23.4 -> 29.5 us); digits made, several heads: two (16 x 2048 of 32 heads
-// of 32, 8 queries, 30.2 -> 24.6 us; 8 x 4096 of 12 of 64, 16 queries, 8 bits 20.1 -> 18.6), made here: three (20.0, two 21.4).
+// SIMD where their registers suffice, nearly (four instead: spills, or 23.4 -> 28.7 us); digits made, several heads: two (16 x 2048 of 32 heads
+// of 32, 8 queries, 29.9 -> 24.4 us; 8 x 4096 of 12 of 64, 16 queries, 8 bits 20.1 -> 18.5), made here: three, with spills at heads of 32 (16 x 4096 of 32 at
+// 4 bits 19.8, two 21.5; at 3 bits 17.6 | 21.3).
 template <int BITS, int NB, int HEADS, bool MADE, bool STREAM, bool CARRY>
 __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 32) ? 2 : 3) attend_weights_kernel(WeightArgs a, WeightPlan plan) {
   constexpr int kRow = 16 * BITS;                          // bytes of a token's row in a block
@@ -352,7 +358,7 @@ __global__ void __launch_bounds__(256, NB == 2 || BITS * HEADS >= (MADE ? 12 : 3
       for (int r = 0; r < 4; ++r) token_r[r] = here >> r & 1 ? token + r * 16 + n16 : 0x7fffffff;
 
       const bool whole = (here & 15) == 15 && token + kTile <= len - (a.queries - 1) && full_rows;
-      // Adds the weights of row tiles from .. to - 1 to `sum`; the next one's rows are read while one is worked on.
+      // Adds the weights of row tiles from .. to - 1 to `sum`, kSide of them side by side where their digits were made before.
       auto add_up = [&](int from, int to, float (&sum)[4], auto&& seen) __attribute__((always_inline)) {
         struct Operands {
           QueryRow row;

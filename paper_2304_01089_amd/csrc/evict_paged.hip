@@ -13,7 +13,7 @@
 // Few moves are done by the same workgroup, many by a second launch over the whole chip.
 // What bounds it: a chain of short steps, each of one to three thousand cycles and most of them across the workgroup's waves: 7
 // sequences of 1531 tokens, 2 heads of 256, budget 700 take 10.3 us (moves 6300 of 18500 cycles, keys and bins 2400, the search
-// 3400).  Long sequences: one compute unit's LDS and instructions per head: 4 of 32768 tokens, 8 heads, budget 4096 take 36.5 us, 28 in
+// 3400).  Long sequences: one compute unit's LDS and instructions per head: 4 of 32768 tokens, 8 heads, budget 4096 take 36.4 us, 28 in
 // the first kernel (of 45000 cycles of a head in the middle 11000 are keys and bins, 7000 the later looks, 18000 votes and lists), 7.8 in the moves.
 #include <hip/hip_runtime.h>
 
@@ -31,9 +31,11 @@ constexpr int kFirstBins = 4096, kLaterBins = 1024;              // of twelve an
 // sixteen up to 8192; they lie in LDS up to 32 of a lane (32768 tokens); longer sequences' are made anew from their records.
 constexpr int kFewItems = 8;
 constexpr int kLdsItems = 32;
-constexpr int kFewMovers = 16;                 // of an item, up to which a lane writes them down by itself (always: 4 x 32768 38.9 us; up to 8, 16 or 32: 36.7)
+// Movers of an item, up to which a lane writes them down by itself (always | up to 8 | 16 | 32: 4 x 32768 39.2 | 36.6 | 36.4 | 36.4 us, 16 x 10000 to
+// 4096, 8 heads, 54.9 | 49.8 | 50.7 | 53.9).
+constexpr int kFewMovers = 16;
 constexpr int kHeldPages = 1024;               // page numbers of a sequence that are kept at hand
-constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them (512 | 2048: 16 x 4000 to 2000, 8 heads, 18.7 | 16.7 us)
+constexpr int kFewMoves = 2048;                // of a head at most where the workgroup that finds them does them (512 | 2048: 16 x 4000 to 2000, 8 heads, 19.1 | 17.1 us)
 constexpr int kMoveChunks = 1024;              // workgroups of a head there at most
 constexpr uint32_t kSafe = 0xffffffffu, kNanKey = 0xfffffffeu;
 
@@ -166,7 +168,7 @@ enum class Keys { registers, lds, made };      // where a token's key is when it
 // WAVES: of the workgroup
 template <int WAVES, Keys KEYS>
 __global__ void __launch_bounds__(WAVES * 64) evict_select_kernel(EvictArgs a, EvictPlan plan) {
-  constexpr int kRun = KEYS == Keys::registers ? kFewItems : 16;             // of its items a lane works on so many together (8 | 16 | 32: 4 x 32768 40.1 | 38.7 | 40.6 us)
+  constexpr int kRun = KEYS == Keys::registers ? kFewItems : 16;             // of its items a lane works on so many together (8 | 16 | 32: 4 x 32768 37.6 | 36.4 | 38.0 us)
   constexpr int kThreads = WAVES * 64, kKeys = KEYS == Keys::lds ? kThreads * kLdsItems : 1;
   constexpr int kAllBins = kFirstBins + 2 * kLaterBins;
   __shared__ __align__(16) int32_t bins[kAllBins];             // (later the lists of a few moves)

@@ -5,9 +5,9 @@
 // and has the constants of its 16 positions in registers.  A lane loads two pieces of eight channels that rotate together (half
 // style: eight and their partners; interleaved: sixteen side by side), takes the eight cosines and sines from LDS, where the
 // wave has put the row's, one pair per lane and once for the wave's heads, and writes fp32.
-// What bounds it: memory, as without the rotation: 8192 tokens of 40 heads of 128, queries included, take 82 us for 378 MB at 4 bits,
-// 4.6 TB/s.  One token: 3.9 us, a launch and a chain of dependent loads (slot and table, rows, positions); the host takes 4.5.
-// (76 registers; held to four workgroups per compute unit it spills: 163 us.)
+// What bounds it: memory, as without the rotation: 8192 tokens of 40 heads of 128, queries included, take 82.7 us for 378 MB at 4 bits,
+// 4.6 TB/s.  One token: 3.9 us, a launch and a chain of dependent loads (slot and table, rows, positions); the host takes 4.8.
+// (150 registers, three workgroups per compute unit; held to four it spills: 163 us.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,7 @@ namespace rptq {
 
 struct RopeQuantLaunch {
   PagedLaunch kv;
-  RopeLaunch q;                                      // (the launch's last q.groups workgroups are the queries'; first 89 | last 84 us, 8192 x 40 x 128 at 4 bits)
+  RopeLaunch q;                                      // (the launch's last q.groups workgroups are the queries'; first 88.6 | last 82.7 us, 8192 x 40 x 128 at 4 bits)
   const int32_t* positions;
   const double* freqs;
   double amplitude;

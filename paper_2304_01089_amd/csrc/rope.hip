@@ -5,10 +5,10 @@
 // A workgroup takes a few rows: first their cosines and sines, one per thread, into LDS, then all heads of the rows, every thread
 // a piece of up to 16 bytes (half style: two, W channels and their W partners).  The angles are thus computed once per row
 // and group of heads and read from memory never.
-// What bounds it: memory: 8192 rows of 80 heads of 128 take 69 us for 336 MB, 4.8 TB/s of as many bytes read as written (a copy reaches
+// What bounds it: memory: 8192 rows of 80 heads of 128 take 69.9 us for 336 MB, 4.8 TB/s of as many bytes read as written (a copy reaches
 // 5.15).  Few rows: the launch and two dependent loads, 2.4 us for one row, of which an empty launch is 1.8.
-// Rows of a workgroup: 2 | 4 | 8 66.4 | 67.2 | 68.3 us here and 83.5 | 81.6 | 82.6 in front of the cache.  Not kept: two or four pieces a
-// thread requested ahead (69.1, 68.1), non-temporal loads and stores (no change).
+// Rows of a workgroup: 2 | 4 | 8 69.2 | 69.9 | 71.0 us here and 85.0 | 82.7 | 84.6 in front of the cache.  Not kept: two or four pieces a
+// thread requested ahead (3 and 1 % more), non-temporal loads and stores (no change).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

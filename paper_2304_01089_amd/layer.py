@@ -294,7 +294,7 @@ class Rotary:
 def rotary(rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None, factor: float = 1.0, trained: float = 0.0,
            slow: float = 1.0, fast: float = 32.0, device="cuda") -> Rotary:
     """Frequencies base^(-2 j / rotary_dim), for contexts longer than the trained one scaled as rptq_rope_freqs says ("linear", "base",
-    "parts")."""
+    "parts").  "parts" comes with an amplitude of 0.1 log(factor) + 1; a model that has another one sets the result's."""
     import torch
     freqs, amplitude = B.rptq_rope_freqs(rotary_dim, base, scaling, factor, trained, slow, fast)
     return Rotary(rotary_dim, torch.from_numpy(freqs).to(device), amplitude, interleaved)
